@@ -42,27 +42,27 @@ def _product(name, op, tokens, workers, experts, width, out, dtype, skew):
 def listed():
     return [
         # a short step of one worker: sixteen tokens of GPT-2 small's width, where the call itself is what counts
-        _dropout("dropout, 16 tokens", 16, 768, "bf16", 0.1),
+        _dropout("dropout 16", 16, 768, "bf16", 0.1),
         # attention and feed-forward dropout of a long step in full precision
-        _dropout("dropout, 16384 tokens f32", 16384, 2048, "f32", 0.2),
+        _dropout("dropout 16384 f32", 16384, 2048, "f32", 0.2),
         # the sublayer's end for eight workers with sixteen tokens each: dropout, residual sum, layer norm
-        _norm("norm, 128 tokens", "norm", 128, 768, "bf16", "bf16", 0.1, 8),
+        _norm("norm 128", "norm", 128, 768, "bf16", "bf16", 0.1, 8),
         # a layer norm alone on an odd width (a pruned or probed model), full precision
-        _norm("norm alone, odd f32", "norm", 6007, 1023, "f32", "", 0.0, 4),
+        _norm("norm alone odd f32", "norm", 6007, 1023, "f32", "", 0.0, 4),
         # eight workers' long batches, the residual stream held in binary32 beside bf16 activations
-        _norm("norm, 32768 tokens", "norm", 32768, 1024, "bf16", "f32", 0.1, 8),
+        _norm("norm 32768", "norm", 32768, 1024, "bf16", "f32", 0.1, 8),
         # the gradients of the two fused cases
-        _norm("norm gradient, 128 tokens", "norm_grad", 128, 768, "bf16", "bf16", 0.1, 8),
-        _norm("norm gradient, 32768 tokens", "norm_grad", 32768, 1024, "bf16", "bf16", 0.1, 8),
+        _norm("norm gradient 128", "norm_grad", 128, 768, "bf16", "bf16", 0.1, 8),
+        _norm("norm gradient 32768", "norm_grad", 32768, 1024, "bf16", "bf16", 0.1, 8),
         # a few tokens for each of eight experts: the experts' weights are all there is to read
-        _product("experts, 96 tokens", "product", 96, 1, 8, 768, 1024, "bf16", 0.5),
+        _product("experts 96", "product", 96, 1, 8, 768, 1024, "bf16", 0.5),
         # a long step of four workers over sixteen experts
-        _product("experts, 32768 tokens", "product", 32768, 4, 16, 2048, 2304, "bf16", 0.3),
+        _product("experts 32768", "product", 32768, 4, 16, 2048, 2304, "bf16", 0.3),
         # the gradient to the tokens, odd sizes that no 16-byte row divides
-        _product("experts dx, odd f16", "product_dx", 5003, 2, 6, 777, 1030, "f16", 1.0),
+        _product("experts dx odd f16", "product_dx", 5003, 2, 6, 777, 1030, "f16", 1.0),
         # weight gradients into the rows of eight workers: a short, skewed step and a long one
-        _product("experts dw, 1000 tokens", "product_dw", 1000, 4, 4, 768, 768, "bf16", 1.5),
-        _product("experts dw, 32768 tokens", "product_dw", 32768, 8, 4, 1024, 2304, "bf16", 0.3),
+        _product("experts dw 1000", "product_dw", 1000, 4, 4, 768, 768, "bf16", 1.5),
+        _product("experts dw 32768", "product_dw", 32768, 8, 4, 1024, 2304, "bf16", 0.3),
     ]
 
 
