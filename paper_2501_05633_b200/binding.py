@@ -7,7 +7,9 @@ from __future__ import annotations
 
 import ctypes
 import os
+import shutil
 import subprocess
+import tempfile
 from typing import Optional, Tuple
 
 import torch
@@ -17,6 +19,9 @@ _ROOT = os.path.dirname(_PKG)
 _SRC = os.path.join(_PKG, "csrc", "regtopk.cu")
 _INC = os.path.join(_ROOT, "include")
 _LIB = os.path.join(_PKG, "libregtopk.so")
+_TRAIN_SRC = [os.path.join(_PKG, "csrc", name) for name in ("dropout_norm.cu",)]
+_TRAIN_DEPS = [os.path.join(_PKG, "csrc", "train_common.cuh"), os.path.join(_INC, "regtopk_train.h"), os.path.join(_INC, "regtopk.h")]
+_TRAIN_LIB = os.path.join(_PKG, "libregtopk_train.so")
 
 OK = 0
 GRAD_F32, GRAD_BF16 = 0, 1
@@ -51,8 +56,32 @@ def library_path() -> str:
     return _LIB
 
 
+def build_training(force: bool = False, verbose: bool = False) -> str:
+    """Compile the training operators' sources for sm_100a into libregtopk_train.so, side by side."""
+    if not force and os.path.exists(_TRAIN_LIB) and os.path.getmtime(_TRAIN_LIB) >= max(
+            os.path.getmtime(f) for f in _TRAIN_SRC + _TRAIN_DEPS):
+        return _TRAIN_LIB
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-I", _INC, "-Xcompiler", "-fPIC"]
+    if verbose:
+        flags.insert(0, "-Xptxas=-v")
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in _TRAIN_SRC]
+        runs = [subprocess.Popen(["nvcc", *flags, "-c", "-o", o, f]) for f, o in zip(_TRAIN_SRC, objects)]
+        for run in runs:
+            run.wait()
+        for run in runs:
+            if run.returncode:
+                raise subprocess.CalledProcessError(run.returncode, run.args)
+        made = os.path.join(tmp, "libregtopk_train.so")
+        subprocess.run(["nvcc", *flags, "--shared", "-o", made, *objects], check=True)
+        shutil.move(made, _TRAIN_LIB)
+    return _TRAIN_LIB
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile csrc/regtopk.cu for sm_100a into the package directory (nvcc cross-compiles without a GPU)."""
+    """Compile csrc/regtopk.cu for sm_100a into the package directory (nvcc cross-compiles without a GPU), and the
+    training operators beside it."""
+    build_training(force, verbose)
     if not force and os.path.exists(_LIB) and os.path.getmtime(_LIB) >= max(
             os.path.getmtime(_SRC), os.path.getmtime(os.path.join(_INC, "regtopk.h"))):
         return _LIB
