@@ -88,6 +88,40 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
                                 int32_t stream_type, const regtopk_dropout_params* drop, void* workspace,
                                 size_t workspace_bytes, void* cuda_stream);
 
+/* Products of rows with the matrix of their group (the tokens of each expert with that expert's weights):
+ *   y[t] = w[g mod weights] x[t]   for the rows t of group g; a row of no group gets zeros.
+ * x [rows][k] and y [rows][m] of `type`, which is BF16 or F16; w holds `weights` matrices, element (i, j) of matrix e at
+ * w[e * w_stride + i * ldw + j].  transposed == 0: matrices [m][k], as a linear layer keeps them.  transposed != 0:
+ * matrices [k][m], used as y[t] = x[t] w: with dy for x and the layer's own [m][k] matrices this is the gradient to the
+ * tokens.  groups is a multiple of weights: groups sorted by (worker, expert) share the experts' matrices.
+ * Products and sums are binary32 on the tensor cores; y is rounded once.  rows < 2^31; k, m < 2^31; k == 0 gives zeros.
+ * workspace: 16-byte aligned, at least regtopk_grouped_matmul_workspace_bytes(...) bytes, which are 0 where x and w have
+ * 16-byte aligned rows (base and leading dimension; for w the stride between matrices too) and otherwise hold a copy of
+ * the one that has not.  Errors: INVALID_ARG, TOO_LARGE (groups), WORKSPACE_TOO_SMALL, NO_DEVICE, CUDA. */
+size_t regtopk_grouped_matmul_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride,
+                                              int32_t transposed, int32_t weights, int64_t rows, int64_t k, int64_t m);
+int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride, int32_t transposed,
+                           int32_t weights, void* y, int64_t ldy, const int64_t* offsets, int32_t groups, int64_t rows,
+                           int64_t k, int64_t m, int32_t type, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The gradient of such products to the matrices, for each group on its own:
+ *   out[g] (+)= sum over the rows t of group g of dy[t] x[t]^T, an [m][k] matrix; a group without rows gives zeros.
+ * dy [rows][m] and x [rows][k] of `type` (BF16 or F16); out binary32, element (i, j) of group g = n * inner + e at
+ * out[n * outer_stride + e * inner_stride + i * ld_out + j]: with inner experts and groups sorted by (worker, expert) this is
+ * each worker's own row of a flat gradient.  accumulate != 0 adds to what out holds, one rounded addition per element.
+ * workspace as above, by regtopk_grouped_matmul_dw_workspace_bytes.  Errors as above. */
+size_t regtopk_grouped_matmul_dw_workspace_bytes(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t groups,
+                                                 int64_t rows, int64_t k, int64_t m);
+int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, float* out, int64_t ld_out,
+                              int64_t inner_stride, int64_t outer_stride, int32_t inner, int32_t accumulate,
+                              const int64_t* offsets, int32_t groups, int64_t rows, int64_t k, int64_t m, int32_t type,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Synchronises the stream.  REGTOPK_OK, REGTOPK_ERR_CUDA, or REGTOPK_ERR_INTERNAL if a product's kernel on the current
+ * device ever gave up waiting for its own copies or tensor core work (every such wait ends after two seconds; the
+ * outputs of that call are then incomplete).  The internal error stays set until the process ends. */
+int regtopk_train_status(void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

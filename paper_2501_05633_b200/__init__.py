@@ -6,4 +6,4 @@ contains none of the method's arithmetic.  `training` marshals into the calls of
 operators of a backward pass that fills the sparsifier's accumulator rows (csrc/dropout_norm.cu, csrc/grouped_matmul.cu).
 """
 from .binding import RegTopK, RegTopKError, aggregate_pairs_static, build, load_library, library_path  # noqa: F401
-from .training import dropout, layer_norm, layer_norm_backward  # noqa: F401
+from .training import dropout, grouped_matmul, grouped_matmul_dw, layer_norm, layer_norm_backward, training_status  # noqa: F401

@@ -19,7 +19,7 @@ _ROOT = os.path.dirname(_PKG)
 _SRC = os.path.join(_PKG, "csrc", "regtopk.cu")
 _INC = os.path.join(_ROOT, "include")
 _LIB = os.path.join(_PKG, "libregtopk.so")
-_TRAIN_SRC = [os.path.join(_PKG, "csrc", name) for name in ("dropout_norm.cu",)]
+_TRAIN_SRC = [os.path.join(_PKG, "csrc", name) for name in ("dropout_norm.cu", "grouped_matmul.cu")]
 _TRAIN_DEPS = [os.path.join(_PKG, "csrc", "train_common.cuh"), os.path.join(_INC, "regtopk_train.h"), os.path.join(_INC, "regtopk.h")]
 _TRAIN_LIB = os.path.join(_PKG, "libregtopk_train.so")
 

@@ -1,0 +1,774 @@
+// Products of tokens with the matrices of their experts, ragged groups, and the gradients to the matrices
+// (include/regtopk_train.h), on the fifth-generation tensor cores.
+//
+// Both kernels are persistent, one block per SM: a thread that issues TMA copies, a thread that issues tcgen05.mma on
+// the tiles that have landed, and a warp group that writes finished accumulators while the next tile is multiplied.
+//
+//   k_rows     D[128 output features][up to 256 tokens] = W[features][k] X[tokens][k]^T.  The features, which are a
+//              whole number of tiles, take the fixed 128 lanes; the tokens of a group, of which there may be any number,
+//              take the columns, whose count the instruction chooses in steps of 16.  A lane then holds one feature,
+//              so that a warp writes consecutive elements of one token's row.
+//   k_weights  D[128 columns of x][up to 256 columns of dy] = sum over tokens; a lane holds one column of x, so that a
+//              warp writes (or adds to) consecutive elements of one row of the gradient at any alignment.
+//
+// Tiles lie in shared memory in the 128-byte swizzle, copied in boxes that are 64 elements (128 bytes) wide.
+
+#include <cuda.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "train_common.cuh"
+
+namespace {
+
+// ---- PTX -------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ u32 smem_at(const void* p) { return (u32)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+__device__ __forceinline__ void bar_expect(u32 bar, u32 bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_done(u32 bar, u32 parity) {
+  u32 ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+
+// Every wait ends: after two seconds the block gives up, says so here, and leaves (regtopk_train_status).
+__device__ unsigned int g_gave_up;
+constexpr uint64_t kPatienceNs = 2000000000ull;
+
+__device__ __noinline__ bool bar_wait_long(u32 bar, u32 parity, volatile u32* quit) {
+  const uint64_t began = now_ns();
+  while (!bar_done(bar, parity)) {
+    if (*quit) return false;
+    if (now_ns() - began > kPatienceNs) {
+      *quit = 1;
+      atomicExch(&g_gave_up, 1u);
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, volatile u32* quit) {
+  return bar_done(bar, parity) || bar_wait_long(bar, parity, quit);
+}
+
+__device__ __forceinline__ void tma_2d(u32 to, const CUtensorMap* map, u32 bar, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_3d(u32 to, const CUtensorMap* map, u32 bar, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void mma(u32 d, uint64_t a, uint64_t b, u32 how, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((u32)add) : "memory");
+}
+__device__ __forceinline__ void mma_commit(u32 bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 32 accumulator columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_read(float (&v)[32], u32 at) {
+  u32 r[32];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(at) : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// 16 of them.
+__device__ __forceinline__ void tmem_read16(float (&v)[16], u32 at) {
+  u32 r[16];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at) : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// ---- descriptors -----------------------------------------------------------------------------------------------------
+// Shared memory operand in the 128-byte swizzle: start, distance of 64-element blocks along the operand's own rows
+// (used where those are the contiguous dimension), distance of groups of eight swizzled lines, both in bytes.
+__device__ __forceinline__ uint64_t operand(u32 at, u32 leading, u32 stride) {
+  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+constexpr int kBox = 64;                   // elements of a line of a box: 128 bytes
+constexpr int kDepth = 64;                 // of the summed dimension in a stage
+constexpr int kBoxBytes = kBox * kDepth * 2;
+constexpr int kLanes = 128;                // accumulator lanes: the fixed side of a tile
+
+// Instruction descriptor: binary32 accumulators, both operands of one 16-bit type, 128 lanes, `columns` columns; _mn: the
+// operand's own rows, not the summed dimension, are contiguous.
+__device__ __forceinline__ u32 instruction(bool bf16, bool a_mn, bool b_mn, int columns) {
+  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (u32)a_mn << 15 | (u32)b_mn << 16 | (u32)(columns >> 3) << 17 | (u32)(kLanes >> 4) << 24;
+}
+
+constexpr int kThreads = 256;  // warp 0 copies, warp 1 multiplies, warp 2 keeps the TMEM, warp 3 clears, warps 4-7 write
+
+template <int kStages> struct Shared {
+  uint64_t full[kStages], empty[kStages], done[2], free_[2], last;
+  u32 tmem, quit;
+};
+
+template <int kStages> __device__ __forceinline__ void set_up(Shared<kStages>& sh, int tmem_columns, int readers) {
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      bar_init(smem_at(&sh.full[i]), 1);
+      bar_init(smem_at(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(smem_at(&sh.done[i]), 1);
+      bar_init(smem_at(&sh.free_[i]), readers);
+    }
+    bar_init(smem_at(&sh.last), 1);
+    sh.quit = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x >> 5 == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&sh.tmem)), "r"(tmem_columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+}
+template <int kStages> __device__ __forceinline__ void tear_down(Shared<kStages>& sh, int tmem_columns) {
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (threadIdx.x >> 5 == 2)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(tmem_columns));
+}
+
+// The copying thread's way through the stages: `turn` counts stages filled so far.
+// After the last one it waits until every stage that was filled has landed and been used, so that nothing is under
+// way when the block ends; if the block has given up, until what was requested has landed.
+template <int kStages> __device__ __forceinline__ void drain(Shared<kStages>& sh, u32 turn) {
+  volatile u32* quit = &sh.quit;
+  const u32 from = turn > (u32)kStages ? turn - kStages : 0;
+  for (u32 t = from; t < turn; ++t) {
+    u32 never = 0;
+    const u32 s = t % kStages, parity = (t / kStages) & 1;
+    if (*quit || !bar_wait(smem_at(&sh.empty[s]), parity, quit)) bar_wait(smem_at(&sh.full[s]), parity, &never);
+  }
+}
+
+// The multiplying thread, when the block has given up: no product may be under way when the block ends.
+template <int kStages> __device__ __forceinline__ void settle(Shared<kStages>& sh) {
+  u32 never = 0;
+  mma_commit(smem_at(&sh.last));
+  bar_wait(smem_at(&sh.last), 0, &never);
+}
+
+__device__ __forceinline__ int64_t limited(int64_t v, int64_t rows) { return v < 0 ? 0 : v > rows ? rows : v; }
+
+// ---- y[t] = w x[t] -----------------------------------------------------------------------------------------------------
+struct RowsArgs {
+  const int64_t* offsets;
+  void* y;
+  int64_t ldy;
+  int groups, weights, rows, k, m;
+  int shared_weights;  // all matrices are the first one
+  int pairs;           // two neighbouring elements of y may be written as one word
+};
+
+constexpr int kTableGroups = REGTOPK_MATMUL_MAX_GROUPS;
+
+// How a group's rows are cut: as many tiles as the widest allows, all of one size but the last.
+__device__ __forceinline__ int tile_rows(int count, int most) {
+  const int tiles = (count + most - 1) / most;
+  return tiles ? ((count + tiles - 1) / tiles + 15) & ~15 : 16;
+}
+
+struct RowTile { int group, row, count, feature; };
+
+template <int kMost>
+__device__ __forceinline__ RowTile row_tile(int64_t id, int feature_tiles, const int* before, const int* start, const int* end, int groups) {
+  const int at = (int)(id / feature_tiles);
+  int lo = 0, hi = groups;  // the last group with before[g] <= at
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (before[mid] <= at) lo = mid; else hi = mid;
+  }
+  const int step = tile_rows(end[lo] - start[lo], kMost);
+  RowTile t;
+  t.group = lo;
+  t.row = start[lo] + (at - before[lo]) * step;
+  t.count = min(step, end[lo] - t.row);
+  t.feature = (int)(id - (int64_t)at * feature_tiles) * kLanes;
+  return t;
+}
+
+template <int kMost> struct RowStage {
+  static constexpr int kBytesA = kLanes * kDepth * 2, kBytes = kBytesA + kMost * kDepth * 2;
+  static constexpr int kCount = kMost == 256 ? 4 : kMost == 128 ? 6 : kMost == 64 ? 8 : 9;
+  static constexpr int kSmem = kCount * kBytes + 1024;
+};
+
+template <typename T, int kMost, bool kTransposed>
+__global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const RowsArgs a) {
+  constexpr int kStages = RowStage<kMost>::kCount, kBytesA = RowStage<kMost>::kBytesA, kBytes = RowStage<kMost>::kBytes;
+  constexpr int kBoxRows = kMost < 64 ? kMost : 64;  // tokens of one copy
+  constexpr int kTmem = 2 * kMost;
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  extern __shared__ uint8_t raw[];
+  __shared__ Shared<kStages> sh;
+  __shared__ int before[kTableGroups + 1], start[kTableGroups], end[kTableGroups];
+  __shared__ int scan[kThreads / 32];
+  const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  set_up(sh, kTmem, 4);
+  // where each group's rows lie and how many tiles come before it
+  constexpr int kPer = (kTableGroups + kThreads - 1) / kThreads;
+  {
+    int own[kPer], sum = 0;
+    const int per = (a.groups + kThreads - 1) / kThreads;
+    for (int i = 0; i < per; ++i) {
+      const int g = threadIdx.x * per + i;
+      own[i] = 0;
+      if (g < a.groups) {
+        const int lo = (int)limited(a.offsets[g], a.rows);
+        int hi = (int)limited(a.offsets[g + 1], a.rows);
+        if (hi < lo) hi = lo;
+        start[g] = lo;
+        end[g] = hi;
+        const int step = tile_rows(hi - lo, kMost);
+        own[i] = (hi - lo + step - 1) / step;
+        sum += own[i];
+      }
+    }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(kAll, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += scan[w];
+    upto -= sum;
+    for (int i = 0; i < per; ++i) {
+      const int g = threadIdx.x * per + i;
+      if (g < a.groups) {
+        before[g] = upto;
+        upto += own[i];
+        if (g == a.groups - 1) before[a.groups] = upto;
+      }
+    }
+    __syncthreads();
+  }
+  const int feature_tiles = (a.m + kLanes - 1) / kLanes, depth = (a.k + kDepth - 1) / kDepth;
+  const int64_t tiles = (int64_t)before[a.groups] * feature_tiles;
+  volatile u32* quit = &sh.quit;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      u32 turn = 0;
+      bool go = true;
+      for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x) {
+        const RowTile t = row_tile<kMost>(id, feature_tiles, before, start, end, a.groups);
+        const int e = a.shared_weights ? 0 : t.group % a.weights;
+        const int boxes = (t.count + kBoxRows - 1) / kBoxRows;
+        for (int d = 0; d < depth; ++d, ++turn) {
+          const u32 s = turn % kStages, parity = (turn / kStages) & 1;
+          if (!(go = bar_wait(smem_at(&sh.empty[s]), parity ^ 1, quit))) break;
+          const u32 at = tiles_at + s * kBytes, bar = smem_at(&sh.full[s]);
+          bar_expect(bar, kBytesA + boxes * kBoxRows * kDepth * 2);
+          if (kTransposed) {
+            tma_3d(at, &w_map, bar, t.feature, d * kDepth, e);
+            tma_3d(at + kBoxBytes, &w_map, bar, t.feature + kBox, d * kDepth, e);
+          } else {
+            tma_3d(at, &w_map, bar, d * kDepth, t.feature, e);
+          }
+          for (int i = 0; i < boxes; ++i)
+            tma_2d(at + kBytesA + i * kBoxRows * kDepth * 2, &x_map, bar, d * kDepth, t.row + i * kBoxRows);
+        }
+      }
+      drain(sh, turn);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      u32 turn = 0, n = 0;
+      bool go = true;
+      for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x, ++n) {
+        const RowTile t = row_tile<kMost>(id, feature_tiles, before, start, end, a.groups);
+        const u32 how = instruction(kBf16, kTransposed, false, (t.count + 15) & ~15);
+        const u32 acc = sh.tmem + (n & 1) * kMost;
+        if (!(go = bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit))) break;
+        tmem_fence_after();
+        for (int d = 0; d < depth; ++d, ++turn) {
+          const u32 s = turn % kStages;
+          if (!(go = bar_wait(smem_at(&sh.full[s]), (turn / kStages) & 1, quit))) break;
+          tmem_fence_after();
+          const u32 at = tiles_at + s * kBytes;
+          const int steps = (min(kDepth, a.k - d * kDepth) + 15) >> 4;
+          for (int i = 0; i < steps; ++i)
+            mma(acc, kTransposed ? operand(at + i * 2048, kBoxBytes, 1024) : operand(at + i * 32, 0, 1024),
+                operand(at + kBytesA + i * 32, 0, 1024), how, d | i);
+          mma_commit(smem_at(&sh.empty[s]));
+        }
+        if (go) mma_commit(smem_at(&sh.done[n & 1]));
+      }
+      if (!go) settle(sh);
+    }
+  } else if (warp == 3) {  // rows of no group
+    const int64_t head = a.groups ? limited(a.offsets[0], a.rows) : a.rows, tail = limited(a.offsets[a.groups], a.rows);
+    T* y = static_cast<T*>(a.y);
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+      if (row >= head && row < tail) {
+        row += (tail - 1 - row) / gridDim.x * gridDim.x;  // on to the last one before the tail
+        continue;
+      }
+      for (int c = lane; c < a.m; c += 32) y[row * a.ldy + c] = from_float<T>(0.0f);
+    }
+  } else if (warp >= 4) {
+    u32 n = 0;
+    const int part = warp & 3;  // the lanes of the accumulator that this warp may read
+    T* y = static_cast<T*>(a.y);
+    for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x, ++n) {
+      const RowTile t = row_tile<kMost>(id, feature_tiles, before, start, end, a.groups);
+      if (!__all_sync(kAll, bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit))) break;
+      tmem_fence_after();
+      const int f = t.feature + part * 32 + lane;
+      T* to = y + (int64_t)t.row * a.ldy + f;
+      for (int c0 = 0; c0 < t.count; c0 += 32) {
+        float v[32];
+        tmem_read(v, sh.tmem + (n & 1) * kMost + c0 + ((u32)(part * 32) << 16));
+        if (a.pairs) {  // lanes of a pair of features exchange halves of two tokens, and each writes one token's pair
+          const bool odd = lane & 1;
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            const float other = __shfl_xor_sync(kAll, odd ? v[c] : v[c + 1], 1);
+            T two[2] = {from_float<T>(odd ? other : v[c]), from_float<T>(odd ? v[c + 1] : other)};
+            const int row = c0 + c + odd;
+            if (row < t.count && f < a.m) *reinterpret_cast<u32*>(to + (int64_t)row * a.ldy - odd) = *reinterpret_cast<u32*>(two);
+          }
+        } else if (f < a.m) {
+#pragma unroll
+          for (int c = 0; c < 32; ++c)
+            if (c0 + c < t.count) to[(int64_t)(c0 + c) * a.ldy] = from_float<T>(v[c]);
+        }
+      }
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_at(&sh.free_[n & 1]));
+    }
+  }
+  tear_down(sh, kTmem);
+}
+
+// ---- out[g] (+)= sum of dy[t] x[t]^T -------------------------------------------------------------------------------------
+struct WeightsArgs {
+  const int64_t* offsets;
+  float* out;
+  int64_t ld_out, inner_stride, outer_stride;
+  int groups, inner, rows, k, m, accumulate;
+};
+
+constexpr int kWeightsThreads = 384;  // as above, with eight warps that write: two for each quarter of the lanes
+// Tokens that one accumulator sums.  The tensor core cuts the running sum off at every step of sixteen products
+// instead of rounding it, so its error grows with the number of steps and always to the same side: 1.8e-5 of the result
+// after 6,000 tokens of one sign.  After this many tokens the sum moves on to registers, where additions round.
+constexpr int kWeightsChain = 256;
+constexpr int kWeightsMost = 256, kWeightsStages = 4;
+constexpr int kWeightsBytesA = kLanes * kDepth * 2, kWeightsStageBytes = kWeightsBytesA + kWeightsMost * kDepth * 2;
+constexpr int kWeightsSmem = kWeightsStages * kWeightsStageBytes + 1024;
+
+struct WeightTile { int group, row, count, k, m, columns; };
+
+__device__ __forceinline__ WeightTile weight_tile(int64_t id, const WeightsArgs& a, int k_tiles, int m_tiles) {
+  WeightTile t;
+  const int per = k_tiles * m_tiles;
+  t.group = (int)(id / per);
+  const int in = (int)(id - (int64_t)t.group * per);
+  t.m = in / k_tiles * kWeightsMost;
+  t.k = in % k_tiles * kLanes;
+  t.columns = min(kWeightsMost, a.m - t.m);
+  t.row = (int)limited(a.offsets[t.group], a.rows);
+  const int end = (int)limited(a.offsets[t.group + 1], a.rows);
+  t.count = max(end - t.row, 0);
+  return t;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kWeightsThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
+  constexpr int kStages = kWeightsStages, kMost = kWeightsMost, kTmem = 2 * kMost;
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  extern __shared__ uint8_t raw[];
+  __shared__ Shared<kStages> sh;
+  const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  set_up(sh, kTmem, 8);
+  const int k_tiles = (a.k + kLanes - 1) / kLanes, m_tiles = (a.m + kMost - 1) / kMost;
+  const int64_t tiles = (int64_t)a.groups * k_tiles * m_tiles;
+  volatile u32* quit = &sh.quit;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      u32 turn = 0;
+      bool go = true;
+      for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x) {
+        const WeightTile t = weight_tile(id, a, k_tiles, m_tiles);
+        const int boxes = (t.columns + kBox - 1) / kBox;
+        for (int d = 0; d < t.count; d += kDepth, ++turn) {
+          const u32 s = turn % kStages;
+          if (!(go = bar_wait(smem_at(&sh.empty[s]), ((turn / kStages) & 1) ^ 1, quit))) break;
+          const u32 at = tiles_at + s * kWeightsStageBytes, bar = smem_at(&sh.full[s]);
+          bar_expect(bar, kWeightsBytesA + boxes * kBoxBytes);
+          tma_2d(at, &x_map, bar, t.k, t.row + d);
+          tma_2d(at + kBoxBytes, &x_map, bar, t.k + kBox, t.row + d);
+          for (int i = 0; i < boxes; ++i) tma_2d(at + kWeightsBytesA + i * kBoxBytes, &dy_map, bar, t.m + i * kBox, t.row + d);
+        }
+      }
+      drain(sh, turn);
+    }
+  } else if (warp == 1) {
+    u32 turn = 0, n = 0;
+    bool go = true;
+    for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x) {
+      const WeightTile t = weight_tile(id, a, k_tiles, m_tiles);
+      if (!t.count) continue;
+      const u32 how = instruction(kBf16, true, true, (t.columns + 15) & ~15);
+      for (int d = 0; d < t.count; d += kDepth, ++turn) {
+        const u32 acc = sh.tmem + (n & 1) * kMost;
+        const bool begins = d % kWeightsChain == 0, ends = (d + kDepth) % kWeightsChain == 0 || d + kDepth >= t.count;
+        if (begins) {
+          if (!(go = __all_sync(kAll, bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit)))) break;
+          tmem_fence_after();
+        }
+        const u32 s = turn % kStages;
+        if (!(go = __all_sync(kAll, bar_wait(smem_at(&sh.full[s]), (turn / kStages) & 1, quit)))) break;
+        const u32 at = tiles_at + s * kWeightsStageBytes;
+        const int here = min(kDepth, t.count - d), steps = (here + 15) >> 4;
+        if (here & 15) {
+          // the last lines of the copy belong to the next group, whose values may be anything: zeros in their place
+          const int boxes = 2 + (t.columns + kBox - 1) / kBox, lines = steps * 16 - here;
+          for (int i = lane; i < boxes * lines * 8; i += 32) {
+            const int box = i / (lines * 8), in = i - box * (lines * 8);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + box * kBoxBytes + here * 128 + in * 16), "r"(0) : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
+        tmem_fence_after();
+        if (lane == 0) {
+          for (int i = 0; i < steps; ++i)
+            mma(acc, operand(at + i * 2048, kBoxBytes, 1024), operand(at + kWeightsBytesA + i * 2048, kBoxBytes, 1024), how, !begins || i);
+          mma_commit(smem_at(&sh.empty[s]));
+          if (ends) mma_commit(smem_at(&sh.done[n & 1]));
+        }
+        __syncwarp();
+        if (ends) ++n;
+      }
+    }
+    if (!go && lane == 0) settle(sh);
+  } else if (warp >= 4) {
+    u32 n = 0;
+    bool go = true;
+    const int part = warp & 3, c0 = (warp >> 2) == 1 ? 0 : kMost / 2;  // this warp's lanes, and the first of its columns
+    for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+      const WeightTile t = weight_tile(id, a, k_tiles, m_tiles);
+      const int k = t.k + part * 32 + lane, columns = t.columns - c0;  // may be none
+      float* to = a.out + (int64_t)(t.group / a.inner) * a.outer_stride + (int64_t)(t.group % a.inner) * a.inner_stride +
+                  (int64_t)(t.m + c0) * a.ld_out + k;
+      float sum[kMost / 2];
+#pragma unroll
+      for (int c = 0; c < kMost / 2; ++c) sum[c] = 0.0f;
+      for (int d = 0; d < t.count; d += kWeightsChain, ++n) {
+        if (!(go = __all_sync(kAll, bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit)))) break;
+        tmem_fence_after();
+#pragma unroll
+        for (int c = 0; c < kMost / 2; c += 16) {
+          if (c < columns) {
+            float v[16];
+            tmem_read16(v, sh.tmem + (n & 1) * kMost + c0 + c + ((u32)(part * 32) << 16));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[c + i] += v[i];
+          }
+        }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_at(&sh.free_[n & 1]));
+      }
+      if (!go) break;
+      if (k >= a.k || (a.accumulate && !t.count)) continue;
+      if (a.accumulate) {
+#pragma unroll
+        for (int c = 0; c < kMost / 2; c += 16) {
+          float old[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (c + i < columns) old[i] = to[(c + i) * a.ld_out];
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (c + i < columns) to[(c + i) * a.ld_out] = sum[c + i] + old[i];
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < kMost / 2; ++c)
+          if (c < columns) to[c * a.ld_out] = sum[c];
+      }
+    }
+  }
+  tear_down(sh, kTmem);
+}
+
+// ---- copies of operands that TMA cannot read -------------------------------------------------------------------------------
+struct CopyArgs {
+  const uint16_t* from;
+  uint16_t* to;
+  int64_t ld, stride, ld_to, lines, cols;  // `lines` lines a matrix, matrices `stride` apart
+  int64_t total;                           // lines of all matrices
+};
+__global__ void __launch_bounds__(256) k_copy(const CopyArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t units = (a.cols + 255) >> 8, all = a.total * units, step = (int64_t)gridDim.x * 8;
+  for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < all; at += step) {
+    const int64_t line = at / units, c0 = (at - line * units) << 8;
+    const uint16_t* from = a.from + line / a.lines * a.stride + line % a.lines * a.ld;
+    uint16_t* to = a.to + line * a.ld_to;
+    uint16_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t c = c0 + j * 32 + lane;
+      if (c < a.cols) v[j] = from[c];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t c = c0 + j * 32 + lane;
+      if (c < a.cols) to[c] = v[j];
+    }
+  }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+  static EncodeTiled known = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return reinterpret_cast<EncodeTiled>(f);
+  }();
+  return known;
+}
+
+// Matrices [count][lines][cols] of 16-bit elements, copied in boxes of 64 columns and `box_lines` lines.  count 0: one matrix, 2-D.
+bool make_map(CUtensorMap* map, const void* p, int32_t type, int64_t cols, int64_t lines, int64_t ld, int count, int64_t stride, int box_lines) {
+  const EncodeTiled encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)lines, (cuuint64_t)(count ? count : 1)};
+  // one line, one matrix: the distance to the next is never used, but has to be one that is allowed
+  cuuint64_t strides[2] = {(cuuint64_t)(lines > 1 ? ld * 2 : (cols * 2 + 15) / 16 * 16), (cuuint64_t)(count > 1 ? stride * 2 : 0)};
+  if (count <= 1) strides[1] = strides[0] * dims[1];
+  const cuuint32_t box[3] = {kBox, (cuuint32_t)box_lines, 1}, ones[3] = {1, 1, 1};
+  return encode(map, type == REGTOPK_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, count ? 3 : 2,
+                const_cast<void*>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Whether TMA can read the matrices where they are; if not, their copy has lines of round_up(cols, 8) elements.
+bool direct(const void* p, int64_t ld, int64_t lines, int count, int64_t stride) {
+  return (uintptr_t)p % 16 == 0 && (lines <= 1 || ld % 8 == 0) && (count <= 1 || stride % 8 == 0);
+}
+int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
+size_t copy_bytes(int64_t lines, int64_t cols, int count) { return ((size_t)lines * count * padded(cols) * 2 + 255) / 256 * 256; }
+
+// Copies matrices into the workspace at *ws and makes p, ld and stride describe the copy.
+int copy_in(const void** p, int64_t* ld, int64_t lines, int64_t cols, int count, int64_t* stride, char** ws, int sms, cudaStream_t s) {
+  CopyArgs c;
+  c.from = static_cast<const uint16_t*>(*p); c.to = reinterpret_cast<uint16_t*>(*ws); c.ld = *ld; c.stride = *stride;
+  c.ld_to = padded(cols); c.lines = lines; c.cols = cols; c.total = lines * count;
+  const int64_t blocks = (c.total * ((cols + 255) / 256) + 7) / 8, most = (int64_t)sms * 8;
+  k_copy<<<(int)(blocks < most ? blocks : most), 256, 0, s>>>(c);
+  *p = *ws;
+  *ws += copy_bytes(lines, cols, count);
+  *ld = c.ld_to;
+  *stride = lines * c.ld_to;
+  return train_rc(cudaGetLastError());
+}
+
+template <auto kKernel> bool allow_smem(int bytes, int dev) {
+  static uint64_t done;  // of this kernel, one bit a device
+  if (__atomic_load_n(&done, __ATOMIC_RELAXED) >> dev & 1) return true;
+  if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  __atomic_fetch_or(&done, 1ull << dev, __ATOMIC_RELAXED);
+  return true;
+}
+
+template <typename T, int kMost, bool kTransposed>
+int launch_rows(const CUtensorMap& w, const CUtensorMap& x, const RowsArgs& a, int64_t tiles, int dev, int sms, cudaStream_t s) {
+  constexpr auto k = k_rows<T, kMost, kTransposed>;
+  if (!allow_smem<k>(RowStage<kMost>::kSmem, dev)) return train_rc(cudaGetLastError());
+  k<<<(int)(tiles < sms ? tiles : sms), kThreads, RowStage<kMost>::kSmem, s>>>(w, x, a);
+  return train_rc(cudaGetLastError());
+}
+
+template <typename T>
+int launch_weights(const CUtensorMap& x, const CUtensorMap& dy, const WeightsArgs& a, int64_t tiles, int dev, int sms, cudaStream_t s) {
+  constexpr auto k = k_weights<T>;
+  if (!allow_smem<k>(kWeightsSmem, dev)) return train_rc(cudaGetLastError());
+  k<<<(int)(tiles < sms ? tiles : sms), kWeightsThreads, kWeightsSmem, s>>>(x, dy, a);
+  return train_rc(cudaGetLastError());
+}
+
+constexpr int64_t kMostRows = 0x7FFFFF00;  // coordinates of a copy are 32-bit, and a tile may reach past the end
+
+bool good_sizes(int64_t rows, int64_t k, int64_t m, int32_t groups) {
+  return rows >= 0 && k >= 0 && m >= 0 && rows <= kMostRows && k <= kMostRows && m <= kMostRows && groups >= 1;
+}
+bool is_short(int32_t type) { return type == REGTOPK_TYPE_BF16 || type == REGTOPK_TYPE_F16; }
+
+}  // namespace
+
+extern "C" {
+
+size_t regtopk_grouped_matmul_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride,
+                                              int32_t transposed, int32_t weights, int64_t rows, int64_t k, int64_t m) {
+  if (!good_sizes(rows, k, m, 1) || weights < 1) return 0;
+  const int64_t lines = transposed ? k : m, cols = transposed ? m : k;
+  const int count = w_stride ? weights : 1;
+  return (direct(x, ldx, rows, 1, 0) ? 0 : copy_bytes(rows, k, 1)) + (direct(w, ldw, lines, count, w_stride) ? 0 : copy_bytes(lines, cols, count));
+}
+
+int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride, int32_t transposed,
+                           int32_t weights, void* y, int64_t ldy, const int64_t* offsets, int32_t groups, int64_t rows,
+                           int64_t k, int64_t m, int32_t type, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!is_short(type) || !good_sizes(rows, k, m, groups) || weights < 1 || groups % weights || !offsets || (uintptr_t)offsets % 8 || w_stride < 0)
+    return REGTOPK_ERR_INVALID_ARG;
+  if (groups > REGTOPK_MATMUL_MAX_GROUPS) return REGTOPK_ERR_TOO_LARGE;
+  if (rows == 0 || m == 0) return REGTOPK_OK;
+  int64_t lines = transposed ? k : m, cols = transposed ? m : k;
+  if (!good_matrix(y, ldy, rows, m, 2)) return REGTOPK_ERR_INVALID_ARG;
+  if (k > 0 && (!good_matrix(x, ldx, rows, k, 2) || !good_matrix(w, ldw, lines, cols, 2))) return REGTOPK_ERR_INVALID_ARG;
+  int dev, sms;
+  if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (k == 0) return train_rc(cudaMemset2DAsync(y, (size_t)(rows > 1 ? ldy : m) * 2, 0, (size_t)m * 2, (size_t)rows, s));
+  const size_t need = regtopk_grouped_matmul_workspace_bytes(x, ldx, w, ldw, w_stride, transposed, weights, rows, k, m);
+  if (need && (!workspace || (uintptr_t)workspace % 16)) return REGTOPK_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return REGTOPK_ERR_WORKSPACE_TOO_SMALL;
+  char* ws = static_cast<char*>(workspace);
+  const int count = w_stride ? weights : 1;
+  int64_t none = 0;
+  int rc;
+  if (!direct(x, ldx, rows, 1, 0) && (rc = copy_in(&x, &ldx, rows, k, 1, &none, &ws, sms, s))) return rc;
+  if (!direct(w, ldw, lines, count, w_stride) && (rc = copy_in(&w, &ldw, lines, cols, count, &w_stride, &ws, sms, s))) return rc;
+
+  // The widest tile of tokens: as wide as a group has rows on average (a narrower one reads the weights again for
+  // nothing, a wider one holds fewer stages), but narrow enough that every SM has a tile.
+  const int64_t average = rows / groups, features = (m + kLanes - 1) / kLanes;
+  int most = average > 128 ? 256 : average > 64 ? 128 : average > 32 ? 64 : 32;
+  CUtensorMap wm, xm;
+  if (!make_map(&wm, w, type, cols, lines, ldw, count, w_stride, transposed ? kDepth : kLanes) ||
+      !make_map(&xm, x, type, k, rows, ldx, 0, 0, most < 64 ? most : 64)) return REGTOPK_ERR_CUDA;
+  RowsArgs a;
+  a.offsets = offsets; a.y = y; a.ldy = ldy; a.groups = groups; a.weights = weights; a.rows = (int)rows; a.k = (int)k; a.m = (int)m;
+  a.shared_weights = count == 1;
+  a.pairs = m % 2 == 0 && (rows == 1 || ldy % 2 == 0) && (uintptr_t)y % 4 == 0;
+  const int64_t tiles = (rows / most + groups) * features;
+#define REGTOPK_ROWS(N)                                                                                    \
+  case N:                                                                                                  \
+    if (type == REGTOPK_TYPE_BF16)                                                                         \
+      return transposed ? launch_rows<__nv_bfloat16, N, true>(wm, xm, a, tiles, dev, sms, s)               \
+                        : launch_rows<__nv_bfloat16, N, false>(wm, xm, a, tiles, dev, sms, s);             \
+    return transposed ? launch_rows<__half, N, true>(wm, xm, a, tiles, dev, sms, s)                        \
+                      : launch_rows<__half, N, false>(wm, xm, a, tiles, dev, sms, s)
+  switch (most) {
+    REGTOPK_ROWS(32);
+    REGTOPK_ROWS(64);
+    REGTOPK_ROWS(128);
+    default:
+    REGTOPK_ROWS(256);
+  }
+#undef REGTOPK_ROWS
+}
+
+size_t regtopk_grouped_matmul_dw_workspace_bytes(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t groups,
+                                                 int64_t rows, int64_t k, int64_t m) {
+  if (!good_sizes(rows, k, m, groups)) return 0;
+  return (direct(dy, ld_dy, rows, 1, 0) ? 0 : copy_bytes(rows, m, 1)) + (direct(x, ldx, rows, 1, 0) ? 0 : copy_bytes(rows, k, 1));
+}
+
+int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, float* out, int64_t ld_out,
+                              int64_t inner_stride, int64_t outer_stride, int32_t inner, int32_t accumulate,
+                              const int64_t* offsets, int32_t groups, int64_t rows, int64_t k, int64_t m, int32_t type,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!is_short(type) || !good_sizes(rows, k, m, groups) || inner < 1 || groups % inner || !offsets || (uintptr_t)offsets % 8 ||
+      inner_stride < 0 || outer_stride < 0) return REGTOPK_ERR_INVALID_ARG;
+  if (groups > REGTOPK_MATMUL_MAX_GROUPS) return REGTOPK_ERR_TOO_LARGE;
+  if (k == 0 || m == 0) return REGTOPK_OK;
+  if (!good_matrix(out, ld_out, m, k, 4)) return REGTOPK_ERR_INVALID_ARG;
+  if (rows > 0 && (!good_matrix(dy, ld_dy, rows, m, 2) || !good_matrix(x, ldx, rows, k, 2))) return REGTOPK_ERR_INVALID_ARG;
+  if (rows == 0 && accumulate) return REGTOPK_OK;
+  int dev, sms;
+  if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  int64_t none = 0;
+  int rc;
+  WeightsArgs a;
+  CUtensorMap xm, ym;
+  if (rows > 0) {
+    const size_t need = regtopk_grouped_matmul_dw_workspace_bytes(dy, ld_dy, x, ldx, groups, rows, k, m);
+    if (need && (!workspace || (uintptr_t)workspace % 16)) return REGTOPK_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return REGTOPK_ERR_WORKSPACE_TOO_SMALL;
+    char* ws = static_cast<char*>(workspace);
+    if (!direct(dy, ld_dy, rows, 1, 0) && (rc = copy_in(&dy, &ld_dy, rows, m, 1, &none, &ws, sms, s))) return rc;
+    if (!direct(x, ldx, rows, 1, 0) && (rc = copy_in(&x, &ldx, rows, k, 1, &none, &ws, sms, s))) return rc;
+    if (!make_map(&xm, x, type, k, rows, ldx, 0, 0, kDepth) || !make_map(&ym, dy, type, m, rows, ld_dy, 0, 0, kDepth)) return REGTOPK_ERR_CUDA;
+  } else {
+    memset(&xm, 0, sizeof xm);  // never used: no group has rows
+    memset(&ym, 0, sizeof ym);
+  }
+  a.offsets = offsets; a.out = out; a.ld_out = ld_out; a.inner_stride = inner_stride; a.outer_stride = outer_stride;
+  a.groups = groups; a.inner = inner; a.rows = (int)rows; a.k = (int)k; a.m = (int)m; a.accumulate = accumulate;
+  const int64_t tiles = (int64_t)groups * ((k + kLanes - 1) / kLanes) * ((m + kWeightsMost - 1) / kWeightsMost);
+  return type == REGTOPK_TYPE_BF16 ? launch_weights<__nv_bfloat16>(xm, ym, a, tiles, dev, sms, s)
+                                   : launch_weights<__half>(xm, ym, a, tiles, dev, sms, s);
+}
+
+int regtopk_train_status(void* cuda_stream) {
+  int dev, sms;
+  if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
+  unsigned int gave_up = 0;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  int rc = train_rc(cudaMemcpyFromSymbolAsync(&gave_up, g_gave_up, sizeof gave_up, 0, cudaMemcpyDeviceToHost, s));
+  const int sync = train_rc(cudaStreamSynchronize(s));
+  if (rc == REGTOPK_OK) rc = sync;
+  return rc != REGTOPK_OK ? rc : gave_up ? REGTOPK_ERR_INTERNAL : REGTOPK_OK;
+}
+
+}  // extern "C"

@@ -22,7 +22,8 @@ _LIB = os.path.join(_PKG, "libregtopk_train.so")
 
 EXPORTS = [
     "regtopk_dropout", "regtopk_layer_norm", "regtopk_layer_norm_backward_workspace_bytes",
-    "regtopk_layer_norm_backward",
+    "regtopk_layer_norm_backward", "regtopk_grouped_matmul_workspace_bytes", "regtopk_grouped_matmul",
+    "regtopk_grouped_matmul_dw_workspace_bytes", "regtopk_grouped_matmul_dw", "regtopk_train_status",
 ]
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -52,6 +53,13 @@ def load_library():
     L.regtopk_layer_norm_backward_workspace_bytes.restype = size
     L.regtopk_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp,
                                               i32, i32, i64, i64, i32, i32, drop, vp, size, vp]
+    L.regtopk_grouped_matmul_workspace_bytes.argtypes = [vp, i64, vp, i64, i64, i32, i32, i64, i64, i64]
+    L.regtopk_grouped_matmul_workspace_bytes.restype = size
+    L.regtopk_grouped_matmul.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, i64, vp, i32, i64, i64, i64, i32, vp, size, vp]
+    L.regtopk_grouped_matmul_dw_workspace_bytes.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64]
+    L.regtopk_grouped_matmul_dw_workspace_bytes.restype = size
+    L.regtopk_grouped_matmul_dw.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i32, i32, vp, i32, i64, i64, i64, i32, vp, size, vp]
+    L.regtopk_train_status.argtypes = [vp]
     _lib = L
     return L
 
@@ -228,3 +236,96 @@ def layer_norm_backward(dy: torch.Tensor, h: torch.Tensor, mean: torch.Tensor, r
             offsets.data_ptr() if offsets is not None else None, groups, int(accumulate), rows, cols, code, TYPES[h.dtype],
             drop, ws.data_ptr(), nbytes, on.stream), "regtopk_layer_norm_backward")
     return dx, dres, dweight, dbias
+
+
+def _short(t: torch.Tensor, name: str) -> int:
+    code = _type(t, name)
+    if code == 0:
+        raise TypeError(f"{name} is bfloat16 or float16")
+    if t.dim() != 2:
+        raise ValueError(f"{name} is a matrix")
+    return code
+
+
+def grouped_matmul(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [rows, m] with y[t] = w[g % E] @ x[t] for the rows t of group g; rows of no group become zeros.
+
+    x [rows, k] and w [E, m, k] are both bfloat16 or both float16; either of w's last two dimensions may be the
+    contiguous one, so w.transpose(1, 2) of a layer's weights gives the gradient to its tokens.  The number of groups
+    is a multiple of E: groups sorted by (worker, expert) use the experts' matrices in turn."""
+    code = _short(x, "x")
+    rows, k, ldx = _rows(x, "x")
+    groups = _offsets(offsets, x)
+    if w.device != x.device or w.dtype != x.dtype or w.dim() != 3 or w.shape[2] != k:
+        raise TypeError(f"w must be [experts, m, {k}] of x's dtype on x's device")
+    count, m = w.shape[0], w.shape[1]
+    if count < 1 or groups % count:
+        raise ValueError("the number of groups must be a multiple of the number of matrices")
+    stride, by_row, by_col = w.stride()
+    if by_col == 1 or k <= 1:
+        transposed, ldw, short = 0, by_row if m > 1 else k, k
+    elif by_row == 1 or m <= 1:
+        transposed, ldw, short = 1, by_col, m
+    else:
+        raise ValueError("w: one of its last two dimensions must be contiguous")
+    if ldw < short:
+        raise ValueError("w: rows overlap")
+    if out is None:
+        out = torch.empty((rows, m), dtype=x.dtype, device=x.device)
+    elif out.device != x.device or out.dtype != x.dtype or out.shape != (rows, m):
+        raise TypeError(f"out must be [{rows}, {m}] of x's dtype on x's device")
+    ldy = _rows(out, "out")[2]
+    L = load_library()
+    px, pw = x.data_ptr(), w.data_ptr()
+    nbytes = L.regtopk_grouped_matmul_workspace_bytes(px, ldx, pw, ldw, stride, transposed, count, rows, k, m)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
+    with _on(x) as on:
+        _check(L.regtopk_grouped_matmul(px, ldx, pw, ldw, stride, transposed, count, out.data_ptr(), ldy, offsets.data_ptr(), groups,
+                                        rows, k, m, code, ws.data_ptr() if nbytes else None, nbytes, on.stream), "regtopk_grouped_matmul")
+    return out
+
+
+def grouped_matmul_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
+                      accumulate: bool = False) -> torch.Tensor:
+    """The gradient of grouped_matmul to the matrices, for every group on its own: out[g] = sum of dy[t] x[t]^T over
+    the rows t of group g, float32 [groups, m, k].
+
+    out may be given, as [groups, m, k] or [workers, experts, m, k] with any strides but contiguous rows (a view of an
+    accumulator's columns, say), and is added to if `accumulate`."""
+    code = _short(dy, "dy")
+    rows, m, ld_dy = _rows(dy, "dy")
+    groups = _offsets(offsets, dy)
+    if x.device != dy.device or x.dtype != dy.dtype or x.dim() != 2 or x.shape[0] != rows:
+        raise TypeError(f"x must be [{rows}, k] of dy's dtype on dy's device")
+    _, k, ldx = _rows(x, "x")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs an out to add to")
+        out = torch.empty((groups, m, k), dtype=torch.float32, device=dy.device)
+    shape = out.shape
+    if out.device != dy.device or out.dtype != torch.float32 or len(shape) not in (3, 4) or shape[-2:] != (m, k) \
+            or shape[:-2].numel() != groups:
+        raise TypeError(f"out must be float32 [{groups}, {m}, {k}] or [workers, experts, {m}, {k}] on dy's device")
+    strides = out.stride()
+    ld_out = strides[-2] if m > 1 else k
+    if (k > 1 and strides[-1] != 1) or ld_out < k:
+        raise ValueError("out: the elements of a row must be contiguous and rows must not overlap")
+    if len(shape) == 3:
+        inner, inner_stride, outer_stride = groups, strides[0], 0
+    else:
+        inner, inner_stride, outer_stride = shape[1], strides[1], strides[0]
+    L = load_library()
+    pdy, px = dy.data_ptr(), x.data_ptr()
+    nbytes = L.regtopk_grouped_matmul_dw_workspace_bytes(pdy, ld_dy, px, ldx, groups, rows, k, m)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device) if nbytes else None
+    with _on(dy) as on:
+        _check(L.regtopk_grouped_matmul_dw(pdy, ld_dy, px, ldx, out.data_ptr(), ld_out, inner_stride, outer_stride, inner, int(accumulate),
+                                           offsets.data_ptr(), groups, rows, k, m, code, ws.data_ptr() if nbytes else None, nbytes,
+                                           on.stream), "regtopk_grouped_matmul_dw")
+    return out
+
+
+def training_status(device=None):
+    """Synchronises the device's current stream; raises if a product's kernel there ever gave up waiting (a bug)."""
+    with torch.cuda.device(device):
+        _check(load_library().regtopk_train_status(torch.cuda.current_stream().cuda_stream), "regtopk_train_status")
