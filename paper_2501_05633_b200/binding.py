@@ -9,6 +9,7 @@ import ctypes
 import os
 import shutil
 import subprocess
+import sysconfig
 import tempfile
 from typing import Optional, Tuple
 
@@ -22,6 +23,8 @@ _LIB = os.path.join(_PKG, "libregtopk.so")
 _TRAIN_SRC = [os.path.join(_PKG, "csrc", name) for name in ("dropout_norm.cu", "grouped_matmul.cu")]
 _TRAIN_DEPS = [os.path.join(_PKG, "csrc", "train_common.cuh"), os.path.join(_INC, "regtopk_train.h"), os.path.join(_INC, "regtopk.h")]
 _TRAIN_LIB = os.path.join(_PKG, "libregtopk_train.so")
+_TRAIN_BINDING = os.path.join(_PKG, "csrc", "training_binding.cpp")
+_TRAIN_MODULE = os.path.join(_PKG, "_training.so")
 
 OK = 0
 GRAD_F32, GRAD_BF16 = 0, 1
@@ -56,25 +59,38 @@ def library_path() -> str:
     return _LIB
 
 
+def _stale(made: str, sources) -> bool:
+    return not os.path.exists(made) or os.path.getmtime(made) < max(os.path.getmtime(f) for f in sources)
+
+
 def build_training(force: bool = False, verbose: bool = False) -> str:
-    """Compile the training operators' sources for sm_100a into libregtopk_train.so, side by side."""
-    if not force and os.path.exists(_TRAIN_LIB) and os.path.getmtime(_TRAIN_LIB) >= max(
-            os.path.getmtime(f) for f in _TRAIN_SRC + _TRAIN_DEPS):
-        return _TRAIN_LIB
-    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-I", _INC, "-Xcompiler", "-fPIC"]
-    if verbose:
-        flags.insert(0, "-Xptxas=-v")
+    """Compile the training operators for sm_100a into libregtopk_train.so, source by source side by side, and the Python
+    module that marshals into it."""
     with tempfile.TemporaryDirectory() as tmp:
-        objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in _TRAIN_SRC]
-        runs = [subprocess.Popen(["nvcc", *flags, "-c", "-o", o, f]) for f, o in zip(_TRAIN_SRC, objects)]
-        for run in runs:
-            run.wait()
-        for run in runs:
-            if run.returncode:
-                raise subprocess.CalledProcessError(run.returncode, run.args)
-        made = os.path.join(tmp, "libregtopk_train.so")
-        subprocess.run(["nvcc", *flags, "--shared", "-o", made, *objects], check=True)
-        shutil.move(made, _TRAIN_LIB)
+        if force or _stale(_TRAIN_LIB, _TRAIN_SRC + _TRAIN_DEPS):
+            flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-I", _INC, "-Xcompiler", "-fPIC"]
+            if verbose:
+                flags.insert(0, "-Xptxas=-v")
+            objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in _TRAIN_SRC]
+            runs = [subprocess.Popen(["nvcc", *flags, "-c", "-o", o, f]) for f, o in zip(_TRAIN_SRC, objects)]
+            for run in runs:
+                run.wait()
+            for run in runs:
+                if run.returncode:
+                    raise subprocess.CalledProcessError(run.returncode, run.args)
+            made = os.path.join(tmp, os.path.basename(_TRAIN_LIB))
+            subprocess.run(["nvcc", *flags, "--shared", "-o", made, *objects], check=True)
+            shutil.move(made, _TRAIN_LIB)
+        if force or _stale(_TRAIN_MODULE, [_TRAIN_BINDING, *_TRAIN_DEPS[1:]]):
+            root = os.path.dirname(torch.__file__)
+            cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc"))))
+            made = os.path.join(tmp, os.path.basename(_TRAIN_MODULE))
+            subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                            "-I", _INC, "-I", os.path.join(root, "include"), "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                            "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-o", made, _TRAIN_BINDING,
+                            "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
+                            "-L", _PKG, "-lregtopk_train", "-Wl,-rpath,$ORIGIN"], check=True)
+            shutil.move(made, _TRAIN_MODULE)
     return _TRAIN_LIB
 
 

@@ -8,7 +8,6 @@ import pytest
 import torch
 
 import paper_2501_05633_b200 as rt
-from paper_2501_05633_b200 import training
 from tests import train_reference as ref
 
 BF, HF = torch.bfloat16, torch.float16
@@ -47,8 +46,7 @@ def test_reference_gradients_against_differences():
 
 
 def test_c_entries_refuse():
-    rt.build()
-    lib, p = training.load_library(), 4096
+    lib, p = ref.c_library(), 4096
 
     def rows(x=p, w=p, y=p, off=p, groups=4, weights=2, type=1, rows=8, k=16, m=16, ldx=16, ldw=16, ldy=16, ws=None, nbytes=0, stride=256):
         return lib.regtopk_grouped_matmul(x, ldx, w, ldw, stride, 0, weights, y, ldy, off, groups, rows, k, m, type, ws, nbytes, None)

@@ -1,4 +1,7 @@
 """The training operators from their definitions, in 64 bits on the host (numpy), for the tests of the CUDA kernels."""
+import ctypes
+import os
+
 import numpy as np
 import torch
 
@@ -65,3 +68,30 @@ def assert_close(got, want, slack, dtype, what):
     most = (ROUND[dtype] * np.abs(np.where(fine, want, 0.0)) + TINY[dtype] + slack + 0 * want)[fine]
     bad = ~(off <= most)
     assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size} too far off, worst {np.nanmax(off / np.maximum(most, 1e-300)):.3g} times the tolerance"
+
+
+class DropoutParams(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("subsequence", ctypes.c_uint32)]
+
+
+def c_library():
+    """The C entries of the training operators with their signatures."""
+    import paper_2501_05633_b200 as rt
+    rt.build()
+    L = ctypes.CDLL(os.path.join(os.path.dirname(rt.__file__), "libregtopk_train.so"))
+    p, i64, i32, f32, size, drop = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t,
+                                    ctypes.POINTER(DropoutParams))
+    for name, args, res in [
+            ("regtopk_dropout", [p, i64, p, i64, i64, i64, i32, drop, p], i32),
+            ("regtopk_layer_norm", [p, i64, p, i64, p, p, f32, p, i64, p, i64, p, p, i64, i64, i32, i32, drop, p], i32),
+            ("regtopk_layer_norm_backward_workspace_bytes", [i64, i64, i32], size),
+            ("regtopk_layer_norm_backward", [p, i64, p, i64, p, p, p, p, i64, p, i64, p, i64, p, i64, p, i64, p, i32, i32, i64, i64,
+                                             i32, i32, drop, p, size, p], i32),
+            ("regtopk_grouped_matmul_workspace_bytes", [p, i64, p, i64, i64, i32, i32, i64, i64, i64], size),
+            ("regtopk_grouped_matmul", [p, i64, p, i64, i64, i32, i32, p, i64, p, i32, i64, i64, i64, i32, p, size, p], i32),
+            ("regtopk_grouped_matmul_dw_workspace_bytes", [p, i64, p, i64, i32, i64, i64, i64], size),
+            ("regtopk_grouped_matmul_dw", [p, i64, p, i64, p, i64, i64, i64, i32, i32, p, i32, i64, i64, i64, i32, p, size, p], i32),
+            ("regtopk_train_status", [p], i32)]:
+        f = getattr(L, name)
+        f.argtypes, f.restype = args, res
+    return L
