@@ -23,44 +23,6 @@
 namespace {
 
 // ---- PTX -------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ u32 smem_at(const void* p) { return (u32)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void bar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-__device__ __forceinline__ void bar_expect(u32 bar, u32 bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool bar_done(u32 bar, u32 parity) {
-  u32 ok;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok;
-}
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
-
-// Every wait ends: after two seconds the block gives up, says so here, and leaves (regtopk_train_status).
-__device__ unsigned int g_gave_up;
-constexpr uint64_t kPatienceNs = 2000000000ull;
-
-__device__ __noinline__ bool bar_wait_long(u32 bar, u32 parity, volatile u32* quit) {
-  const uint64_t began = now_ns();
-  while (!bar_done(bar, parity)) {
-    if (*quit) return false;
-    if (now_ns() - began > kPatienceNs) {
-      *quit = 1;
-      atomicExch(&g_gave_up, 1u);
-      return false;
-    }
-  }
-  return true;
-}
-__device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, volatile u32* quit) {
-  return bar_done(bar, parity) || bar_wait_long(bar, parity, quit);
-}
-
 __device__ __forceinline__ void tma_2d(u32 to, const CUtensorMap* map, u32 bar, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
@@ -763,12 +725,10 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
 int regtopk_train_status(void* cuda_stream) {
   int dev, sms;
   if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
-  unsigned int gave_up = 0;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  int rc = train_rc(cudaMemcpyFromSymbolAsync(&gave_up, g_gave_up, sizeof gave_up, 0, cudaMemcpyDeviceToHost, s));
-  const int sync = train_rc(cudaStreamSynchronize(s));
-  if (rc == REGTOPK_OK) rc = sync;
-  return rc != REGTOPK_OK ? rc : gave_up ? REGTOPK_ERR_INTERNAL : REGTOPK_OK;
+  int rc = gave_up(s);
+  if (rc == 0) rc = regtopk_norm_gave_up(s);
+  return rc > 0 ? REGTOPK_ERR_INTERNAL : rc;
 }
 
 }  // extern "C"
