@@ -23,20 +23,63 @@
 namespace {
 
 // ---- PTX -------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void tma_2d(u32 to, const CUtensorMap* map, u32 bar, int x, int y) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-               ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+// Copies of boxes.  kCtas 2: the barrier may be the other block's of a pair.
+template <int kCtas> __device__ __forceinline__ void tma_2d(u32 to, const CUtensorMap* map, u32 bar, int x, int y) {
+  if constexpr (kCtas == 2)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
-__device__ __forceinline__ void tma_3d(u32 to, const CUtensorMap* map, u32 bar, int x, int y, int z) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-               ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+template <int kCtas> __device__ __forceinline__ void tma_3d(u32 to, const CUtensorMap* map, u32 bar, int x, int y, int z) {
+  if constexpr (kCtas == 2)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void mma(u32 d, uint64_t a, uint64_t b, u32 how, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-               ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((u32)add) : "memory");
+template <int kCtas> __device__ __forceinline__ void mma(u32 d, uint64_t a, uint64_t b, u32 how, bool add) {
+  if constexpr (kCtas == 2)
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((u32)add) : "memory");
+  else
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((u32)add) : "memory");
 }
-__device__ __forceinline__ void mma_commit(u32 bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// Arrives on the barrier (of both blocks of a pair) when the products issued so far are done.
+template <int kCtas> __device__ __forceinline__ void mma_commit(u32 bar) {
+  if constexpr (kCtas == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// The place in the first block of a pair that corresponds to one here.
+template <int kCtas> __device__ __forceinline__ u32 in_first(u32 at) {
+  if constexpr (kCtas == 1) return at;
+  u32 there;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(at));
+  return there;
+}
+// Arrives on a barrier of the first block.  kOrders: what this thread has written is seen by who waits there.  Where that is
+// nothing, because an accumulator has only been read, ordering would wait for all of this thread's stores to memory.
+template <int kCtas, bool kOrders> __device__ __forceinline__ void bar_arrive_first(u32 bar) {
+  if constexpr (kCtas == 1 && kOrders) bar_arrive(bar);
+  else if constexpr (kCtas == 1) asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+  else if constexpr (kOrders) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<2>(bar)) : "memory");
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<2>(bar)) : "memory");
+}
+template <int kCtas> __device__ __forceinline__ u32 cta_rank() {
+  if constexpr (kCtas == 1) return 0;
+  u32 r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// All threads of the block, or of both blocks of a pair.
+template <int kCtas> __device__ __forceinline__ void sync_all() {
+  if constexpr (kCtas == 1) __syncthreads();
+  else asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -76,75 +119,122 @@ __device__ __forceinline__ void tmem_read16(float (&v)[16], u32 at) {
 
 // ---- descriptors -----------------------------------------------------------------------------------------------------
 // Shared memory operand in the 128-byte swizzle: start, distance of 64-element blocks along the operand's own rows
-// (used where those are the contiguous dimension), distance of groups of eight swizzled lines, both in bytes.
+// (used where those are the contiguous dimension), distance of groups of eight swizzled lines, in bytes.
 __device__ __forceinline__ uint64_t operand(u32 at, u32 leading, u32 stride) {
-  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+  const u32 lo = at >> 4 | leading >> 4 << 16, hi = stride >> 4 | 1u << 14 | 2u << 29;  // shared addresses are below 2^18
+  return (uint64_t)hi << 32 | lo;
+}
+// One lane of a converged warp.  The warp that issues products runs as a whole and elects a lane for the instructions
+// themselves: its addresses and descriptors are then uniform, which the instructions want (with a single thread in the
+// loop a stage of four products took 430 ns to issue, however few columns they had).
+__device__ __forceinline__ bool elected() {
+  u32 yes;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+  return yes;
 }
 constexpr int kBox = 64;                   // elements of a line of a box: 128 bytes
-constexpr int kDepth = 64;                 // of the summed dimension in a stage
-constexpr int kBoxBytes = kBox * kDepth * 2;
+// Of the summed dimension in a stage.  Two lines of a box deep where that dimension is the contiguous one: a stage of 64
+// holds too little work for what it costs to wait for it, issue it and hand it back.
+constexpr int kDepth = 128;
+constexpr int kBoxBytes = kBox * kDepth * 2;  // a box whose lines are the summed dimension
+constexpr int kStepBytes = 16 * kBox * 2;     // from one step of sixteen such lines to the next
 constexpr int kLanes = 128;                // accumulator lanes: the fixed side of a tile
 
-// Instruction descriptor: binary32 accumulators, both operands of one 16-bit type, 128 lanes, `columns` columns; _mn: the
-// operand's own rows, not the summed dimension, are contiguous.
-__device__ __forceinline__ u32 instruction(bool bf16, bool a_mn, bool b_mn, int columns) {
-  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (u32)a_mn << 15 | (u32)b_mn << 16 | (u32)(columns >> 3) << 17 | (u32)(kLanes >> 4) << 24;
+// Instruction descriptor: binary32 accumulators, both operands of one 16-bit type, 128 lanes of each block, `columns`
+// columns; _mn: the operand's own rows, not the summed dimension, are contiguous.
+template <int kCtas> __device__ __forceinline__ u32 instruction(bool bf16, bool a_mn, bool b_mn, int columns) {
+  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (u32)a_mn << 15 | (u32)b_mn << 16 | (u32)(columns >> 3) << 17 | (u32)(kCtas * kLanes >> 4) << 24;
 }
 
-constexpr int kThreads = 256;  // warp 0 copies, warp 1 multiplies, warp 2 keeps the TMEM, warp 3 clears, warps 4-7 write
+// The products of one stage, up to eight steps of sixteen of the summed dimension.  An operand whose own rows are contiguous
+// (kMn) lies in boxes whose lines are the summed dimension; the other kind in two halves of 64 of it, `half` bytes apart.
+template <bool kMn> __device__ __forceinline__ uint64_t step_of(uint64_t operand, int i, u32 half) {
+  return operand + ((kMn ? i * kStepBytes : (i >> 2) * half + (i & 3) * 32) >> 4);
+}
+template <int kCtas, bool kMnA, bool kMnB>
+__device__ __forceinline__ void multiply(u32 acc, uint64_t a, u32 half_a, uint64_t b, u32 half_b, u32 how, int steps, bool begins) {
+  if (steps == kDepth / 16) {
+#pragma unroll
+    for (int i = 0; i < kDepth / 16; ++i) mma<kCtas>(acc, step_of<kMnA>(a, i, half_a), step_of<kMnB>(b, i, half_b), how, i || !begins);
+  } else {
+    for (int i = 0; i < steps; ++i) mma<kCtas>(acc, step_of<kMnA>(a, i, half_a), step_of<kMnB>(b, i, half_b), how, i || !begins);
+  }
+}
 
+// Columns come in steps of sixteen, thirty-two for a pair.
+template <int kCtas> __device__ __forceinline__ int rounded(int columns) { return (columns + 16 * kCtas - 1) / (16 * kCtas) * (16 * kCtas); }
+
+// Warp 0 copies, warp 1 multiplies, warp 2 keeps the TMEM, warp 3 clears; warps 4-11 write, two for each quarter of the lanes.
+constexpr int kThreads = 384, kWriters = 8;
+
+// `full`, `free_`, `last` and `masked` are the first block's of a pair alone; the other block's copies and warps arrive there too.
 template <int kStages> struct Shared {
-  uint64_t full[kStages], empty[kStages], done[2], free_[2], last;
+  uint64_t full[kStages], empty[kStages];   // a stage has landed; has been used
+  uint64_t landed[kStages], masked[kStages]; // k_weights, pairs: the second block's half of a group's last tokens has landed there; has been masked
+  uint64_t done[2], free_[2], last;          // an accumulator is finished; has been read; all products are done
   u32 tmem, quit;
 };
 
-template <int kStages> __device__ __forceinline__ void set_up(Shared<kStages>& sh, int tmem_columns, int readers) {
+template <int kCtas, int kStages> __device__ __forceinline__ void set_up(Shared<kStages>& sh, int tmem_columns, int readers) {
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       bar_init(smem_at(&sh.full[i]), 1);
       bar_init(smem_at(&sh.empty[i]), 1);
+      bar_init(smem_at(&sh.landed[i]), 1);
+      bar_init(smem_at(&sh.masked[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(smem_at(&sh.done[i]), 1);
-      bar_init(smem_at(&sh.free_[i]), readers);
+      bar_init(smem_at(&sh.free_[i]), readers * kCtas);
     }
     bar_init(smem_at(&sh.last), 1);
     sh.quit = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (threadIdx.x >> 5 == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&sh.tmem)), "r"(tmem_columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (kCtas == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&sh.tmem)), "r"(tmem_columns) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&sh.tmem)), "r"(tmem_columns) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
   }
   tmem_fence_before();
   __syncthreads();
+  sync_all<kCtas>();
   tmem_fence_after();
 }
-template <int kStages> __device__ __forceinline__ void tear_down(Shared<kStages>& sh, int tmem_columns) {
+// No block of a pair leaves before the other: its barriers and its shared memory are in use until then.
+template <int kCtas, int kStages> __device__ __forceinline__ void tear_down(Shared<kStages>& sh, int tmem_columns) {
   tmem_fence_before();
   __syncthreads();
+  sync_all<kCtas>();
   tmem_fence_after();
-  if (threadIdx.x >> 5 == 2)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(tmem_columns));
+  if (threadIdx.x >> 5 == 2) {
+    if constexpr (kCtas == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(tmem_columns));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(tmem_columns));
+  }
 }
 
 // The copying thread's way through the stages: `turn` counts stages filled so far.
-// After the last one it waits until every stage that was filled has landed and been used, so that nothing is under
-// way when the block ends; if the block has given up, until what was requested has landed.
-template <int kStages> __device__ __forceinline__ void drain(Shared<kStages>& sh, u32 turn) {
+// After the last one it waits until every stage that was filled has been used, so that nothing is under way when the
+// block ends; if the block has given up, until what was requested has landed (in a pair the first block's barrier
+// says so for both; the second block then waits for the first at the end).
+template <int kStages> __device__ __forceinline__ void drain(Shared<kStages>& sh, u32 turn, bool first) {
   volatile u32* quit = &sh.quit;
   const u32 from = turn > (u32)kStages ? turn - kStages : 0;
   for (u32 t = from; t < turn; ++t) {
     u32 never = 0;
     const u32 s = t % kStages, parity = (t / kStages) & 1;
-    if (*quit || !bar_wait(smem_at(&sh.empty[s]), parity, quit)) bar_wait(smem_at(&sh.full[s]), parity, &never);
+    if ((*quit || !bar_wait(smem_at(&sh.empty[s]), parity, quit)) && first) bar_wait(smem_at(&sh.full[s]), parity, &never);
   }
 }
 
 // The multiplying thread, when the block has given up: no product may be under way when the block ends.
-template <int kStages> __device__ __forceinline__ void settle(Shared<kStages>& sh) {
+template <int kCtas, int kStages> __device__ __forceinline__ void settle(Shared<kStages>& sh) {
   u32 never = 0;
-  mma_commit(smem_at(&sh.last));
+  mma_commit<kCtas>(smem_at(&sh.last));
   bar_wait(smem_at(&sh.last), 0, &never);
 }
 
@@ -170,7 +260,7 @@ __device__ __forceinline__ int tile_rows(int count, int most) {
 
 struct RowTile { int group, row, count, feature; };
 
-template <int kMost>
+template <int kMost, int kCtas>
 __device__ __forceinline__ RowTile row_tile(int64_t id, int feature_tiles, const int* before, const int* start, const int* end, int groups) {
   const int at = (int)(id / feature_tiles);
   int lo = 0, hi = groups;  // the last group with before[g] <= at
@@ -183,20 +273,23 @@ __device__ __forceinline__ RowTile row_tile(int64_t id, int feature_tiles, const
   t.group = lo;
   t.row = start[lo] + (at - before[lo]) * step;
   t.count = min(step, end[lo] - t.row);
-  t.feature = (int)(id - (int64_t)at * feature_tiles) * kLanes;
+  t.feature = (int)(id - (int64_t)at * feature_tiles) * (kCtas * kLanes);
   return t;
 }
 
-template <int kMost> struct RowStage {
-  static constexpr int kBytesA = kLanes * kDepth * 2, kBytes = kBytesA + kMost * kDepth * 2;
-  static constexpr int kCount = kMost == 256 ? 4 : kMost == 128 ? 6 : kMost == 64 ? 8 : 9;
+// The tokens of a tile, of which there are up to kMost, are divided between the blocks of a pair.
+template <int kMost, int kCtas> struct RowStage {
+  static constexpr int kTokens = kMost / kCtas, kBytesA = kLanes * kDepth * 2, kBytes = kBytesA + kTokens * kDepth * 2;
+  static constexpr int kHalfA = kBytesA / 2, kHalfB = kTokens * kBox * 2;
+  static constexpr int kCount = kTokens == 128 ? 3 : kTokens == 64 ? 4 : 5;
   static constexpr int kSmem = kCount * kBytes + 1024;
 };
 
-template <typename T, int kMost, bool kTransposed>
+template <typename T, int kMost, bool kTransposed, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const RowsArgs a) {
-  constexpr int kStages = RowStage<kMost>::kCount, kBytesA = RowStage<kMost>::kBytesA, kBytes = RowStage<kMost>::kBytes;
-  constexpr int kBoxRows = kMost < 64 ? kMost : 64;  // tokens of one copy
+  typedef RowStage<kMost, kCtas> Stage;
+  constexpr int kStages = Stage::kCount, kBytesA = Stage::kBytesA, kBytes = Stage::kBytes;
+  constexpr int kBoxRows = Stage::kTokens < 64 ? Stage::kTokens : 64;  // tokens of one copy
   constexpr int kTmem = 2 * kMost;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ uint8_t raw[];
@@ -204,20 +297,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
   __shared__ int before[kTableGroups + 1], start[kTableGroups], end[kTableGroups];
   __shared__ int scan[kThreads / 32];
   const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
-  set_up(sh, kTmem, 4);
-  // where each group's rows lie and how many tiles come before it
-  constexpr int kPer = (kTableGroups + kThreads - 1) / kThreads;
+  const u32 rank = cta_rank<kCtas>();
+
+  set_up<kCtas>(sh, kTmem, kWriters);
+  // where each group's rows lie and how many tiles come before it; groups that share a matrix one after the other, so that
+  // it is read from memory once (four workers over sixteen matrices of 9 MB: 752 MB read without that, 285 MB are needed)
+  constexpr int kPer = (kTableGroups + kThreads - 1) / kThreads;  // groups of a thread
   {
     int own[kPer], sum = 0;
-    const int per = (a.groups + kThreads - 1) / kThreads;
+    const int per = (a.groups + kThreads - 1) / kThreads, sharers = a.groups / a.weights;
     for (int i = 0; i < per; ++i) {
       const int g = threadIdx.x * per + i;
       own[i] = 0;
       if (g < a.groups) {
-        const int lo = (int)limited(a.offsets[g], a.rows);
-        int hi = (int)limited(a.offsets[g + 1], a.rows);
+        const int of = (g % sharers) * a.weights + g / sharers;  // in the table the groups of one matrix are neighbours
+        const int lo = (int)limited(a.offsets[of], a.rows);
+        int hi = (int)limited(a.offsets[of + 1], a.rows);
         if (hi < lo) hi = lo;
         start[g] = lo;
         end[g] = hi;
@@ -246,59 +343,75 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
     }
     __syncthreads();
   }
-  const int feature_tiles = (a.m + kLanes - 1) / kLanes, depth = (a.k + kDepth - 1) / kDepth;
+  const int feature_tiles = (a.m + kCtas * kLanes - 1) / (kCtas * kLanes);
   const int64_t tiles = (int64_t)before[a.groups] * feature_tiles;
+  const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
   volatile u32* quit = &sh.quit;
 
   if (warp == 0) {
-    if (lane == 0) {
-      u32 turn = 0;
-      bool go = true;
-      for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x) {
-        const RowTile t = row_tile<kMost>(id, feature_tiles, before, start, end, a.groups);
-        const int e = a.shared_weights ? 0 : t.group % a.weights;
-        const int boxes = (t.count + kBoxRows - 1) / kBoxRows;
-        for (int d = 0; d < depth; ++d, ++turn) {
-          const u32 s = turn % kStages, parity = (turn / kStages) & 1;
-          if (!(go = bar_wait(smem_at(&sh.empty[s]), parity ^ 1, quit))) break;
-          const u32 at = tiles_at + s * kBytes, bar = smem_at(&sh.full[s]);
-          bar_expect(bar, kBytesA + boxes * kBoxRows * kDepth * 2);
+    u32 s = 0, parity = 1, turn = 0;
+    bool ok = true;
+    const u32 full = in_first<kCtas>(smem_at(&sh.full[0]));
+    for (int64_t id = pair; id < tiles; id += pairs) {
+      const RowTile t = row_tile<kMost, kCtas>(id, feature_tiles, before, start, end, a.groups);
+      const int e = a.shared_weights ? 0 : t.group / (a.groups / a.weights);
+      const int here = rounded<kCtas>(t.count) / kCtas, boxes = (here + kBoxRows - 1) / kBoxRows;  // this block's tokens
+      const int feature = t.feature + (int)rank * kLanes, row = t.row + (int)rank * here;
+      for (int d = 0; d < a.k; d += kDepth) {
+        ok = ok && bar_wait(smem_at(&sh.empty[s]), parity, quit);
+        __syncwarp();
+        if (elected() && ok) {
+          const int halves = a.k - d > kBox ? 2 : 1;
+          const u32 at = tiles_at + s * kBytes, bar = full + s * 8;
+          if (rank == 0)
+            bar_expect(smem_at(&sh.full[s]), kCtas * ((kTransposed ? 2 : halves) * Stage::kHalfA + halves * boxes * kBoxRows * kBox * 2));
           if (kTransposed) {
-            tma_3d(at, &w_map, bar, t.feature, d * kDepth, e);
-            tma_3d(at + kBoxBytes, &w_map, bar, t.feature + kBox, d * kDepth, e);
-          } else {
-            tma_3d(at, &w_map, bar, d * kDepth, t.feature, e);
+            tma_3d<kCtas>(at, &w_map, bar, feature, d, e);
+            tma_3d<kCtas>(at + kBoxBytes, &w_map, bar, feature + kBox, d, e);
           }
-          for (int i = 0; i < boxes; ++i)
-            tma_2d(at + kBytesA + i * kBoxRows * kDepth * 2, &x_map, bar, d * kDepth, t.row + i * kBoxRows);
+          for (int h = 0; h < halves; ++h) {
+            if (!kTransposed) tma_3d<kCtas>(at + h * Stage::kHalfA, &w_map, bar, d + h * kBox, feature, e);
+            for (int i = 0; i < boxes; ++i)
+              tma_2d<kCtas>(at + kBytesA + h * Stage::kHalfB + i * kBoxRows * kBox * 2, &x_map, bar, d + h * kBox, row + i * kBoxRows);
+          }
+        }
+        __syncwarp();
+        turn += ok;
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1;
         }
       }
-      drain(sh, turn);
     }
+    if (elected()) drain(sh, turn, rank == 0);
   } else if (warp == 1) {
-    if (lane == 0) {
-      u32 turn = 0, n = 0;
-      bool go = true;
-      for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x, ++n) {
-        const RowTile t = row_tile<kMost>(id, feature_tiles, before, start, end, a.groups);
-        const u32 how = instruction(kBf16, kTransposed, false, (t.count + 15) & ~15);
+    if (rank == 0) {
+      u32 s = 0, parity = 0, n = 0;
+      bool ok = true;
+      for (int64_t id = pair; id < tiles; id += pairs, ++n) {
+        const RowTile t = row_tile<kMost, kCtas>(id, feature_tiles, before, start, end, a.groups);
+        const u32 how = instruction<kCtas>(kBf16, kTransposed, false, rounded<kCtas>(t.count));
         const u32 acc = sh.tmem + (n & 1) * kMost;
-        if (!(go = bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit))) break;
+        ok = ok && bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit);
         tmem_fence_after();
-        for (int d = 0; d < depth; ++d, ++turn) {
-          const u32 s = turn % kStages;
-          if (!(go = bar_wait(smem_at(&sh.full[s]), (turn / kStages) & 1, quit))) break;
-          tmem_fence_after();
-          const u32 at = tiles_at + s * kBytes;
-          const int steps = (min(kDepth, a.k - d * kDepth) + 15) >> 4;
-          for (int i = 0; i < steps; ++i)
-            mma(acc, kTransposed ? operand(at + i * 2048, kBoxBytes, 1024) : operand(at + i * 32, 0, 1024),
-                operand(at + kBytesA + i * 32, 0, 1024), how, d | i);
-          mma_commit(smem_at(&sh.empty[s]));
+        for (int d = 0; d < a.k; d += kDepth) {
+          ok = ok && bar_wait(smem_at(&sh.full[s]), parity, quit);
+          __syncwarp();
+          if (elected() && ok) {
+            const u32 at = tiles_at + s * kBytes;
+            multiply<kCtas, kTransposed, false>(acc, operand(at, kTransposed ? kBoxBytes : 0, 1024), Stage::kHalfA,
+                                                operand(at + kBytesA, 0, 1024), Stage::kHalfB, how, (min(kDepth, a.k - d) + 15) >> 4, d == 0);
+            mma_commit<kCtas>(smem_at(&sh.empty[s]));
+            if (d + kDepth >= a.k) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
+          }
+          __syncwarp();
+          if (++s == kStages) {
+            s = 0;
+            parity ^= 1;
+          }
         }
-        if (go) mma_commit(smem_at(&sh.done[n & 1]));
       }
-      if (!go) settle(sh);
+      if (elected() && !ok) settle<kCtas>(sh);
     }
   } else if (warp == 3) {  // rows of no group
     const int64_t head = a.groups ? limited(a.offsets[0], a.rows) : a.rows, tail = limited(a.offsets[a.groups], a.rows);
@@ -312,38 +425,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
     }
   } else if (warp >= 4) {
     u32 n = 0;
-    const int part = warp & 3;  // the lanes of the accumulator that this warp may read
+    const int part = warp & 3, first = (warp >> 2) == 1 ? 0 : 32;  // the lanes that this warp may read, and its first columns
+    const u32 swap = (lane & 1) ? 0x3276 : 0x5410;
     T* y = static_cast<T*>(a.y);
-    for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x, ++n) {
-      const RowTile t = row_tile<kMost>(id, feature_tiles, before, start, end, a.groups);
-      if (!__all_sync(kAll, bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit))) break;
+    for (int64_t id = pair; id < tiles; id += pairs, ++n) {
+      const RowTile t = row_tile<kMost, kCtas>(id, feature_tiles, before, start, end, a.groups);
+      bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit);  // given up: go on with what there is
+      __syncwarp();
       tmem_fence_after();
-      const int f = t.feature + part * 32 + lane;
-      T* to = y + (int64_t)t.row * a.ldy + f;
-      for (int c0 = 0; c0 < t.count; c0 += 32) {
+      const int f = t.feature + (int)rank * kLanes + part * 32 + lane;
+      for (int c0 = first; c0 < t.count; c0 += 64) {
         float v[32];
         tmem_read(v, sh.tmem + (n & 1) * kMost + c0 + ((u32)(part * 32) << 16));
+        T* to = y + (int64_t)(t.row + c0) * a.ldy + f;
+        const int left = f < a.m ? t.count - c0 : 0;
         if (a.pairs) {  // lanes of a pair of features exchange halves of two tokens, and each writes one token's pair
-          const bool odd = lane & 1;
+          const int odd = lane & 1;
+          to += odd * (a.ldy - 1);
 #pragma unroll
           for (int c = 0; c < 32; c += 2) {
-            const float other = __shfl_xor_sync(kAll, odd ? v[c] : v[c + 1], 1);
-            T two[2] = {from_float<T>(odd ? other : v[c]), from_float<T>(odd ? v[c + 1] : other)};
-            const int row = c0 + c + odd;
-            if (row < t.count && f < a.m) *reinterpret_cast<u32*>(to + (int64_t)row * a.ldy - odd) = *reinterpret_cast<u32*>(two);
+            const u32 own = packed(v[c], v[c + 1], T()), other = __shfl_xor_sync(kAll, own, 1);
+            if (c + odd < left) *reinterpret_cast<u32*>(to) = __byte_perm(own, other, swap);
+            to += 2 * a.ldy;
           }
-        } else if (f < a.m) {
+        } else {
 #pragma unroll
-          for (int c = 0; c < 32; ++c)
-            if (c0 + c < t.count) to[(int64_t)(c0 + c) * a.ldy] = from_float<T>(v[c]);
+          for (int c = 0; c < 32; ++c) {
+            if (c < left) *to = from_float<T>(v[c]);
+            to += a.ldy;
+          }
         }
       }
       tmem_fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(smem_at(&sh.free_[n & 1]));
+      if (lane == 0) bar_arrive_first<kCtas, false>(smem_at(&sh.free_[n & 1]));
     }
   }
-  tear_down(sh, kTmem);
+  tear_down<kCtas>(sh, kTmem);
 }
 
 // ---- out[g] (+)= sum of dy[t] x[t]^T -------------------------------------------------------------------------------------
@@ -354,24 +472,27 @@ struct WeightsArgs {
   int groups, inner, rows, k, m, accumulate;
 };
 
-constexpr int kWeightsThreads = 384;  // as above, with eight warps that write: two for each quarter of the lanes
 // Tokens that one accumulator sums.  The tensor core cuts the running sum off at every step of sixteen products
 // instead of rounding it, so its error grows with the number of steps and always to the same side: 1.8e-5 of the result
 // after 6,000 tokens of one sign.  After this many tokens the sum moves on to registers, where additions round.
 constexpr int kWeightsChain = 256;
-constexpr int kWeightsMost = 256, kWeightsStages = 4;
-constexpr int kWeightsBytesA = kLanes * kDepth * 2, kWeightsStageBytes = kWeightsBytesA + kWeightsMost * kDepth * 2;
-constexpr int kWeightsSmem = kWeightsStages * kWeightsStageBytes + 1024;
+constexpr int kWeightsMost = 256;
+template <int kCtas> struct WeightStage {  // the columns of dy are divided between the blocks of a pair
+  static constexpr int kBytesA = kLanes * kDepth * 2, kBytes = kBytesA + kWeightsMost / kCtas * kDepth * 2;
+  static constexpr int kCount = kCtas == 2 ? 3 : 2;
+  static constexpr int kSmem = kCount * kBytes + 1024;
+};
 
 struct WeightTile { int group, row, count, k, m, columns; };
 
+template <int kCtas>
 __device__ __forceinline__ WeightTile weight_tile(int64_t id, const WeightsArgs& a, int k_tiles, int m_tiles) {
   WeightTile t;
   const int per = k_tiles * m_tiles;
   t.group = (int)(id / per);
   const int in = (int)(id - (int64_t)t.group * per);
   t.m = in / k_tiles * kWeightsMost;
-  t.k = in % k_tiles * kLanes;
+  t.k = in % k_tiles * (kCtas * kLanes);
   t.columns = min(kWeightsMost, a.m - t.m);
   t.row = (int)limited(a.offsets[t.group], a.rows);
   const int end = (int)limited(a.offsets[t.group + 1], a.rows);
@@ -379,92 +500,123 @@ __device__ __forceinline__ WeightTile weight_tile(int64_t id, const WeightsArgs&
   return t;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kWeightsThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
-  constexpr int kStages = kWeightsStages, kMost = kWeightsMost, kTmem = 2 * kMost;
+template <typename T, int kCtas>
+__global__ void __launch_bounds__(kThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
+  typedef WeightStage<kCtas> Stage;
+  constexpr int kStages = Stage::kCount, kMost = kWeightsMost, kTmem = 2 * kMost;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ uint8_t raw[];
   __shared__ Shared<kStages> sh;
   const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  set_up(sh, kTmem, 8);
-  const int k_tiles = (a.k + kLanes - 1) / kLanes, m_tiles = (a.m + kMost - 1) / kMost;
+  const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const u32 rank = cta_rank<kCtas>();
+  set_up<kCtas>(sh, kTmem, kWriters);
+  const int k_tiles = (a.k + kCtas * kLanes - 1) / (kCtas * kLanes), m_tiles = (a.m + kMost - 1) / kMost;
   const int64_t tiles = (int64_t)a.groups * k_tiles * m_tiles;
+  const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
   volatile u32* quit = &sh.quit;
 
   if (warp == 0) {
-    if (lane == 0) {
-      u32 turn = 0;
-      bool go = true;
-      for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x) {
-        const WeightTile t = weight_tile(id, a, k_tiles, m_tiles);
-        const int boxes = (t.columns + kBox - 1) / kBox;
-        for (int d = 0; d < t.count; d += kDepth, ++turn) {
-          const u32 s = turn % kStages;
-          if (!(go = bar_wait(smem_at(&sh.empty[s]), ((turn / kStages) & 1) ^ 1, quit))) break;
-          const u32 at = tiles_at + s * kWeightsStageBytes, bar = smem_at(&sh.full[s]);
-          bar_expect(bar, kWeightsBytesA + boxes * kBoxBytes);
-          tma_2d(at, &x_map, bar, t.k, t.row + d);
-          tma_2d(at + kBoxBytes, &x_map, bar, t.k + kBox, t.row + d);
-          for (int i = 0; i < boxes; ++i) tma_2d(at + kWeightsBytesA + i * kBoxBytes, &dy_map, bar, t.m + i * kBox, t.row + d);
+    u32 s = 0, parity = 1, turn = 0;
+    bool ok = true;
+    const u32 full = in_first<kCtas>(smem_at(&sh.full[0]));
+    for (int64_t id = pair; id < tiles; id += pairs) {
+      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+      const int half = rounded<kCtas>(t.columns) / kCtas, boxes = (half + kBox - 1) / kBox;  // this block's columns of dy
+      const int k = t.k + (int)rank * kLanes, m = t.m + (int)rank * half;
+      for (int d = 0; d < t.count; d += kDepth) {
+        ok = ok && bar_wait(smem_at(&sh.empty[s]), parity, quit);
+        __syncwarp();
+        if (elected() && ok) {
+          // the second block has to mask the end of a group itself, so it hears itself when that has landed
+          const bool end = kCtas == 2 && t.count - d < kDepth && (t.count - d) % 16;
+          const u32 at = tiles_at + s * Stage::kBytes, bytes = Stage::kBytesA + boxes * kBoxBytes;
+          const u32 bar = end && rank ? smem_at(&sh.landed[s]) : full + s * 8;
+          if (rank == 0) bar_expect(smem_at(&sh.full[s]), end ? bytes : kCtas * bytes);
+          else if (end) bar_expect(smem_at(&sh.landed[s]), bytes);
+          tma_2d<kCtas>(at, &x_map, bar, k, t.row + d);
+          tma_2d<kCtas>(at + kBoxBytes, &x_map, bar, k + kBox, t.row + d);
+          for (int i = 0; i < boxes; ++i) tma_2d<kCtas>(at + Stage::kBytesA + i * kBoxBytes, &dy_map, bar, m + i * kBox, t.row + d);
+        }
+        __syncwarp();
+        turn += ok;
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1;
         }
       }
-      drain(sh, turn);
     }
+    if (elected()) drain(sh, turn, rank == 0);
   } else if (warp == 1) {
-    u32 turn = 0, n = 0;
-    bool go = true;
-    for (int64_t id = blockIdx.x; id < tiles && go; id += gridDim.x) {
-      const WeightTile t = weight_tile(id, a, k_tiles, m_tiles);
-      if (!t.count) continue;
-      const u32 how = instruction(kBf16, true, true, (t.columns + 15) & ~15);
-      for (int d = 0; d < t.count; d += kDepth, ++turn) {
-        const u32 acc = sh.tmem + (n & 1) * kMost;
-        const bool begins = d % kWeightsChain == 0, ends = (d + kDepth) % kWeightsChain == 0 || d + kDepth >= t.count;
-        if (begins) {
-          if (!(go = __all_sync(kAll, bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit)))) break;
-          tmem_fence_after();
-        }
-        const u32 s = turn % kStages;
-        if (!(go = __all_sync(kAll, bar_wait(smem_at(&sh.full[s]), (turn / kStages) & 1, quit)))) break;
-        const u32 at = tiles_at + s * kWeightsStageBytes;
+    u32 s = 0, parity = 0, n = 0, ends = 0;  // ends: a bit for each stage, whether an odd number of groups has ended in it
+    bool ok = true;
+    for (int64_t id = pair; id < tiles; id += pairs) {
+      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+      const int columns = rounded<kCtas>(t.columns), boxes = 2 + (columns / kCtas + kBox - 1) / kBox;
+      const u32 how = instruction<kCtas>(kBf16, true, true, columns);
+      for (int d = 0; d < t.count; d += kDepth) {
+        const bool begins = d % kWeightsChain == 0, ends_here = (d + kDepth) % kWeightsChain == 0 || d + kDepth >= t.count;
+        const u32 at = tiles_at + s * Stage::kBytes;
         const int here = min(kDepth, t.count - d), steps = (here + 15) >> 4;
-        if (here & 15) {
+        const bool masks = here & 15;
+        if (rank == 0) {
+          if (begins) {
+            ok = ok && bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit);
+            tmem_fence_after();
+          }
+          ok = ok && bar_wait(smem_at(&sh.full[s]), parity, quit);
+        } else if (masks) {
+          ok = ok && bar_wait(smem_at(&sh.landed[s]), (ends >> s) & 1, quit);
+        }
+        if (masks) {
           // the last lines of the copy belong to the next group, whose values may be anything: zeros in their place
-          const int boxes = 2 + (t.columns + kBox - 1) / kBox, lines = steps * 16 - here;
-          for (int i = lane; i < boxes * lines * 8; i += 32) {
+          const int lines = steps * 16 - here;
+          for (int i = lane; i < boxes * lines * 8 && ok; i += 32) {
             const int box = i / (lines * 8), in = i - box * (lines * 8);
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + box * kBoxBytes + here * 128 + in * 16), "r"(0) : "memory");
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (kCtas == 2) {
+            if (rank == 0) {
+              ok = ok && bar_wait(smem_at(&sh.masked[s]), (ends >> s) & 1, quit);
+              asm volatile("fence.acq_rel.cluster;" ::: "memory");
+            } else if (elected() && ok) {
+              bar_arrive_first<kCtas, true>(smem_at(&sh.masked[s]));
+            }
+            ends ^= 1u << s;
+          }
         }
         __syncwarp();
-        tmem_fence_after();
-        if (lane == 0) {
-          for (int i = 0; i < steps; ++i)
-            mma(acc, operand(at + i * 2048, kBoxBytes, 1024), operand(at + kWeightsBytesA + i * 2048, kBoxBytes, 1024), how, !begins || i);
-          mma_commit(smem_at(&sh.empty[s]));
-          if (ends) mma_commit(smem_at(&sh.done[n & 1]));
+        if (rank == 0 && elected() && ok) {
+          multiply<kCtas, true, true>(sh.tmem + (n & 1) * kMost, operand(at, kBoxBytes, 1024), 0,
+                                      operand(at + Stage::kBytesA, kBoxBytes, 1024), 0, how, steps, begins);
+          mma_commit<kCtas>(smem_at(&sh.empty[s]));
+          if (ends_here) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
         }
         __syncwarp();
-        if (ends) ++n;
+        if (ends_here) ++n;
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1;
+        }
       }
     }
-    if (!go && lane == 0) settle(sh);
+    if (rank == 0 && elected() && !ok) settle<kCtas>(sh);
   } else if (warp >= 4) {
     u32 n = 0;
-    bool go = true;
     const int part = warp & 3, c0 = (warp >> 2) == 1 ? 0 : kMost / 2;  // this warp's lanes, and the first of its columns
-    for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x) {
-      const WeightTile t = weight_tile(id, a, k_tiles, m_tiles);
-      const int k = t.k + part * 32 + lane, columns = t.columns - c0;  // may be none
+    for (int64_t id = pair; id < tiles; id += pairs) {
+      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+      const int k = t.k + (int)rank * kLanes + part * 32 + lane, columns = t.columns - c0;  // may be none
       float* to = a.out + (int64_t)(t.group / a.inner) * a.outer_stride + (int64_t)(t.group % a.inner) * a.inner_stride +
                   (int64_t)(t.m + c0) * a.ld_out + k;
       float sum[kMost / 2];
 #pragma unroll
       for (int c = 0; c < kMost / 2; ++c) sum[c] = 0.0f;
       for (int d = 0; d < t.count; d += kWeightsChain, ++n) {
-        if (!(go = __all_sync(kAll, bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit)))) break;
+        bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit);  // given up: go on with what there is
+        __syncwarp();
         tmem_fence_after();
 #pragma unroll
         for (int c = 0; c < kMost / 2; c += 16) {
@@ -477,9 +629,8 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) k_weights(const __grid_con
         }
         tmem_fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(smem_at(&sh.free_[n & 1]));
+        if (lane == 0) bar_arrive_first<kCtas, false>(smem_at(&sh.free_[n & 1]));
       }
-      if (!go) break;
       if (k >= a.k || (a.accumulate && !t.count)) continue;
       if (a.accumulate) {
 #pragma unroll
@@ -499,7 +650,7 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) k_weights(const __grid_con
       }
     }
   }
-  tear_down(sh, kTmem);
+  tear_down<kCtas>(sh, kTmem);
 }
 
 // ---- copies of operands that TMA cannot read -------------------------------------------------------------------------------
@@ -591,20 +742,38 @@ template <auto kKernel> bool allow_smem(int bytes, int dev) {
   return true;
 }
 
-template <typename T, int kMost, bool kTransposed>
-int launch_rows(const CUtensorMap& w, const CUtensorMap& x, const RowsArgs& a, int64_t tiles, int dev, int sms, cudaStream_t s) {
-  constexpr auto k = k_rows<T, kMost, kTransposed>;
-  if (!allow_smem<k>(RowStage<kMost>::kSmem, dev)) return train_rc(cudaGetLastError());
-  k<<<(int)(tiles < sms ? tiles : sms), kThreads, RowStage<kMost>::kSmem, s>>>(w, x, a);
-  return train_rc(cudaGetLastError());
+// Blocks for `tiles` tiles, one for each SM at most; in pairs if a tile is a pair's.
+template <int kCtas, typename K, typename... Args>
+int launch(K kernel, int64_t tiles, int threads, int smem, int sms, cudaStream_t s, const Args&... args) {
+  const int64_t most = sms / kCtas;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = kCtas;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(tiles < most ? tiles : most) * kCtas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = kCtas == 2 ? 1 : 0;
+  return train_rc(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
-template <typename T>
-int launch_weights(const CUtensorMap& x, const CUtensorMap& dy, const WeightsArgs& a, int64_t tiles, int dev, int sms, cudaStream_t s) {
-  constexpr auto k = k_weights<T>;
-  if (!allow_smem<k>(kWeightsSmem, dev)) return train_rc(cudaGetLastError());
-  k<<<(int)(tiles < sms ? tiles : sms), kWeightsThreads, kWeightsSmem, s>>>(x, dy, a);
-  return train_rc(cudaGetLastError());
+template <typename T, int kMost, bool kTransposed, int kCtas>
+int launch_rows(const CUtensorMap& w, const CUtensorMap& x, const RowsArgs& a, int64_t token_tiles, int dev, int sms, cudaStream_t s) {
+  constexpr auto k = k_rows<T, kMost, kTransposed, kCtas>;
+  constexpr int smem = RowStage<kMost, kCtas>::kSmem;
+  if (!allow_smem<k>(smem, dev)) return train_rc(cudaGetLastError());
+  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)), kThreads, smem, sms, s, w, x, a);
+}
+
+template <typename T, int kCtas>
+int launch_weights(const CUtensorMap& x, const CUtensorMap& dy, const WeightsArgs& a, int dev, int sms, cudaStream_t s) {
+  constexpr auto k = k_weights<T, kCtas>;
+  if (!allow_smem<k>(WeightStage<kCtas>::kSmem, dev)) return train_rc(cudaGetLastError());
+  const int64_t tiles = (int64_t)a.groups * ((a.k + kCtas * kLanes - 1) / (kCtas * kLanes)) * ((a.m + kWeightsMost - 1) / kWeightsMost);
+  return launch<kCtas>(k, tiles, kThreads, WeightStage<kCtas>::kSmem, sms, s, x, dy, a);
 }
 
 constexpr int64_t kMostRows = 0x7FFFFF00;  // coordinates of a copy are 32-bit, and a tile may reach past the end
@@ -652,8 +821,8 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
 
   // The widest tile of tokens: as wide as a group has rows on average (a narrower one reads the weights again for
   // nothing, a wider one holds fewer stages), but narrow enough that every SM has a tile.
-  const int64_t average = rows / groups, features = (m + kLanes - 1) / kLanes;
-  int most = average > 128 ? 256 : average > 64 ? 128 : average > 32 ? 64 : 32;
+  const int64_t average = rows / groups;
+  const int most = average > 64 ? (m > kLanes ? 256 : 128) : average > 32 ? 64 : 32;
   CUtensorMap wm, xm;
   if (!make_map(&wm, w, type, cols, lines, ldw, count, w_stride, transposed ? kDepth : kLanes) ||
       !make_map(&xm, x, type, k, rows, ldx, 0, 0, most < 64 ? most : 64)) return REGTOPK_ERR_CUDA;
@@ -661,20 +830,20 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   a.offsets = offsets; a.y = y; a.ldy = ldy; a.groups = groups; a.weights = weights; a.rows = (int)rows; a.k = (int)k; a.m = (int)m;
   a.shared_weights = count == 1;
   a.pairs = m % 2 == 0 && (rows == 1 || ldy % 2 == 0) && (uintptr_t)y % 4 == 0;
-  const int64_t tiles = (rows / most + groups) * features;
-#define REGTOPK_ROWS(N)                                                                                    \
+  const int64_t tiles = rows / most + groups;  // of tokens, at most
+#define REGTOPK_ROWS(N, C)                                                                                 \
   case N:                                                                                                  \
     if (type == REGTOPK_TYPE_BF16)                                                                         \
-      return transposed ? launch_rows<__nv_bfloat16, N, true>(wm, xm, a, tiles, dev, sms, s)               \
-                        : launch_rows<__nv_bfloat16, N, false>(wm, xm, a, tiles, dev, sms, s);             \
-    return transposed ? launch_rows<__half, N, true>(wm, xm, a, tiles, dev, sms, s)                        \
-                      : launch_rows<__half, N, false>(wm, xm, a, tiles, dev, sms, s)
+      return transposed ? launch_rows<__nv_bfloat16, N, true, C>(wm, xm, a, tiles, dev, sms, s)            \
+                        : launch_rows<__nv_bfloat16, N, false, C>(wm, xm, a, tiles, dev, sms, s);          \
+    return transposed ? launch_rows<__half, N, true, C>(wm, xm, a, tiles, dev, sms, s)                     \
+                      : launch_rows<__half, N, false, C>(wm, xm, a, tiles, dev, sms, s)
   switch (most) {
-    REGTOPK_ROWS(32);
-    REGTOPK_ROWS(64);
-    REGTOPK_ROWS(128);
+    REGTOPK_ROWS(32, 1);
+    REGTOPK_ROWS(64, 1);
+    REGTOPK_ROWS(128, 1);
     default:
-    REGTOPK_ROWS(256);
+    REGTOPK_ROWS(256, 2);
   }
 #undef REGTOPK_ROWS
 }
@@ -717,9 +886,10 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
   }
   a.offsets = offsets; a.out = out; a.ld_out = ld_out; a.inner_stride = inner_stride; a.outer_stride = outer_stride;
   a.groups = groups; a.inner = inner; a.rows = (int)rows; a.k = (int)k; a.m = (int)m; a.accumulate = accumulate;
-  const int64_t tiles = (int64_t)groups * ((k + kLanes - 1) / kLanes) * ((m + kWeightsMost - 1) / kWeightsMost);
-  return type == REGTOPK_TYPE_BF16 ? launch_weights<__nv_bfloat16>(xm, ym, a, tiles, dev, sms, s)
-                                   : launch_weights<__half>(xm, ym, a, tiles, dev, sms, s);
+  const bool pairs = k > kLanes;
+  if (type == REGTOPK_TYPE_BF16)
+    return pairs ? launch_weights<__nv_bfloat16, 2>(xm, ym, a, dev, sms, s) : launch_weights<__nv_bfloat16, 1>(xm, ym, a, dev, sms, s);
+  return pairs ? launch_weights<__half, 2>(xm, ym, a, dev, sms, s) : launch_weights<__half, 1>(xm, ym, a, dev, sms, s);
 }
 
 int regtopk_train_status(void* cuda_stream) {

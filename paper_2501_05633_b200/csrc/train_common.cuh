@@ -185,21 +185,20 @@ __device__ __forceinline__ bool bar_done(u32 bar, u32 parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
 
-// Every wait ends: after two seconds the block gives up, says so here, and leaves (regtopk_train_status).
+// Every wait ends: after four billion cycles (two seconds at the highest clock) the block gives up, says so here, and leaves
+// (regtopk_train_status).
 __device__ unsigned int g_gave_up;
-constexpr uint64_t kPatienceNs = 2000000000ull;
+constexpr long long kPatience = 4000000000ll;
 
 __device__ __noinline__ bool bar_wait_long(u32 bar, u32 parity, volatile u32* quit) {
-  const uint64_t began = now_ns();
-  while (!bar_done(bar, parity)) {
+  long long began = 0;
+  for (u32 tries = 1; !bar_done(bar, parity); ++tries) {
+    if (tries % 32) continue;
+    const long long now = clock64();
+    if (!began) began = now;
     if (*quit) return false;
-    if (now_ns() - began > kPatienceNs) {
+    if (now - began > kPatience) {
       *quit = 1;
       atomicExch(&g_gave_up, 1u);
       return false;
