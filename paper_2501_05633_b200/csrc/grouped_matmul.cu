@@ -164,13 +164,16 @@ __device__ __forceinline__ void multiply(u32 acc, uint64_t a, u32 half_a, uint64
 // Columns come in steps of sixteen, thirty-two for a pair.
 template <int kCtas> __device__ __forceinline__ int rounded(int columns) { return (columns + 16 * kCtas - 1) / (16 * kCtas) * (16 * kCtas); }
 
-// Warp 0 copies, warp 1 multiplies, warp 2 keeps the TMEM, warp 3 clears; warps 4-11 write, two for each quarter of the lanes.
-constexpr int kThreads = 384, kWriters = 8;
+// Warp 0 copies, warp 1 multiplies, warp 2 keeps the TMEM, warp 3 clears; the others write, some for each quarter of the
+// lanes: two where the outputs are rounded to 16 bits (four are no faster), four for the weight gradients, where the time goes
+// into waiting for loads and stores (32,768 tokens over 32 matrices of 1024 x 2304: 183 us against 221 us with two).
+constexpr int kRowShare = 2, kWeightShare = 4;
+constexpr int threads_of(int share) { return 128 + 128 * share; }
 
-// `full`, `free_`, `last` and `masked` are the first block's of a pair alone; the other block's copies and warps arrive there too.
+// `full`, `masked`, `free_` and `last` are the first block's of a pair alone; the other block's copies and warps arrive there too.
 template <int kStages> struct Shared {
   uint64_t full[kStages], empty[kStages];   // a stage has landed; has been used
-  uint64_t landed[kStages], masked[kStages]; // k_weights, pairs: the second block's half of a group's last tokens has landed there; has been masked
+  uint64_t landed[kStages], masked[kStages]; // k_weights: this block's part of a group's last tokens has landed; all of it has been masked
   uint64_t done[2], free_[2], last;          // an accumulator is finished; has been read; all products are done
   u32 tmem, quit;
 };
@@ -181,7 +184,7 @@ template <int kCtas, int kStages> __device__ __forceinline__ void set_up(Shared<
       bar_init(smem_at(&sh.full[i]), 1);
       bar_init(smem_at(&sh.empty[i]), 1);
       bar_init(smem_at(&sh.landed[i]), 1);
-      bar_init(smem_at(&sh.masked[i]), 1);
+      bar_init(smem_at(&sh.masked[i]), kCtas);
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(smem_at(&sh.done[i]), 1);
@@ -217,17 +220,19 @@ template <int kCtas, int kStages> __device__ __forceinline__ void tear_down(Shar
   }
 }
 
-// The copying thread's way through the stages: `turn` counts stages filled so far.
-// After the last one it waits until every stage that was filled has been used, so that nothing is under way when the
-// block ends; if the block has given up, until what was requested has landed (in a pair the first block's barrier
-// says so for both; the second block then waits for the first at the end).
-template <int kStages> __device__ __forceinline__ void drain(Shared<kStages>& sh, u32 turn, bool first) {
+// The copying thread at its end: `turn` stages have been filled.  It waits until each of them has been used, so that nothing is
+// under way when the block ends; if the block has given up, until what was requested has landed.  In a pair the first
+// block's barriers say so for both, and the second block waits for the first at the end.  Bits of `ended`: the stage
+// was last filled with the end of a group (k_weights), whose landing `landed` tells; bits of `odd`: it did so an odd number of times.
+template <int kStages> __device__ __forceinline__ void drain(Shared<kStages>& sh, u32 turn, bool first, u32 ended, u32 odd) {
   volatile u32* quit = &sh.quit;
   const u32 from = turn > (u32)kStages ? turn - kStages : 0;
   for (u32 t = from; t < turn; ++t) {
     u32 never = 0;
     const u32 s = t % kStages, parity = (t / kStages) & 1;
-    if ((*quit || !bar_wait(smem_at(&sh.empty[s]), parity, quit)) && first) bar_wait(smem_at(&sh.full[s]), parity, &never);
+    if (!*quit && bar_wait(smem_at(&sh.empty[s]), parity, quit)) continue;
+    if (ended >> s & 1) bar_wait(smem_at(&sh.landed[s]), (odd >> s & 1) ^ 1, &never);
+    else if (first) bar_wait(smem_at(&sh.full[s]), parity, &never);
   }
 }
 
@@ -250,6 +255,7 @@ struct RowsArgs {
   int pairs;           // two neighbouring elements of y may be written as one word
 };
 
+constexpr int kRowThreads = threads_of(kRowShare);
 constexpr int kTableGroups = REGTOPK_MATMUL_MAX_GROUPS;
 
 // How a group's rows are cut: as many tiles as the widest allows, all of one size but the last.
@@ -286,7 +292,7 @@ template <int kMost, int kCtas> struct RowStage {
 };
 
 template <typename T, int kMost, bool kTransposed, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const RowsArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const RowsArgs a) {
   typedef RowStage<kMost, kCtas> Stage;
   constexpr int kStages = Stage::kCount, kBytesA = Stage::kBytesA, kBytes = Stage::kBytes;
   constexpr int kBoxRows = Stage::kTokens < 64 ? Stage::kTokens : 64;  // tokens of one copy
@@ -295,19 +301,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
   extern __shared__ uint8_t raw[];
   __shared__ Shared<kStages> sh;
   __shared__ int before[kTableGroups + 1], start[kTableGroups], end[kTableGroups];
-  __shared__ int scan[kThreads / 32];
+  __shared__ int scan[kRowThreads / 32];
   const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
   const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   const u32 rank = cta_rank<kCtas>();
 
-  set_up<kCtas>(sh, kTmem, kWriters);
+  set_up<kCtas>(sh, kTmem, 4 * kRowShare);
   // where each group's rows lie and how many tiles come before it; groups that share a matrix one after the other, so that
   // it is read from memory once (four workers over sixteen matrices of 9 MB: 752 MB read without that, 285 MB are needed)
-  constexpr int kPer = (kTableGroups + kThreads - 1) / kThreads;  // groups of a thread
+  constexpr int kPer = (kTableGroups + kRowThreads - 1) / kRowThreads;  // groups of a thread
   {
     int own[kPer], sum = 0;
-    const int per = (a.groups + kThreads - 1) / kThreads, sharers = a.groups / a.weights;
+    const int per = (a.groups + kRowThreads - 1) / kRowThreads, sharers = a.groups / a.weights;
     for (int i = 0; i < per; ++i) {
       const int g = threadIdx.x * per + i;
       own[i] = 0;
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
         }
       }
     }
-    if (elected()) drain(sh, turn, rank == 0);
+    if (elected()) drain(sh, turn, rank == 0, 0, 0);
   } else if (warp == 1) {
     if (rank == 0) {
       u32 s = 0, parity = 0, n = 0;
@@ -425,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
     }
   } else if (warp >= 4) {
     u32 n = 0;
-    const int part = warp & 3, first = (warp >> 2) == 1 ? 0 : 32;  // the lanes that this warp may read, and its first columns
+    const int part = warp & 3, first = ((warp >> 2) - 1) * 32;  // the lanes that this warp may read, and its first columns
     const u32 swap = (lane & 1) ? 0x3276 : 0x5410;
     T* y = static_cast<T*>(a.y);
     for (int64_t id = pair; id < tiles; id += pairs, ++n) {
@@ -434,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows(const __grid_constant__ CU
       __syncwarp();
       tmem_fence_after();
       const int f = t.feature + (int)rank * kLanes + part * 32 + lane;
-      for (int c0 = first; c0 < t.count; c0 += 64) {
+      for (int c0 = first; c0 < t.count; c0 += 32 * kRowShare) {
         float v[32];
         tmem_read(v, sh.tmem + (n & 1) * kMost + c0 + ((u32)(part * 32) << 16));
         T* to = y + (int64_t)(t.row + c0) * a.ldy + f;
@@ -474,8 +480,11 @@ struct WeightsArgs {
 
 // Tokens that one accumulator sums.  The tensor core cuts the running sum off at every step of sixteen products
 // instead of rounding it, so its error grows with the number of steps and always to the same side: 1.8e-5 of the result
-// after 6,000 tokens of one sign.  After this many tokens the sum moves on to registers, where additions round.
-constexpr int kWeightsChain = 256;
+// after 6,000 tokens of one sign.  After this many tokens the sum moves on to registers, where additions round: 2.4e-7 for
+// values of one sign, 4.8e-7 for normal ones (256 tokens: 8e-8 and 2.4e-7, but 164 us where this takes 147 us, for 4,096
+// tokens in each of eight groups; 1,024: 1e-6).
+constexpr int kWeightsChain = 512;
+constexpr int kWeightThreads = threads_of(kWeightShare);
 constexpr int kWeightsMost = 256;
 template <int kCtas> struct WeightStage {  // the columns of dy are divided between the blocks of a pair
   static constexpr int kBytesA = kLanes * kDepth * 2, kBytes = kBytesA + kWeightsMost / kCtas * kDepth * 2;
@@ -501,7 +510,7 @@ __device__ __forceinline__ WeightTile weight_tile(int64_t id, const WeightsArgs&
 }
 
 template <typename T, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
+__global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
   typedef WeightStage<kCtas> Stage;
   constexpr int kStages = Stage::kCount, kMost = kWeightsMost, kTmem = 2 * kMost;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -510,14 +519,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights(const __grid_constant__
   const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
   const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const u32 rank = cta_rank<kCtas>();
-  set_up<kCtas>(sh, kTmem, kWriters);
+  set_up<kCtas>(sh, kTmem, 4 * kWeightShare);
   const int k_tiles = (a.k + kCtas * kLanes - 1) / (kCtas * kLanes), m_tiles = (a.m + kMost - 1) / kMost;
   const int64_t tiles = (int64_t)a.groups * k_tiles * m_tiles;
   const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
   volatile u32* quit = &sh.quit;
 
   if (warp == 0) {
-    u32 s = 0, parity = 1, turn = 0;
+    u32 s = 0, parity = 1, turn = 0, ended = 0, odd = 0;
     bool ok = true;
     const u32 full = in_first<kCtas>(smem_at(&sh.full[0]));
     for (int64_t id = pair; id < tiles; id += pairs) {
@@ -525,104 +534,111 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights(const __grid_constant__
       const int half = rounded<kCtas>(t.columns) / kCtas, boxes = (half + kBox - 1) / kBox;  // this block's columns of dy
       const int k = t.k + (int)rank * kLanes, m = t.m + (int)rank * half;
       for (int d = 0; d < t.count; d += kDepth) {
+        const bool end = t.count - d < kDepth && (t.count - d) % 16;
         ok = ok && bar_wait(smem_at(&sh.empty[s]), parity, quit);
         __syncwarp();
         if (elected() && ok) {
-          // the second block has to mask the end of a group itself, so it hears itself when that has landed
-          const bool end = kCtas == 2 && t.count - d < kDepth && (t.count - d) % 16;
+          // the end of a group is masked first, by a warp of the block that has it
           const u32 at = tiles_at + s * Stage::kBytes, bytes = Stage::kBytesA + boxes * kBoxBytes;
-          const u32 bar = end && rank ? smem_at(&sh.landed[s]) : full + s * 8;
-          if (rank == 0) bar_expect(smem_at(&sh.full[s]), end ? bytes : kCtas * bytes);
-          else if (end) bar_expect(smem_at(&sh.landed[s]), bytes);
+          const u32 bar = end ? smem_at(&sh.landed[s]) : full + s * 8;
+          if (end) bar_expect(smem_at(&sh.landed[s]), bytes);
+          if (rank == 0) bar_expect(smem_at(&sh.full[s]), end ? 0 : kCtas * bytes);
           tma_2d<kCtas>(at, &x_map, bar, k, t.row + d);
           tma_2d<kCtas>(at + kBoxBytes, &x_map, bar, k + kBox, t.row + d);
           for (int i = 0; i < boxes; ++i) tma_2d<kCtas>(at + Stage::kBytesA + i * kBoxBytes, &dy_map, bar, m + i * kBox, t.row + d);
         }
         __syncwarp();
         turn += ok;
+        ended = (ended & ~(1u << s)) | (u32)end << s;
+        odd ^= (u32)end << s;
         if (++s == kStages) {
           s = 0;
           parity ^= 1;
         }
       }
     }
-    if (elected()) drain(sh, turn, rank == 0);
+    if (elected()) drain(sh, turn, rank == 0, ended, odd);
   } else if (warp == 1) {
-    u32 s = 0, parity = 0, n = 0, ends = 0;  // ends: a bit for each stage, whether an odd number of groups has ended in it
-    bool ok = true;
-    for (int64_t id = pair; id < tiles; id += pairs) {
-      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
-      const int columns = rounded<kCtas>(t.columns), boxes = 2 + (columns / kCtas + kBox - 1) / kBox;
-      const u32 how = instruction<kCtas>(kBf16, true, true, columns);
-      for (int d = 0; d < t.count; d += kDepth) {
-        const bool begins = d % kWeightsChain == 0, ends_here = (d + kDepth) % kWeightsChain == 0 || d + kDepth >= t.count;
-        const u32 at = tiles_at + s * Stage::kBytes;
-        const int here = min(kDepth, t.count - d), steps = (here + 15) >> 4;
-        const bool masks = here & 15;
-        if (rank == 0) {
+    if (rank == 0) {
+      u32 s = 0, parity = 0, n = 0, odd = 0;  // odd: a bit for each stage, whether an odd number of groups has ended in it
+      bool ok = true;
+      for (int64_t id = pair; id < tiles; id += pairs) {
+        const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+        const u32 how = instruction<kCtas>(kBf16, true, true, rounded<kCtas>(t.columns));
+        for (int d = 0; d < t.count; d += kDepth) {
+          const bool begins = d % kWeightsChain == 0, ends = (d + kDepth) % kWeightsChain == 0 || d + kDepth >= t.count;
+          const int here = min(kDepth, t.count - d);
           if (begins) {
             ok = ok && bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit);
             tmem_fence_after();
           }
           ok = ok && bar_wait(smem_at(&sh.full[s]), parity, quit);
-        } else if (masks) {
-          ok = ok && bar_wait(smem_at(&sh.landed[s]), (ends >> s) & 1, quit);
-        }
-        if (masks) {
-          // the last lines of the copy belong to the next group, whose values may be anything: zeros in their place
-          const int lines = steps * 16 - here;
-          for (int i = lane; i < boxes * lines * 8 && ok; i += 32) {
-            const int box = i / (lines * 8), in = i - box * (lines * 8);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + box * kBoxBytes + here * 128 + in * 16), "r"(0) : "memory");
+          if (here & 15) {
+            ok = ok && bar_wait(smem_at(&sh.masked[s]), (odd >> s) & 1, quit);
+            if (kCtas == 2) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+            odd ^= 1u << s;
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (kCtas == 2) {
-            if (rank == 0) {
-              ok = ok && bar_wait(smem_at(&sh.masked[s]), (ends >> s) & 1, quit);
-              asm volatile("fence.acq_rel.cluster;" ::: "memory");
-            } else if (elected() && ok) {
-              bar_arrive_first<kCtas, true>(smem_at(&sh.masked[s]));
-            }
-            ends ^= 1u << s;
+          if (elected() && ok) {
+            const u32 at = tiles_at + s * Stage::kBytes;
+            multiply<kCtas, true, true>(sh.tmem + (n & 1) * kMost, operand(at, kBoxBytes, 1024), 0,
+                                        operand(at + Stage::kBytesA, kBoxBytes, 1024), 0, how, (here + 15) >> 4, begins);
+            mma_commit<kCtas>(smem_at(&sh.empty[s]));
+            if (ends) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
           }
-        }
-        __syncwarp();
-        if (rank == 0 && elected() && ok) {
-          multiply<kCtas, true, true>(sh.tmem + (n & 1) * kMost, operand(at, kBoxBytes, 1024), 0,
-                                      operand(at + Stage::kBytesA, kBoxBytes, 1024), 0, how, steps, begins);
-          mma_commit<kCtas>(smem_at(&sh.empty[s]));
-          if (ends_here) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
-        }
-        __syncwarp();
-        if (ends_here) ++n;
-        if (++s == kStages) {
-          s = 0;
-          parity ^= 1;
+          __syncwarp();
+          if (ends) ++n;
+          if (++s == kStages) {
+            s = 0;
+            parity ^= 1;
+          }
         }
       }
+      if (elected() && !ok) settle<kCtas>(sh);
     }
-    if (rank == 0 && elected() && !ok) settle<kCtas>(sh);
+  } else if (warp == 3) {
+    // The last lines of a group's last copy belong to the next group, whose values may be anything: zeros in their place, up
+    // to the sixteen lines that a product takes.
+    u32 s = 0, odd = 0;
+    bool ok = true;
+    for (int64_t id = pair; id < tiles; id += pairs) {
+      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+      if (!t.count) continue;
+      s = (s + (t.count - 1) / kDepth) % kStages;  // the stage of its last copy
+      if (t.count & 15) {
+        const u32 at = tiles_at + s * Stage::kBytes + (t.count % kDepth) * 128;
+        const int lines = 16 - (t.count & 15), boxes = 2 + (rounded<kCtas>(t.columns) / kCtas + kBox - 1) / kBox;
+        ok = ok && bar_wait(smem_at(&sh.landed[s]), (odd >> s) & 1, quit);
+        for (int box = 0; box < boxes && ok; ++box)
+          for (int i = lane; i < lines * 8; i += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + box * kBoxBytes + i * 16), "r"(0) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (elected() && ok) bar_arrive_first<kCtas, true>(smem_at(&sh.masked[s]));
+        odd ^= 1u << s;
+      }
+      if (++s == kStages) s = 0;
+    }
   } else if (warp >= 4) {
     u32 n = 0;
-    const int part = warp & 3, c0 = (warp >> 2) == 1 ? 0 : kMost / 2;  // this warp's lanes, and the first of its columns
+    constexpr int kOwn = kMost / kWeightShare;
+    const int part = warp & 3, c0 = ((warp >> 2) - 1) * kOwn;  // this warp's lanes, and the first of its columns
+    const u32 from = sh.tmem + c0 + ((u32)(part * 32) << 16);
     for (int64_t id = pair; id < tiles; id += pairs) {
       const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
       const int k = t.k + (int)rank * kLanes + part * 32 + lane, columns = t.columns - c0;  // may be none
-      float* to = a.out + (int64_t)(t.group / a.inner) * a.outer_stride + (int64_t)(t.group % a.inner) * a.inner_stride +
-                  (int64_t)(t.m + c0) * a.ld_out + k;
-      float sum[kMost / 2];
+      float sum[kOwn];
 #pragma unroll
-      for (int c = 0; c < kMost / 2; ++c) sum[c] = 0.0f;
+      for (int c = 0; c < kOwn; ++c) sum[c] = 0.0f;
       for (int d = 0; d < t.count; d += kWeightsChain, ++n) {
         bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit);  // given up: go on with what there is
         __syncwarp();
         tmem_fence_after();
 #pragma unroll
-        for (int c = 0; c < kMost / 2; c += 16) {
+        for (int c = 0; c < kOwn; c += 16) {
           if (c < columns) {
             float v[16];
-            tmem_read16(v, sh.tmem + (n & 1) * kMost + c0 + c + ((u32)(part * 32) << 16));
+            tmem_read16(v, from + (n & 1) * kMost + c);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum[c + i] += v[i];
           }
@@ -632,21 +648,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights(const __grid_constant__
         if (lane == 0) bar_arrive_first<kCtas, false>(smem_at(&sh.free_[n & 1]));
       }
       if (k >= a.k || (a.accumulate && !t.count)) continue;
-      if (a.accumulate) {
+      float* to = a.out + (int64_t)(t.group / a.inner) * a.outer_stride + (int64_t)(t.group % a.inner) * a.inner_stride +
+                  (int64_t)(t.m + c0) * a.ld_out + k;
 #pragma unroll
-        for (int c = 0; c < kMost / 2; c += 16) {
-          float old[16];
+      for (int c = 0; c < kOwn; c += 16) {
+        float* next = to;
+        if (a.accumulate) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (c + i < columns) old[i] = to[(c + i) * a.ld_out];
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (c + i < columns) to[(c + i) * a.ld_out] = sum[c + i] + old[i];
+          for (int i = 0; i < 16; ++i, next += a.ld_out)
+            if (c + i < columns) sum[c + i] += *next;
         }
-      } else {
 #pragma unroll
-        for (int c = 0; c < kMost / 2; ++c)
-          if (c < columns) to[c * a.ld_out] = sum[c];
+        for (int i = 0; i < 16; ++i, to += a.ld_out)
+          if (c + i < columns) *to = sum[c + i];
       }
     }
   }
@@ -765,7 +779,7 @@ int launch_rows(const CUtensorMap& w, const CUtensorMap& x, const RowsArgs& a, i
   constexpr auto k = k_rows<T, kMost, kTransposed, kCtas>;
   constexpr int smem = RowStage<kMost, kCtas>::kSmem;
   if (!allow_smem<k>(smem, dev)) return train_rc(cudaGetLastError());
-  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)), kThreads, smem, sms, s, w, x, a);
+  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)), kRowThreads, smem, sms, s, w, x, a);
 }
 
 template <typename T, int kCtas>
@@ -773,7 +787,7 @@ int launch_weights(const CUtensorMap& x, const CUtensorMap& dy, const WeightsArg
   constexpr auto k = k_weights<T, kCtas>;
   if (!allow_smem<k>(WeightStage<kCtas>::kSmem, dev)) return train_rc(cudaGetLastError());
   const int64_t tiles = (int64_t)a.groups * ((a.k + kCtas * kLanes - 1) / (kCtas * kLanes)) * ((a.m + kWeightsMost - 1) / kWeightsMost);
-  return launch<kCtas>(k, tiles, kThreads, WeightStage<kCtas>::kSmem, sms, s, x, dy, a);
+  return launch<kCtas>(k, tiles, kWeightThreads, WeightStage<kCtas>::kSmem, sms, s, x, dy, a);
 }
 
 constexpr int64_t kMostRows = 0x7FFFFF00;  // coordinates of a copy are 32-bit, and a tile may reach past the end
