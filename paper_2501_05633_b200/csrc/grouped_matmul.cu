@@ -264,24 +264,31 @@ __device__ __forceinline__ int tile_rows(int count, int most) {
   return tiles ? ((count + tiles - 1) / tiles + 15) & ~15 : 16;
 }
 
-struct RowTile { int group, row, count, feature; };
-
-template <int kMost, int kCtas>
-__device__ __forceinline__ RowTile row_tile(int64_t id, int feature_tiles, const int* before, const int* start, const int* end, int groups) {
-  const int at = (int)(id / feature_tiles);
-  int lo = 0, hi = groups;  // the last group with before[g] <= at
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (before[mid] <= at) lo = mid; else hi = mid;
+// The tiles of a pair (or a block), every `pairs`-th of all: for each tile of tokens those of the features one after the other.
+// Each warp walks through them by additions.
+struct RowWalk {
+  int token_tiles, feature_tiles, step_tokens, step_features;
+  int at, in, group;               // tile of tokens, tile of features; the former's group
+  int row, count, feature;         // the tile: first token, tokens, first feature
+  const int *before, *start, *end; // of each group in the table's order: tiles of tokens before it, its rows
+  template <int kMost, int kCtas> __device__ __forceinline__ void find() {
+    if (at >= token_tiles) return;
+    while (at >= before[group + 1]) ++group;
+    const int step = tile_rows(end[group] - start[group], kMost);
+    row = start[group] + (at - before[group]) * step;
+    count = min(step, end[group] - row);
+    feature = in * (kCtas * kLanes);
   }
-  const int step = tile_rows(end[lo] - start[lo], kMost);
-  RowTile t;
-  t.group = lo;
-  t.row = start[lo] + (at - before[lo]) * step;
-  t.count = min(step, end[lo] - t.row);
-  t.feature = (int)(id - (int64_t)at * feature_tiles) * (kCtas * kLanes);
-  return t;
-}
+  template <int kMost, int kCtas> __device__ __forceinline__ void next() {
+    at += step_tokens;
+    in += step_features;
+    if (in >= feature_tiles) {
+      in -= feature_tiles;
+      ++at;
+    }
+    find<kMost, kCtas>();
+  }
+};
 
 // The tokens of a tile, of which there are up to kMost, are divided between the blocks of a pair.
 template <int kMost, int kCtas> struct RowStage {
@@ -350,16 +357,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
     __syncthreads();
   }
   const int feature_tiles = (a.m + kCtas * kLanes - 1) / (kCtas * kLanes);
-  const int64_t tiles = (int64_t)before[a.groups] * feature_tiles;
-  const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
+  const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas, tiles = before[a.groups];
+  RowWalk t{tiles, feature_tiles, pairs / feature_tiles, pairs % feature_tiles, pair / feature_tiles, pair % feature_tiles, 0, 0, 0, 0, before, start, end};
+  t.find<kMost, kCtas>();
   volatile u32* quit = &sh.quit;
 
   if (warp == 0) {
     u32 s = 0, parity = 1, turn = 0;
     bool ok = true;
     const u32 full = in_first<kCtas>(smem_at(&sh.full[0]));
-    for (int64_t id = pair; id < tiles; id += pairs) {
-      const RowTile t = row_tile<kMost, kCtas>(id, feature_tiles, before, start, end, a.groups);
+    for (; t.at < tiles; t.next<kMost, kCtas>()) {
       const int e = a.shared_weights ? 0 : t.group / (a.groups / a.weights);
       const int here = rounded<kCtas>(t.count) / kCtas, boxes = (here + kBoxRows - 1) / kBoxRows;  // this block's tokens
       const int feature = t.feature + (int)rank * kLanes, row = t.row + (int)rank * here;
@@ -394,8 +401,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
     if (rank == 0) {
       u32 s = 0, parity = 0, n = 0;
       bool ok = true;
-      for (int64_t id = pair; id < tiles; id += pairs, ++n) {
-        const RowTile t = row_tile<kMost, kCtas>(id, feature_tiles, before, start, end, a.groups);
+      for (; t.at < tiles; t.next<kMost, kCtas>(), ++n) {
         const u32 how = instruction<kCtas>(kBf16, kTransposed, false, rounded<kCtas>(t.count));
         const u32 acc = sh.tmem + (n & 1) * kMost;
         ok = ok && bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit);
@@ -434,8 +440,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
     const int part = warp & 3, first = ((warp >> 2) - 1) * 32;  // the lanes that this warp may read, and its first columns
     const u32 swap = (lane & 1) ? 0x3276 : 0x5410;
     T* y = static_cast<T*>(a.y);
-    for (int64_t id = pair; id < tiles; id += pairs, ++n) {
-      const RowTile t = row_tile<kMost, kCtas>(id, feature_tiles, before, start, end, a.groups);
+    for (; t.at < tiles; t.next<kMost, kCtas>(), ++n) {
       bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit);  // given up: go on with what there is
       __syncwarp();
       tmem_fence_after();
@@ -492,22 +497,31 @@ template <int kCtas> struct WeightStage {  // the columns of dy are divided betw
   static constexpr int kSmem = kCount * kBytes + 1024;
 };
 
-struct WeightTile { int group, row, count, k, m, columns; };
-
-template <int kCtas>
-__device__ __forceinline__ WeightTile weight_tile(int64_t id, const WeightsArgs& a, int k_tiles, int m_tiles) {
-  WeightTile t;
-  const int per = k_tiles * m_tiles;
-  t.group = (int)(id / per);
-  const int in = (int)(id - (int64_t)t.group * per);
-  t.m = in / k_tiles * kWeightsMost;
-  t.k = in % k_tiles * (kCtas * kLanes);
-  t.columns = min(kWeightsMost, a.m - t.m);
-  t.row = (int)limited(a.offsets[t.group], a.rows);
-  const int end = (int)limited(a.offsets[t.group + 1], a.rows);
-  t.count = max(end - t.row, 0);
-  return t;
-}
+// The tiles of a pair (or a block), every `pairs`-th of all: for each group the tiles of its matrix.
+struct WeightWalk {
+  int groups, k_tiles, tiles, step_groups, step_tiles;  // tiles: of a matrix
+  int group, in;
+  int row, count, k, m, columns;  // the tile: its group's rows; first column of x, first column and columns of dy
+  const int2* rows;               // of each group: first row, number of rows
+  int all_m;
+  template <int kCtas> __device__ __forceinline__ void find() {
+    if (group >= groups) return;
+    row = rows[group].x;
+    count = rows[group].y;
+    m = in / k_tiles * kWeightsMost;
+    k = in % k_tiles * (kCtas * kLanes);
+    columns = min(kWeightsMost, all_m - m);
+  }
+  template <int kCtas> __device__ __forceinline__ void next() {
+    group += step_groups;
+    in += step_tiles;
+    if (in >= tiles) {
+      in -= tiles;
+      ++group;
+    }
+    find<kCtas>();
+  }
+};
 
 template <typename T, int kCtas>
 __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
@@ -516,21 +530,27 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ uint8_t raw[];
   __shared__ Shared<kStages> sh;
+  __shared__ int2 rows[kTableGroups];
   const u32 tiles_at = (smem_at(raw) + 1023) & ~1023u;
   const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const u32 rank = cta_rank<kCtas>();
   set_up<kCtas>(sh, kTmem, 4 * kWeightShare);
-  const int k_tiles = (a.k + kCtas * kLanes - 1) / (kCtas * kLanes), m_tiles = (a.m + kMost - 1) / kMost;
-  const int64_t tiles = (int64_t)a.groups * k_tiles * m_tiles;
+  for (int g = threadIdx.x; g < a.groups; g += kWeightThreads) {
+    const int lo = (int)limited(a.offsets[g], a.rows), hi = (int)limited(a.offsets[g + 1], a.rows);
+    rows[g] = make_int2(lo, max(hi - lo, 0));
+  }
+  __syncthreads();
+  const int k_tiles = (a.k + kCtas * kLanes - 1) / (kCtas * kLanes), m_tiles = (a.m + kMost - 1) / kMost, matrix = k_tiles * m_tiles;
   const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
+  WeightWalk t{a.groups, k_tiles, matrix, pairs / matrix, pairs % matrix, pair / matrix, pair % matrix, 0, 0, 0, 0, 0, rows, a.m};
+  t.find<kCtas>();
   volatile u32* quit = &sh.quit;
 
   if (warp == 0) {
     u32 s = 0, parity = 1, turn = 0, ended = 0, odd = 0;
     bool ok = true;
     const u32 full = in_first<kCtas>(smem_at(&sh.full[0]));
-    for (int64_t id = pair; id < tiles; id += pairs) {
-      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+    for (; t.group < a.groups; t.next<kCtas>()) {
       const int half = rounded<kCtas>(t.columns) / kCtas, boxes = (half + kBox - 1) / kBox;  // this block's columns of dy
       const int k = t.k + (int)rank * kLanes, m = t.m + (int)rank * half;
       for (int d = 0; d < t.count; d += kDepth) {
@@ -562,8 +582,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
     if (rank == 0) {
       u32 s = 0, parity = 0, n = 0, odd = 0;  // odd: a bit for each stage, whether an odd number of groups has ended in it
       bool ok = true;
-      for (int64_t id = pair; id < tiles; id += pairs) {
-        const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+      for (; t.group < a.groups; t.next<kCtas>()) {
         const u32 how = instruction<kCtas>(kBf16, true, true, rounded<kCtas>(t.columns));
         for (int d = 0; d < t.count; d += kDepth) {
           const bool begins = d % kWeightsChain == 0, ends = (d + kDepth) % kWeightsChain == 0 || d + kDepth >= t.count;
@@ -601,8 +620,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
     // to the sixteen lines that a product takes.
     u32 s = 0, odd = 0;
     bool ok = true;
-    for (int64_t id = pair; id < tiles; id += pairs) {
-      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+    for (; t.group < a.groups; t.next<kCtas>()) {
       if (!t.count) continue;
       s = (s + (t.count - 1) / kDepth) % kStages;  // the stage of its last copy
       if (t.count & 15) {
@@ -624,8 +642,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
     constexpr int kOwn = kMost / kWeightShare;
     const int part = warp & 3, c0 = ((warp >> 2) - 1) * kOwn;  // this warp's lanes, and the first of its columns
     const u32 from = sh.tmem + c0 + ((u32)(part * 32) << 16);
-    for (int64_t id = pair; id < tiles; id += pairs) {
-      const WeightTile t = weight_tile<kCtas>(id, a, k_tiles, m_tiles);
+    for (; t.group < a.groups; t.next<kCtas>()) {
       const int k = t.k + (int)rank * kLanes + part * 32 + lane, columns = t.columns - c0;  // may be none
       float sum[kOwn];
 #pragma unroll
@@ -845,6 +862,7 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   a.shared_weights = count == 1;
   a.pairs = m % 2 == 0 && (rows == 1 || ldy % 2 == 0) && (uintptr_t)y % 4 == 0;
   const int64_t tiles = rows / most + groups;  // of tokens, at most
+  if (tiles * ((m + kLanes - 1) / kLanes) > INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
 #define REGTOPK_ROWS(N, C)                                                                                 \
   case N:                                                                                                  \
     if (type == REGTOPK_TYPE_BF16)                                                                         \
@@ -900,6 +918,7 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
   }
   a.offsets = offsets; a.out = out; a.ld_out = ld_out; a.inner_stride = inner_stride; a.outer_stride = outer_stride;
   a.groups = groups; a.inner = inner; a.rows = (int)rows; a.k = (int)k; a.m = (int)m; a.accumulate = accumulate;
+  if ((k + kLanes - 1) / kLanes * ((m + kWeightsMost - 1) / kWeightsMost) * groups > INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
   const bool pairs = k > kLanes;
   if (type == REGTOPK_TYPE_BF16)
     return pairs ? launch_weights<__nv_bfloat16, 2>(xm, ym, a, dev, sms, s) : launch_weights<__nv_bfloat16, 1>(xm, ym, a, dev, sms, s);
