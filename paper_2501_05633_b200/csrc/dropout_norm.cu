@@ -61,27 +61,26 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
   const u32 first = blockIdx.x * (kDropThreads * kDropStep);
-  {
-    Eight<T> v[kDropStep];
-    u32 row[kDropStep], group[kDropStep];
+  Eight<T> v[kDropStep];
+  u32 row[kDropStep], group[kDropStep];
+  begin_after_predecessor();
 #pragma unroll
-    for (int i = 0; i < kDropStep; ++i) {
-      const u32 at = first + i * kDropThreads + threadIdx.x;
-      row[i] = __umulhi(at, a.magic) >> a.shift;
-      group[i] = at - row[i] * a.groups;
-      if (at < a.total) v[i].fetch(x + row[i] * a.ldx + group[i] * 8);
-    }
+  for (int i = 0; i < kDropStep; ++i) {
+    const u32 at = first + i * kDropThreads + threadIdx.x;
+    row[i] = __umulhi(at, a.magic) >> a.shift;
+    group[i] = at - row[i] * a.groups;
+    if (at < a.total) v[i].fetch(x + row[i] * a.ldx + group[i] * 8);
+  }
 #pragma unroll
-    for (int i = 0; i < kDropStep; ++i) {
-      const u32 at = first + i * kDropThreads + threadIdx.x;
-      if (a.drop.threshold) {
-        Octet f;
-        v[i].get(f);
-        Numbers(a.drop, row[i], group[i]).drop(f, a.drop);
-        v[i].put(f);
-      }
-      if (at < a.total) v[i].store(y + row[i] * a.ldy + group[i] * 8);
+  for (int i = 0; i < kDropStep; ++i) {
+    const u32 at = first + i * kDropThreads + threadIdx.x;
+    if (a.drop.threshold) {
+      Octet f;
+      v[i].get(f);
+      Numbers(a.drop, row[i], group[i]).drop(f, a.drop);
+      v[i].put(f);
     }
+    if (at < a.total) v[i].store(y + row[i] * a.ldy + group[i] * 8);
   }
 }
 
@@ -92,6 +91,7 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_any(const DropoutArgs 
   T* y = static_cast<T*>(a.y);
   const int lane = threadIdx.x & 31;
   const int64_t units = (a.cols + 255) >> 8, total = a.rows * units;
+  begin_after_predecessor();
   const int64_t step = (int64_t)gridDim.x * (kDropThreads / 32);
   for (int64_t at = (int64_t)blockIdx.x * (kDropThreads / 32) + (threadIdx.x >> 5); at < total; at += step) {
     const int64_t row = total >> 32 ? at / units : (u32)at / (u32)units, col0 = (at - row * units) << 8;
@@ -112,12 +112,11 @@ int launch_dropout(DropoutArgs& a, bool vec, int sms, cudaStream_t s) {
     a.total = (u32)(a.rows * groups);
     a.magic = groups == 1 ? 0u : (u32)(((uint64_t)1 << (31 + s31)) / (uint64_t)groups + 1);
     a.shift = groups == 1 ? 0u : (u32)(s31 - 1);
-    k_dropout_vec<T><<<(a.total + kDropThreads * kDropStep - 1) / (kDropThreads * kDropStep), kDropThreads, 0, s>>>(a);
+    return start(k_dropout_vec<T>, (a.total + kDropThreads * kDropStep - 1) / (kDropThreads * kDropStep), kDropThreads, 0, s, a);
   } else {
     const int64_t tasks = (a.rows * ((a.cols + 255) >> 8) + kDropThreads / 32 - 1) / (kDropThreads / 32), most = (int64_t)sms * 8;
-    k_dropout_any<T><<<(int)(tasks < most ? tasks : most), kDropThreads, 0, s>>>(a);
+    return start(k_dropout_any<T>, (unsigned)(tasks < most ? tasks : most), kDropThreads, 0, s, a);
   }
-  return train_rc(cudaGetLastError());
 }
 
 // ---- rows through shared memory ------------------------------------------------------------------------------------
@@ -298,6 +297,7 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
   extern __shared__ __align__(16) char smem[];
   __shared__ Common common;
   const Team t(a.ring.warps, U);
+  begin_after_predecessor();
   float *weight = reinterpret_cast<float*>(smem), *bias = weight + padded(a.cols);
   const int64_t first = (int64_t)blockIdx.x * a.ring.teams + t.index, step = (int64_t)gridDim.x * a.ring.teams;
   Ring ring = make_ring<RING>(common, a.ring, a.source, reinterpret_cast<char*>(bias + padded(a.cols)), t, first, step, a.rows);
@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
   extern __shared__ __align__(16) char smem[];
   __shared__ Common common;
   const Team t(a.ring.warps, U);
+  begin_after_predecessor();
   float *weight = reinterpret_cast<float*>(smem), *joint = weight + padded(a.cols);  // joint: the teams' sums, if there are two or more
   const int64_t r0 = blockIdx.x * a.block_rows, r1 = min(a.rows, r0 + a.block_rows), first = r0 + t.index, step = a.ring.teams;
   Ring ring = make_ring<RING>(common, a.ring, a.source, reinterpret_cast<char*>(joint + (a.ring.teams > 1 ? 2 * padded(a.cols) : 0)), t, first, step, r1);
@@ -431,7 +432,6 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const float inv = 1.0f / (float)a.cols;
   u32 turn = 0;
   int64_t row = first;
@@ -585,7 +585,7 @@ struct NormSumArgs {
 
 __global__ void __launch_bounds__(256) k_norm_sum(const NormSumArgs a) {
   __shared__ float part[2][8][32];
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while k_norm_back ends
+  begin_after_predecessor();
   const int g = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
   const int64_t lo = offset_at(a.offsets, g, a.rows), hi = offset_at(a.offsets, g + 1, a.rows);
   float w = 0.0f, b = 0.0f;
@@ -689,12 +689,9 @@ int launch_norm(const NormArgs& a, const Plan& p, int dev, int sms, cudaStream_t
   if (p.rings) {
     constexpr auto k = k_norm<T, S, VEC, U, true>;
     if (!allow_smem<k>(dev)) return train_rc(cudaGetLastError());
-    k<<<blocks, p.threads, p.smem, s>>>(a);
-  } else {
-    constexpr auto k = k_norm<T, S, VEC, U, false>;
-    k<<<blocks, p.threads, 0, s>>>(a);
+    return start(k, blocks, p.threads, p.smem, s, a);
   }
-  return train_rc(cudaGetLastError());
+  return start(k_norm<T, S, VEC, U, false>, blocks, p.threads, 0, s, a);
 }
 
 template <typename T, typename S, bool VEC, int U>
@@ -703,13 +700,11 @@ int launch_norm_back(const NormBackArgs& a, const Plan& p, int dev, cudaStream_t
   if (p.rings) {
     constexpr auto k = k_norm_back<T, S, VEC, U, true>;
     if (!allow_smem<k>(dev)) return train_rc(cudaGetLastError());
-    k<<<blocks, p.threads, p.smem, s>>>(a);
-  } else {
-    constexpr auto k = k_norm_back<T, S, VEC, U, false>;
-    if (!allow_smem<k>(dev)) return train_rc(cudaGetLastError());
-    k<<<blocks, p.threads, p.smem, s>>>(a);
+    return start(k, blocks, p.threads, p.smem, s, a);
   }
-  return train_rc(cudaGetLastError());
+  constexpr auto k = k_norm_back<T, S, VEC, U, false>;
+  if (!allow_smem<k>(dev)) return train_rc(cudaGetLastError());
+  return start(k, blocks, p.threads, p.smem, s, a);
 }
 
 // For the workspace's size, which is asked for without a device.
@@ -842,16 +837,7 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
     NormSumArgs n;
     n.partial = static_cast<const float*>(workspace); n.dweight = dweight; n.dbias = dbias; n.ld_dweight = ld_dweight; n.ld_dbias = ld_dbias;
     n.rows = rows; n.block_rows = a.block_rows; n.cols = (int)cols; n.accumulate = accumulate; n.offsets = offsets;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)((cols + 31) / 32), (unsigned)groups);
-    cfg.blockDim = dim3(32, 8);
-    cfg.stream = s;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return train_rc(cudaLaunchKernelEx(&cfg, k_norm_sum, n));
+    return start(k_norm_sum, dim3((unsigned)((cols + 31) / 32), (unsigned)groups), dim3(32, 8), 0, s, n);
   }
   return REGTOPK_OK;
 }

@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
   const u32 rank = cta_rank<kCtas>();
 
   set_up<kCtas>(sh, kTmem, 4 * kRowShare);
+  begin_after_predecessor();
   // where each group's rows lie and how many tiles come before it; groups that share a matrix one after the other, so that
   // it is read from memory once (four workers over sixteen matrices of 9 MB: 752 MB read without that, 285 MB are needed)
   constexpr int kPer = (kTableGroups + kRowThreads - 1) / kRowThreads;  // groups of a thread
@@ -535,6 +536,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
   const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const u32 rank = cta_rank<kCtas>();
   set_up<kCtas>(sh, kTmem, 4 * kWeightShare);
+  begin_after_predecessor();
   for (int g = threadIdx.x; g < a.groups; g += kWeightThreads) {
     const int lo = (int)limited(a.offsets[g], a.rows), hi = (int)limited(a.offsets[g + 1], a.rows);
     rows[g] = make_int2(lo, max(hi - lo, 0));
@@ -686,29 +688,37 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
 
 // ---- copies of operands that TMA cannot read -------------------------------------------------------------------------------
 struct CopyArgs {
-  const uint16_t* from;
-  uint16_t* to;
-  int64_t ld, stride, ld_to, lines, cols;  // `lines` lines a matrix, matrices `stride` apart
-  int64_t total;                           // lines of all matrices
+  const char* from;
+  uint4* to;
+  int64_t pitch, stride;    // bytes from line to line and from matrix to matrix
+  int64_t lines, total;     // lines of a matrix and of all
+  int cols, words;          // of a line: elements, 16-byte words of the copy
 };
-__global__ void __launch_bounds__(256) k_copy(const CopyArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t units = (a.cols + 255) >> 8, all = a.total * units, step = (int64_t)gridDim.x * 8;
-  for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < all; at += step) {
-    const int64_t line = at / units, c0 = (at - line * units) << 8;
-    const uint16_t* from = a.from + line / a.lines * a.stride + line % a.lines * a.ld;
-    uint16_t* to = a.to + line * a.ld_to;
-    uint16_t v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t c = c0 + j * 32 + lane;
-      if (c < a.cols) v[j] = from[c];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t c = c0 + j * 32 + lane;
-      if (c < a.cols) to[c] = v[j];
-    }
+struct CopyBoth { CopyArgs c[2]; unsigned blocks; };  // the second's work begins at block `blocks`
+
+// A thread writes one word of eight elements from the two aligned words that hold them, shifted together.  Those at the ends of
+// a line may hold bytes of others, which belong to the same allocation; they land past the columns, where nobody looks.
+constexpr int kCopyThreads = 256;
+__global__ void __launch_bounds__(kCopyThreads) k_copy(const __grid_constant__ CopyBoth both) {
+  const bool second = blockIdx.x >= both.blocks;
+  const CopyArgs& a = both.c[second];
+  const unsigned block = blockIdx.x - (second ? both.blocks : 0), blocks = second ? gridDim.x - both.blocks : both.blocks;
+  const int64_t all = a.total * a.words, step = (int64_t)blocks * kCopyThreads;
+  begin_after_predecessor();
+  for (int64_t at = (int64_t)block * kCopyThreads + threadIdx.x; at < all; at += step) {
+    const int64_t line = all >> 32 ? at / a.words : (u32)at / (u32)a.words;
+    const int word = (int)(at - line * a.words);
+    const int64_t matrix = a.total == a.lines ? 0 : line / a.lines;
+    const char* p = a.from + matrix * a.stride + (line - matrix * a.lines) * a.pitch + word * 16;
+    const u32 skip = (u32)(uintptr_t)p & 15u;  // even
+    const uint4* q = reinterpret_cast<const uint4*>(p - skip);
+    const uint4 lo = q[0], hi = 16 - (int)skip < min(16, (a.cols - word * 8) * 2) ? q[1] : make_uint4(0, 0, 0, 0);
+    u32 w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (skip & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = w[6], w[5] = w[7];
+    if (skip & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = w[4], w[4] = w[5];
+    const u32 shift = (skip & 2) * 8;
+    a.to[at] = make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift),
+                          __funnelshift_r(w[2], w[3], shift), __funnelshift_r(w[3], w[4], shift));
   }
 }
 
@@ -751,19 +761,33 @@ bool direct(const void* p, int64_t ld, int64_t lines, int count, int64_t stride)
 int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
 size_t copy_bytes(int64_t lines, int64_t cols, int count) { return ((size_t)lines * count * padded(cols) * 2 + 255) / 256 * 256; }
 
-// Copies matrices into the workspace at *ws and makes p, ld and stride describe the copy.
-int copy_in(const void** p, int64_t* ld, int64_t lines, int64_t cols, int count, int64_t* stride, char** ws, int sms, cudaStream_t s) {
-  CopyArgs c;
-  c.from = static_cast<const uint16_t*>(*p); c.to = reinterpret_cast<uint16_t*>(*ws); c.ld = *ld; c.stride = *stride;
-  c.ld_to = padded(cols); c.lines = lines; c.cols = cols; c.total = lines * count;
-  const int64_t blocks = (c.total * ((cols + 255) / 256) + 7) / 8, most = (int64_t)sms * 8;
-  k_copy<<<(int)(blocks < most ? blocks : most), 256, 0, s>>>(c);
-  *p = *ws;
-  *ws += copy_bytes(lines, cols, count);
-  *ld = c.ld_to;
-  *stride = lines * c.ld_to;
-  return train_rc(cudaGetLastError());
-}
+// Operands to copy into the workspace, and their copies.
+struct Copies {
+  CopyBoth both;
+  int count = 0;
+  char* ws;
+  // Makes p, ld and stride describe the copy.
+  void add(const void** p, int64_t* ld, int64_t lines, int64_t cols, int matrices, int64_t* stride) {
+    CopyArgs& c = both.c[count++];
+    c.from = static_cast<const char*>(*p); c.to = reinterpret_cast<uint4*>(ws); c.pitch = *ld * 2; c.stride = *stride * 2;
+    c.lines = lines; c.total = lines * matrices; c.cols = (int)cols; c.words = (int)(padded(cols) / 8);
+    *p = ws;
+    ws += copy_bytes(lines, cols, matrices);
+    *ld = padded(cols);
+    *stride = lines * *ld;
+  }
+  int run(int sms, cudaStream_t s) {
+    if (!count) return REGTOPK_OK;
+    unsigned blocks[2] = {0, 0};
+    for (int i = 0; i < count; ++i) {
+      const int64_t n = (both.c[i].total * both.c[i].words + kCopyThreads - 1) / kCopyThreads, most = (int64_t)sms * 16;
+      blocks[i] = (unsigned)(n < most ? n : most);
+    }
+    both.blocks = blocks[0];
+    if (count == 1) both.c[1] = both.c[0];
+    return start(k_copy, blocks[0] + blocks[1], kCopyThreads, 0, s, both);
+  }
+};
 
 template <auto kKernel> bool allow_smem(int bytes, int dev) {
   static uint64_t done;  // of this kernel, one bit a device
@@ -777,18 +801,7 @@ template <auto kKernel> bool allow_smem(int bytes, int dev) {
 template <int kCtas, typename K, typename... Args>
 int launch(K kernel, int64_t tiles, int threads, int smem, int sms, cudaStream_t s, const Args&... args) {
   const int64_t most = sms / kCtas;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = kCtas;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)(tiles < most ? tiles : most) * kCtas);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = kCtas == 2 ? 1 : 0;
-  return train_rc(cudaLaunchKernelEx(&cfg, kernel, args...));
+  return start<kCtas>(kernel, (unsigned)(tiles < most ? tiles : most) * kCtas, threads, smem, s, args...);
 }
 
 template <typename T, int kMost, bool kTransposed, int kCtas>
@@ -843,12 +856,14 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   const size_t need = regtopk_grouped_matmul_workspace_bytes(x, ldx, w, ldw, w_stride, transposed, weights, rows, k, m);
   if (need && (!workspace || (uintptr_t)workspace % 16)) return REGTOPK_ERR_INVALID_ARG;
   if (workspace_bytes < need) return REGTOPK_ERR_WORKSPACE_TOO_SMALL;
-  char* ws = static_cast<char*>(workspace);
   const int count = w_stride ? weights : 1;
   int64_t none = 0;
-  int rc;
-  if (!direct(x, ldx, rows, 1, 0) && (rc = copy_in(&x, &ldx, rows, k, 1, &none, &ws, sms, s))) return rc;
-  if (!direct(w, ldw, lines, count, w_stride) && (rc = copy_in(&w, &ldw, lines, cols, count, &w_stride, &ws, sms, s))) return rc;
+  Copies copies;
+  copies.ws = static_cast<char*>(workspace);
+  if (!direct(x, ldx, rows, 1, 0)) copies.add(&x, &ldx, rows, k, 1, &none);
+  if (!direct(w, ldw, lines, count, w_stride)) copies.add(&w, &ldw, lines, cols, count, &w_stride);
+  const int rc = copies.run(sms, s);
+  if (rc != REGTOPK_OK) return rc;
 
   // The widest tile of tokens: as wide as a group has rows on average (a narrower one reads the weights again for
   // nothing, a wider one holds fewer stages), but narrow enough that every SM has a tile.
@@ -900,17 +915,19 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
   int dev, sms;
   if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  int64_t none = 0;
-  int rc;
   WeightsArgs a;
   CUtensorMap xm, ym;
   if (rows > 0) {
     const size_t need = regtopk_grouped_matmul_dw_workspace_bytes(dy, ld_dy, x, ldx, groups, rows, k, m);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return REGTOPK_ERR_INVALID_ARG;
     if (workspace_bytes < need) return REGTOPK_ERR_WORKSPACE_TOO_SMALL;
-    char* ws = static_cast<char*>(workspace);
-    if (!direct(dy, ld_dy, rows, 1, 0) && (rc = copy_in(&dy, &ld_dy, rows, m, 1, &none, &ws, sms, s))) return rc;
-    if (!direct(x, ldx, rows, 1, 0) && (rc = copy_in(&x, &ldx, rows, k, 1, &none, &ws, sms, s))) return rc;
+    int64_t none = 0;
+    Copies copies;
+    copies.ws = static_cast<char*>(workspace);
+    if (!direct(dy, ld_dy, rows, 1, 0)) copies.add(&dy, &ld_dy, rows, m, 1, &none);
+    if (!direct(x, ldx, rows, 1, 0)) copies.add(&x, &ldx, rows, k, 1, &none);
+    const int rc = copies.run(sms, s);
+    if (rc != REGTOPK_OK) return rc;
     if (!make_map(&xm, x, type, k, rows, ldx, 0, 0, kDepth) || !make_map(&ym, dy, type, m, rows, ld_dy, 0, 0, kDepth)) return REGTOPK_ERR_CUDA;
   } else {
     memset(&xm, 0, sizeof xm);  // never used: no group has rows

@@ -210,12 +210,40 @@ __device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, volatile u32* quit
   return bar_done(bar, parity) || bar_wait_long(bar, parity, quit);
 }
 
+// ---- launches that overlap ---------------------------------------------------------------------------------------
+// Every kernel here is launched with programmatic stream serialisation: its blocks may be started while the kernel before
+// it in the stream still runs.  It lets its own successor start early in turn, and waits for its predecessor before it
+// touches any memory that a kernel may write.
+__device__ __forceinline__ void begin_after_predecessor() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // ---- host --------------------------------------------------------------------------------------------------------
 inline int train_rc(cudaError_t e) {
   if (e == cudaSuccess) return REGTOPK_OK;
   cudaGetLastError();
   return e == cudaErrorNoDevice || e == cudaErrorInsufficientDriver || e == cudaErrorNoKernelImageForDevice
              ? REGTOPK_ERR_NO_DEVICE : REGTOPK_ERR_CUDA;
+}
+
+// Launches a kernel as described at begin_after_predecessor; kCtas 2: in pairs of blocks.
+template <int kCtas = 1, typename... Params, typename... Args>
+int start(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCtas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = kCtas == 2 ? 2 : 1;
+  return train_rc(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
 constexpr int kMaxDevices = 64;
