@@ -238,16 +238,25 @@ template <bool VEC> __device__ __forceinline__ void read_vector(Octet& f, const 
     for (int i = 0; i < 4; ++i) f[i] = make_float2(p[64 * i], p[64 * i + 32]);
   }
 }
-// The same eight columns straight from global memory, for a team that has one row alone.  NULL: zeros.
-template <bool VEC> __device__ __forceinline__ void load_vector(Octet& f, const float* from, int64_t c0, int lane, int cols) {
-  float e[8];
+// The same eight columns straight from global memory, for a team that has few rows.  `wide`: the vector is 16-byte aligned.  NULL:
+// zeros.
+template <bool VEC> __device__ __forceinline__ void load_vector(Octet& f, const float* from, bool wide, int64_t c0, int lane, int cols) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int64_t c = c0 + lane_col<VEC>(lane, j);
-    e[j] = from && c < cols ? from[c] : 0.0f;
+  for (int i = 0; i < 4; ++i) f[i] = both(0.0f);
+  if (!from) return;
+  if (VEC && wide) {
+    if (c0 + lane * 8 >= cols) return;
+    const float4* p = reinterpret_cast<const float4*>(from + c0 + lane * 8);
+    const float4 lo = p[0], hi = p[1];
+    f[0] = make_float2(lo.x, lo.y); f[1] = make_float2(lo.z, lo.w);
+    f[2] = make_float2(hi.x, hi.y); f[3] = make_float2(hi.z, hi.w);
+  } else {
+    float e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = c0 + lane_col<VEC>(lane, j) < cols ? from[c0 + lane_col<VEC>(lane, j)] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(e[2 * i], e[2 * i + 1]);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = make_float2(e[2 * i], e[2 * i + 1]);
 }
 
 // Shared memory of a block: barriers, values that the warps of a team exchange, vectors, rings.
@@ -282,7 +291,7 @@ struct NormArgs {
   void *y, *h;
   float *mean, *rstd;
   int64_t ldy, ldh, rows;
-  int cols;
+  int cols, wide;
   float eps;
   Drop drop;
   RingShape ring;
@@ -368,8 +377,8 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
         read_vector<VEC>(w, weight, c0, t.lane);
         read_vector<VEC>(b, bias, c0, t.lane);
       } else {
-        load_vector<VEC>(w, a.weight, c0, t.lane, a.cols);
-        load_vector<VEC>(b, a.bias, c0, t.lane, a.cols);
+        load_vector<VEC>(w, a.weight, a.wide, c0, t.lane, a.cols);
+        load_vector<VEC>(b, a.bias, a.wide, c0, t.lane, a.cols);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[u][i] = fma2(mul2(add2(f[u][i], both(-mean)), both(rstd)), w[i], b[i]);
@@ -384,7 +393,7 @@ struct NormBackArgs {
   const float *mean, *rstd, *weight;
   void *dx, *dres;
   int64_t ld_dx, ld_dres, rows, block_rows;
-  int cols, groups;
+  int cols, groups, wide;
   const int64_t* offsets;  // NULL: one group of all rows
   float* partial;          // [blocks + groups][2][cols], or NULL: no weight gradients
   Drop drop;
@@ -467,15 +476,17 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
       const S* h = ring.row_of<S, RING>(row, 1);
       const float shift = -mean * rstd;  // (h - mean) rstd = h rstd + shift
       float2 s1 = both(0.0f), s2 = both(0.0f);
+      constexpr int kKept = RING ? 1 : U;  // without rings, what has been read stays in registers
+      Octet kept_d[kKept], kept_v[kKept], kept_w[kKept];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
-        Octet d, v, w;
+        Octet &d = kept_d[u % kKept], &v = kept_v[u % kKept], &w = kept_w[u % kKept];
         read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);  // zeros past the end, so nothing is added there
         read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
         if (RING) read_vector<VEC>(w, weight, c0, t.lane);
-        else load_vector<VEC>(w, a.weight, c0, t.lane, a.cols);
+        else load_vector<VEC>(w, a.weight, a.wide, c0, t.lane, a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float2 unit = fma2(v[i], both(rstd), both(shift)), p = mul2(d[i], w[i]);
@@ -500,16 +511,17 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
       m2 *= inv;
       // rstd (dy w - m1 - unit m2) = dy w rstd + h slope + level
       const float slope = -m2 * rstd * rstd, level = -(m1 + shift * m2) * rstd;
-      asm volatile("" ::: "memory");  // what follows is read from shared memory again: kept, it would not fit the registers
+      if (RING) asm volatile("" ::: "memory");  // what follows is read from shared memory again: kept, it would not fit the registers
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
-        Octet d, v, w;
-        read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);
-        read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
-        if (RING) read_vector<VEC>(w, weight, c0, t.lane);
-        else load_vector<VEC>(w, a.weight, c0, t.lane, a.cols);
+        Octet &d = kept_d[u % kKept], &v = kept_v[u % kKept], &w = kept_w[u % kKept];
+        if (RING) {
+          read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);
+          read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
+          read_vector<VEC>(w, weight, c0, t.lane);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[i] = fma2(mul2(d[i], w[i]), both(rstd), fma2(v[i], both(slope), both(level)));
         if (a.ring.row_bytes[2]) {
@@ -766,7 +778,7 @@ int regtopk_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t
   a.source[1] = {static_cast<const char*>(residual), ld_residual * (int64_t)ssize};
   a.source[2] = {nullptr, 0};
   a.weight = weight; a.bias = bias; a.y = y; a.h = h; a.mean = mean; a.rstd = rstd; a.ldy = ldy; a.ldh = ldh; a.rows = rows;
-  a.cols = (int)cols; a.eps = eps;
+  a.cols = (int)cols; a.eps = eps; a.wide = (uintptr_t)weight % 16 == 0 && (uintptr_t)bias % 16 == 0;
   // Up to 1,024 columns two units a warp and 24 warps on an SM: 32,768 rows of bfloat16 beside a binary32 stream take
   // 71.7 us, 77.7 us with four units and sixteen warps.  Wider, where the warps of a row wait for one another: 8,192 rows of
   // 4,096 bfloat16 columns 73.7 us against 61.5 us.
@@ -820,7 +832,7 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
     a.source[1] = {static_cast<const char*>(h), ldh * (int64_t)ssize};
     a.source[2] = {static_cast<const char*>(dh), ld_dh * (int64_t)ssize};
     a.mean = mean; a.rstd = rstd; a.weight = weight; a.dx = dx; a.dres = dresidual; a.ld_dx = ld_dx; a.ld_dres = ld_dresidual;
-    a.rows = rows; a.cols = (int)cols; a.groups = groups; a.offsets = offsets; a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    a.rows = rows; a.cols = (int)cols; a.wide = (uintptr_t)weight % 16 == 0; a.groups = groups; a.offsets = offsets; a.partial = sums ? static_cast<float*>(workspace) : nullptr;
     const Plan p = plan_of(cols, rows, {size, ssize, dh ? ssize : 0}, size + ssize == 4 ? 4 : 2, 2, 1, 2, sms);
     a.ring = p.ring;
     const int64_t blocks = (int64_t)sms * (p.blocks < 4 ? p.blocks : 4), turns = (rows + blocks * p.ring.teams - 1) / (blocks * p.ring.teams);
