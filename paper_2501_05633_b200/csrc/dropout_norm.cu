@@ -12,8 +12,8 @@ namespace {
 // ---- eight columns of a row ------------------------------------------------------------------------------------------
 // This lane's columns of the unit that begins at column c0; zeros past the end of the row.  SHARED: the row is in shared
 // memory, otherwise in global.
-template <typename T, bool VEC, bool SHARED>
-__device__ __forceinline__ void read_eight(Octet& f, const T* row, int64_t c0, int lane, int64_t cols) {
+template <typename T, bool VEC, bool SHARED, typename Column>
+__device__ __forceinline__ void read_eight(Octet& f, const T* row, Column c0, int lane, Column cols) {
   if (VEC) {
     Eight<T> v;
     if (c0 + lane * 8 >= cols) v.clear();
@@ -28,8 +28,8 @@ __device__ __forceinline__ void read_eight(Octet& f, const T* row, int64_t c0, i
     for (int i = 0; i < 4; ++i) f[i] = make_float2(e[2 * i], e[2 * i + 1]);
   }
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_eight(const Octet& f, T* row, int64_t c0, int lane, int64_t cols) {
+template <typename T, bool VEC, typename Column>
+__device__ __forceinline__ void store_eight(const Octet& f, T* row, Column c0, int lane, Column cols) {
   if (VEC) {
     Eight<T> v;
     v.put(f);
@@ -128,7 +128,7 @@ int launch_dropout(DropoutArgs& a, bool vec, int sms, cudaStream_t s) {
 // A copy takes whole 16-byte words, those at both ends of an unaligned row included: the other bytes in them belong to
 // the same allocation and are not looked at.
 constexpr int kMostWarps = 16;   // of a block
-constexpr int kMostStages = 8;
+constexpr int kMostStages = 4;
 
 struct Source {  // one array's rows
   const char* p;
@@ -144,13 +144,13 @@ struct RingShape {
 
 struct Team {
   int warps, index, warp, lane;  // its warps; this thread's team, warp within the team, lane
-  int64_t col0;                  // this warp's first column
+  int col0;                      // this warp's first column
   __device__ __forceinline__ Team(int warps_, int units) : warps(warps_) {
     const int w = threadIdx.x >> 5;
     index = w / warps;
     warp = w - index * warps;
     lane = threadIdx.x & 31;
-    col0 = (int64_t)warp * units * 256;
+    col0 = warp * units * 256;
   }
   __device__ __forceinline__ bool leads() const { return warp == 0 && lane == 0; }
   __device__ __forceinline__ void sync() const {
@@ -160,17 +160,24 @@ struct Team {
 };
 
 // A team's ring: it holds the rows first, first + step, ... below `end` of the arrays, one after the other.
-struct Ring {
+// WALKS: where the copies go on from is kept in registers and goes from row to row by additions; otherwise it is worked out
+// from the row.  The forward pass is faster with the former (6,000 rows of 1,000 bfloat16 columns 17.6 us against 19.0 us),
+// the backward pass, which has no registers to spare, with the latter (2,048 rows of 8,192: 73 us against 84 us).
+template <bool WALKS> struct Ring {
   const RingShape& shape;
   const Source* source;
   char* base;
   u32 bars;
   volatile u32* quit;
   int64_t step, end;
-  u32 stage, phase;  // where the next row to be read lies
+  u32 stage, phase;      // where the next row to be read lies
+  const char* ahead[3];  // WALKS: of each array the row to be requested next,
+  int64_t leap[3], left; //   bytes from one to the one after, and how many are left
+  u32 low[3];            //   the low part of the address of the next row to be read
 
-  __device__ __forceinline__ void request(int64_t row, u32 into) const {  // the team's first lane only
-    if (row >= end) return;
+  __device__ __forceinline__ void request(int64_t row, u32 into) {  // the team's first lane only
+    if (WALKS ? left <= 0 : row >= end) return;
+    if (WALKS) --left;
     const u32 bar = bars + into * 8;
     u32 at = smem_at(base) + into * shape.stage_bytes, total = 0;
     u32 to[3], size[3];
@@ -179,13 +186,14 @@ struct Ring {
     for (int i = 0; i < 3; ++i) {
       size[i] = 0;
       if (!shape.row_bytes[i]) continue;
-      const char* p = source[i].p + row * source[i].pitch;
+      const char* p = WALKS ? ahead[i] : source[i].p + row * source[i].pitch;
       const u32 skip = (u32)(uintptr_t)p & 15u;
       from[i] = p - skip;
       to[i] = at;
       size[i] = (skip + shape.row_bytes[i] + 15u) & ~15u;
       total += size[i];
       at += shape.room[i];
+      if (WALKS) ahead[i] += leap[i];
     }
     bar_expect(bar, total);
 #pragma unroll
@@ -197,15 +205,19 @@ struct Ring {
   // Waits for the next row.  Should it not come, the kernel runs to its end with what there is (see bar_wait).
   __device__ __forceinline__ void await() const { bar_wait(bars + stage * 8, phase, quit); }
   // Array number `array` of the next row, which is row `row` of the arrays.
-  template <typename T, bool RING> __device__ __forceinline__ const T* row_of(int64_t row, int array) const {
+  template <typename T, bool VEC, bool RING> __device__ __forceinline__ const T* row_of(int64_t row, int array) const {
     if (!RING) return reinterpret_cast<const T*>(source[array].p + row * source[array].pitch);
     const char* p = base + stage * shape.stage_bytes;
     for (int i = 0; i < array; ++i) p += shape.room[i];
-    return reinterpret_cast<const T*>(p + ((uintptr_t)(source[array].p + row * source[array].pitch) & 15));
+    if (!VEC) p += (WALKS ? low[array] : (u32)(uintptr_t)source[array].p + (u32)row * (u32)source[array].pitch) & 15u;
+    return reinterpret_cast<const T*>(p);
   }
   // The next row, `row`, has been read by the whole team: its place is for the row `stages` rows on.
   __device__ __forceinline__ void pass(int64_t row, bool leads) {
-    if (leads) request(row + shape.stages * step, stage);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (WALKS) low[i] += (u32)leap[i];
+    if (leads) request(WALKS ? 0 : row + shape.stages * step, stage);
     if (++stage == (u32)shape.stages) {
       stage = 0;
       phase ^= 1;
@@ -226,7 +238,7 @@ template <bool VEC> __device__ __forceinline__ void fetch_vector(float* to, cons
     else *dst = 0.0f;
   }
 }
-template <bool VEC> __device__ __forceinline__ void read_vector(Octet& f, const float* from, int64_t c0, int lane) {
+template <bool VEC> __device__ __forceinline__ void read_vector(Octet& f, const float* from, int c0, int lane) {
   if (VEC) {
     const float4 lo = *reinterpret_cast<const float4*>(from + c0 + lane * 4);
     const float4 hi = *reinterpret_cast<const float4*>(from + c0 + 128 + lane * 4);
@@ -240,7 +252,7 @@ template <bool VEC> __device__ __forceinline__ void read_vector(Octet& f, const 
 }
 // The same eight columns straight from global memory, for a team that has few rows.  `wide`: the vector is 16-byte aligned.  NULL:
 // zeros.
-template <bool VEC> __device__ __forceinline__ void load_vector(Octet& f, const float* from, bool wide, int64_t c0, int lane, int cols) {
+template <bool VEC> __device__ __forceinline__ void load_vector(Octet& f, const float* from, bool wide, int c0, int lane, int cols) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = both(0.0f);
   if (!from) return;
@@ -269,12 +281,21 @@ struct Common {
 __device__ __forceinline__ int padded(int cols) { return (cols + 255) & ~255; }
 
 // Sets a team's ring up and requests its first rows.
-template <bool RING>
-__device__ __forceinline__ Ring make_ring(Common& common, const RingShape& shape, const Source* source, char* rings, const Team& t,
-                                          int64_t first, int64_t step, int64_t end) {
-  const Ring ring{shape, source, rings + t.index * shape.stages * shape.stage_bytes, smem_at(&common.bars[t.index][0]), &common.quit,
-                  step, end, 0, 0};
+template <bool RING, bool WALKS>
+__device__ __forceinline__ Ring<WALKS> make_ring(Common& common, const RingShape& shape, const Source* source, char* rings, const Team& t,
+                                                 int64_t first, int64_t step, int64_t end) {
+  Ring<WALKS> ring{shape, source, rings + t.index * shape.stages * shape.stage_bytes, smem_at(&common.bars[t.index][0]), &common.quit,
+                   step, end, 0, 0};
   if (!RING) return ring;
+  if (WALKS) {
+    ring.left = first < end ? (end - first + step - 1) / step : 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      ring.ahead[i] = source[i].p + first * source[i].pitch;
+      ring.leap[i] = step * source[i].pitch;
+      ring.low[i] = (u32)(uintptr_t)ring.ahead[i];
+    }
+  }
   if (threadIdx.x == 0) common.quit = 0;
   if (t.leads()) {
     for (int i = 0; i < shape.stages; ++i) bar_init(ring.bars + i * 8, 1);
@@ -282,6 +303,17 @@ __device__ __forceinline__ Ring make_ring(Common& common, const RingShape& shape
     for (int i = 0; i < shape.stages; ++i) ring.request(first + i * step, i);
   }
   return ring;
+}
+
+// a / b to binary32's accuracy by the reciprocal of b and one correction (Newton); exact where the quotient is a whole number.
+__device__ __forceinline__ float quotient(float a, float b, float reciprocal) {
+  const float q = a * reciprocal, better = fmaf(fmaf(-q, b, a), reciprocal, q);
+  return better == better ? better : q;  // infinity
+}
+// 1 / sqrt(x) by the approximation and one step of Newton's method; where that has no value (0, infinity), the approximation.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float y = rsqrtf(x), better = y * fmaf(-0.5f * x * y, y, 1.5f);
+  return better == better ? better : y;
 }
 
 // ---- layer norm, forward ---------------------------------------------------------------------------------------------
@@ -309,25 +341,29 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
   begin_after_predecessor();
   float *weight = reinterpret_cast<float*>(smem), *bias = weight + padded(a.cols);
   const int64_t first = (int64_t)blockIdx.x * a.ring.teams + t.index, step = (int64_t)gridDim.x * a.ring.teams;
-  Ring ring = make_ring<RING>(common, a.ring, a.source, reinterpret_cast<char*>(bias + padded(a.cols)), t, first, step, a.rows);
+  Ring<true> ring = make_ring<RING, true>(common, a.ring, a.source, reinterpret_cast<char*>(bias + padded(a.cols)), t, first, step, a.rows);
   if (RING) {
     fetch_vector<VEC>(weight, a.weight, a.cols);
     fetch_vector<VEC>(bias, a.bias, a.cols);
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
   }
-  const auto share = [&](int warp) { return (float)max(0, min(U * 256, a.cols - warp * U * 256)); };  // a warp's columns
-  const float own = share(t.warp);
+  // columns of every warp but the last, and of the last; of this warp
+  const float full = U * 256, last = (float)(a.cols - (t.warps - 1) * U * 256), own = t.warp == t.warps - 1 ? last : full;
+  const float cols = (float)a.cols, per_col = 1.0f / cols, per_own = 1.0f / own;
+  T* y = static_cast<T*>(a.y) + first * a.ldy;
+  S* sum_out = static_cast<S*>(a.h) + first * a.ldh;
+  const int64_t y_leap = step * a.ldy, h_leap = step * a.ldh;
   u32 turn = 0;
-  for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+  for (int64_t row = first; row < a.rows; row += step, turn ^= 1, y += y_leap, sum_out += h_leap) {
     if (RING) ring.await();
     Octet f[U];
     float2 sum = both(0.0f), square = both(0.0f);
-    const T* x = ring.row_of<T, RING>(row, 0);
-    const S* residual = ring.row_of<S, RING>(row, 1);
+    const T* x = ring.row_of<T, VEC, RING>(row, 0);
+    const S* residual = ring.row_of<S, VEC, RING>(row, 1);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t c0 = t.col0 + u * 256;
+      const int c0 = t.col0 + u * 256;
       read_eight<T, VEC, RING>(f[u], x, c0, t.lane, a.cols);
       if (a.drop.threshold) drop_unit<VEC>(f[u], a.drop, (uint64_t)row, c0, t.lane);
       if (a.ring.row_bytes[1]) {
@@ -339,10 +375,10 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum = add2(sum, f[u][i]);  // zeros past the end
     }
-    float mean = own > 0.0f ? warp_sum(sum.x + sum.y) / own : 0.0f;
+    float mean = quotient(warp_sum(sum.x + sum.y), own, per_own);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t c0 = t.col0 + u * 256;
+      const int c0 = t.col0 + u * 256;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float2 c = add2(f[u][i], both(-mean));
@@ -357,21 +393,23 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
     if (RING) ring.pass(row, t.leads());
     if (t.warps > 1) {
       const float2* v = &common.exchange[turn][t.index * t.warps];
-      mean = spread = 0.0f;
-      for (int i = 0; i < t.warps; ++i) mean += share(i) * v[i].x;
-      mean /= (float)a.cols;
-      for (int i = 0; i < t.warps; ++i) spread += v[i].y + share(i) * (v[i].x - mean) * (v[i].x - mean);
+      const float2 end = v[t.warps - 1];
+      mean = 0.0f;
+      for (int i = 0; i < t.warps - 1; ++i) mean += v[i].x;
+      mean = quotient(fmaf(full, mean, last * end.x), cols, per_col);
+      spread = fmaf(last * (end.x - mean), end.x - mean, end.y);
+      for (int i = 0; i < t.warps - 1; ++i) spread += fmaf(full * (v[i].x - mean), v[i].x - mean, v[i].y);
     }
-    const float rstd = 1.0f / sqrtf(spread / (float)a.cols + a.eps);
+    const float rstd = inverse_root(fmaf(spread, per_col, a.eps));
     if (t.leads()) {
       a.mean[row] = mean;
       a.rstd[row] = rstd;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t c0 = t.col0 + u * 256;
+      const int c0 = t.col0 + u * 256;
       if (c0 >= a.cols) break;
-      if (a.h) store_eight<S, VEC>(f[u], static_cast<S*>(a.h) + row * a.ldh, c0, t.lane, a.cols);
+      if (a.h) store_eight<S, VEC>(f[u], sum_out, c0, t.lane, a.cols);
       Octet w, b;
       if (RING) {
         read_vector<VEC>(w, weight, c0, t.lane);
@@ -382,7 +420,7 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[u][i] = fma2(mul2(add2(f[u][i], both(-mean)), both(rstd)), w[i], b[i]);
-      store_eight<T, VEC>(f[u], static_cast<T*>(a.y) + row * a.ldy, c0, t.lane, a.cols);
+      store_eight<T, VEC>(f[u], y, c0, t.lane, a.cols);
     }
   }
 }
@@ -429,7 +467,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
   begin_after_predecessor();
   float *weight = reinterpret_cast<float*>(smem), *joint = weight + padded(a.cols);  // joint: the teams' sums, if there are two or more
   const int64_t r0 = blockIdx.x * a.block_rows, r1 = min(a.rows, r0 + a.block_rows), first = r0 + t.index, step = a.ring.teams;
-  Ring ring = make_ring<RING>(common, a.ring, a.source, reinterpret_cast<char*>(joint + (a.ring.teams > 1 ? 2 * padded(a.cols) : 0)), t, first, step, r1);
+  Ring<false> ring = make_ring<RING, false>(common, a.ring, a.source, reinterpret_cast<char*>(joint + (a.ring.teams > 1 ? 2 * padded(a.cols) : 0)), t, first, step, r1);
   if (RING) fetch_vector<VEC>(weight, a.weight, a.cols);
   int g = a.partial ? group_of(a.offsets, a.groups, r0, a.rows, t.lane) : a.groups;
   float mean = 0.0f, rstd = 0.0f;
@@ -472,15 +510,15 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
         next_rstd = a.rstd[row + step];
       }
       if (RING) ring.await();
-      const T* dy = ring.row_of<T, RING>(row, 0);
-      const S* h = ring.row_of<S, RING>(row, 1);
+      const T* dy = ring.row_of<T, VEC, RING>(row, 0);
+      const S* h = ring.row_of<S, VEC, RING>(row, 1);
       const float shift = -mean * rstd;  // (h - mean) rstd = h rstd + shift
       float2 s1 = both(0.0f), s2 = both(0.0f);
       constexpr int kKept = RING ? 1 : U;  // without rings, what has been read stays in registers
       Octet kept_d[kKept], kept_v[kKept], kept_w[kKept];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t c0 = t.col0 + u * 256;
+        const int c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
         Octet &d = kept_d[u % kKept], &v = kept_v[u % kKept], &w = kept_w[u % kKept];
         read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);  // zeros past the end, so nothing is added there
@@ -514,7 +552,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
       if (RING) asm volatile("" ::: "memory");  // what follows is read from shared memory again: kept, it would not fit the registers
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t c0 = t.col0 + u * 256;
+        const int c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
         Octet &d = kept_d[u % kKept], &v = kept_v[u % kKept], &w = kept_w[u % kKept];
         if (RING) {
@@ -525,7 +563,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[i] = fma2(mul2(d[i], w[i]), both(rstd), fma2(v[i], both(slope), both(level)));
         if (a.ring.row_bytes[2]) {
-          read_eight<S, VEC, RING>(v, ring.row_of<S, RING>(row, 2), c0, t.lane, a.cols);
+          read_eight<S, VEC, RING>(v, ring.row_of<S, VEC, RING>(row, 2), c0, t.lane, a.cols);
 #pragma unroll
           for (int i = 0; i < 4; ++i) d[i] = add2(d[i], v[i]);
         }
@@ -545,7 +583,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
           if (t.index == i) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-              const int64_t c0 = t.col0 + u * 256;
+              const int c0 = t.col0 + u * 256;
               if (c0 >= a.cols) break;
               // any place will do that a lane finds again: pair k of the lane's eight lies at k * 64 + lane * 2
               float2 *w = reinterpret_cast<float2*>(joint + c0) + t.lane, *b = reinterpret_cast<float2*>(joint + padded(a.cols) + c0) + t.lane;
@@ -573,7 +611,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int64_t c = t.col0 + u * 256 + lane_col<VEC>(t.lane, j);
+            const int c = t.col0 + u * 256 + lane_col<VEC>(t.lane, j);
             if (c < a.cols) {
               out[c] = (j & 1) ? dw[u][j >> 1].y : dw[u][j >> 1].x;
               out[a.cols + c] = (j & 1) ? db[u][j >> 1].y : db[u][j >> 1].x;
@@ -586,7 +624,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
   }
 }
 
-// The weight gradients: for each group the sum of its blocks' partial sums, eight runs of them side by side.
+// The weight gradients: for each group the sum of its blocks' partial sums, kRuns runs of them side by side.
 struct NormSumArgs {
   const float* partial;
   float *dweight, *dbias;
@@ -595,8 +633,9 @@ struct NormSumArgs {
   const int64_t* offsets;
 };
 
-__global__ void __launch_bounds__(256) k_norm_sum(const NormSumArgs a) {
-  __shared__ float part[2][8][32];
+constexpr int kRuns = 16;
+__global__ void __launch_bounds__(32 * kRuns) k_norm_sum(const NormSumArgs a) {
+  __shared__ float part[2][kRuns][33];
   begin_after_predecessor();
   const int g = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
   const int64_t lo = offset_at(a.offsets, g, a.rows), hi = offset_at(a.offsets, g + 1, a.rows);
@@ -604,7 +643,7 @@ __global__ void __launch_bounds__(256) k_norm_sum(const NormSumArgs a) {
   if (c < a.cols && lo < hi) {
     const int64_t last = (hi - 1) / a.block_rows;
 #pragma unroll 4
-    for (int64_t block = lo / a.block_rows + threadIdx.y; block <= last; block += 8) {
+    for (int64_t block = lo / a.block_rows + threadIdx.y; block <= last; block += kRuns) {
       const float* p = a.partial + (block + g) * 2 * a.cols;
       w += p[c];
       b += p[a.cols + c];
@@ -613,22 +652,26 @@ __global__ void __launch_bounds__(256) k_norm_sum(const NormSumArgs a) {
   part[0][threadIdx.y][threadIdx.x] = w;
   part[1][threadIdx.y][threadIdx.x] = b;
   __syncthreads();
-  if (threadIdx.y < 2 && c < a.cols) {
-    float* out = threadIdx.y ? a.dbias : a.dweight;
-    if (!out) return;
-    float s = 0.0f;
+  // each warp adds the runs of some of the 64 sums, a lane a run
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += part[threadIdx.y][i][threadIdx.x];
-    out += g * (threadIdx.y ? a.ld_dbias : a.ld_dweight) + c;
-    *out = a.accumulate ? *out + s : s;
+  for (int i = threadIdx.y; i < 64; i += kRuns) {
+    const int which = i & 1, at = blockIdx.x * 32 + (i >> 1);
+    const float s = warp_sum((int)threadIdx.x < kRuns ? part[which][threadIdx.x][i >> 1] : 0.0f);
+    float* out = which ? a.dbias : a.dweight;
+    if (threadIdx.x == 0 && out && at < a.cols) {
+      out += g * (which ? a.ld_dbias : a.ld_dweight) + at;
+      *out = a.accumulate ? *out + s : s;
+    }
   }
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
 // How a row is shared and how the shared memory of an SM is divided.
-//   rings: `blocks` blocks of eight warps on an SM (one block of sixteen for the widest rows); a warp takes up to
+//   rings: `blocks` blocks of eight warps on an SM (one of sixteen for the widest rows); a warp takes up to
 //   `most_units` units.  `vectors` float32 vectors of the columns lie beside the rings, `joint` more where a block has two
-//   teams or more.
+//   teams or more.  Two rows of a team are under way, up to four where an SM has fewer than twelve teams (8 teams, 32,768 rows of
+//   1,024 columns, bfloat16 beside a binary32 stream: 69.5 us against 85 us; with twelve, 6,000 rows of 1,000 bfloat16 columns
+//   only start later: 17.8 us against 15.6 us).
 //   no rings, where a team would have one row at most (or two rows do not fit): as many warps a row as it has units,
 //   because then the time is that of one row (backward pass, 1,000 rows of 1,000 columns: 14.3 us against 20.5 us with four
 //   units a warp).
@@ -662,8 +705,9 @@ inline Plan plan_of(int64_t cols, int64_t rows, const size_t (&size)[3], int mos
     for (;; --teams) {
       p.smem = (size_t)column_bytes * (vectors + (teams > 1 ? joint : 0));
       const int stages = (kSmemOfSm / p.blocks - kSmemOfBlock - (int)p.smem) / (teams * p.ring.stage_bytes);
+      const int most_stages = p.blocks * teams >= 12 ? 2 : kMostStages;
       p.ring.teams = teams;
-      p.ring.stages = stages > kMostStages ? kMostStages : stages;
+      p.ring.stages = stages > most_stages ? most_stages : stages;
       if (stages >= 2) break;
       if (teams == 1) {
         if (p.blocks == 1) break;
@@ -779,13 +823,16 @@ int regtopk_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t
   a.source[2] = {nullptr, 0};
   a.weight = weight; a.bias = bias; a.y = y; a.h = h; a.mean = mean; a.rstd = rstd; a.ldy = ldy; a.ldh = ldh; a.rows = rows;
   a.cols = (int)cols; a.eps = eps; a.wide = (uintptr_t)weight % 16 == 0 && (uintptr_t)bias % 16 == 0;
-  // Up to 1,024 columns two units a warp and 24 warps on an SM: 32,768 rows of bfloat16 beside a binary32 stream take
-  // 71.7 us, 77.7 us with four units and sixteen warps.  Wider, where the warps of a row wait for one another: 8,192 rows of
-  // 4,096 bfloat16 columns 73.7 us against 61.5 us.
-  const Plan p = plan_of(cols, rows, {size, residual ? ssize : 0, 0}, cols <= 1024 || size + ssize == 8 ? 2 : 4, cols <= 1024 ? 3 : 2, 2, 0, sms);
-  a.ring = p.ring;
   const bool vec = cols % 8 == 0 && rows_aligned(x, ldx, size, rows) && rows_aligned(y, ldy, size, rows) &&
                    rows_aligned(residual, ld_residual, ssize, rows) && rows_aligned(h, ldh, ssize, rows);
+  // Up to 1,024 columns two units a warp and 24 warps on an SM, sixteen where a binary32 stream comes in beside more than 512; wider,
+  // where the warps of a row wait for one another, four units and sixteen warps.  32,768 rows of 1,024 bfloat16 columns: 61.7 us,
+  // 70.4 us with four units; beside a binary32 stream 69.5 us, 78.0 us with 24 warps; 8,192 rows of 4,096: 55.9 us, 73.7 us with
+  // two units.
+  const bool few = cols > 512 && cols <= 1024 && vec && residual && ssize == 4;
+  const Plan p = plan_of(cols, rows, {size, residual ? ssize : 0, 0}, cols <= 1024 || size + ssize == 8 ? 2 : 4,
+                         cols <= 1024 && !few ? 3 : 2, 2, 0, sms);
+  a.ring = p.ring;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
 #define REGTOPK_NORM(T, S, V, U) launch_norm<T, S, V, U>(a, p, dev, sms, s)
   return REGTOPK_BY_TYPE(REGTOPK_NORM);
@@ -849,7 +896,7 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
     NormSumArgs n;
     n.partial = static_cast<const float*>(workspace); n.dweight = dweight; n.dbias = dbias; n.ld_dweight = ld_dweight; n.ld_dbias = ld_dbias;
     n.rows = rows; n.block_rows = a.block_rows; n.cols = (int)cols; n.accumulate = accumulate; n.offsets = offsets;
-    return start(k_norm_sum, dim3((unsigned)((cols + 31) / 32), (unsigned)groups), dim3(32, 8), 0, s, n);
+    return start(k_norm_sum, dim3((unsigned)((cols + 31) / 32), (unsigned)groups), dim3(32, kRuns), 0, s, n);
   }
   return REGTOPK_OK;
 }
