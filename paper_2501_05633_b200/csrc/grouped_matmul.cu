@@ -694,7 +694,14 @@ struct CopyArgs {
   int64_t lines, total;     // lines of a matrix and of all
   int cols, words;          // of a line: elements, 16-byte words of the copy
 };
-struct CopyBoth { CopyArgs c[2]; unsigned blocks; };  // the second's work begins at block `blocks`
+// The second's work begins at block `blocks`.  Matrices number `skips` holds (the first or the second operand's, or none's) are
+// copied only if one of their groups has rows.
+struct CopyBoth {
+  CopyArgs c[2];
+  unsigned blocks;
+  int skips, groups, weights;
+  const int64_t* offsets;
+};
 
 // A thread writes one word of eight elements from the two aligned words that hold them, shifted together.  Those at the ends of
 // a line may hold bytes of others, which belong to the same allocation; they land past the columns, where nobody looks.
@@ -704,11 +711,21 @@ __global__ void __launch_bounds__(kCopyThreads) k_copy(const __grid_constant__ C
   const CopyArgs& a = both.c[second];
   const unsigned block = blockIdx.x - (second ? both.blocks : 0), blocks = second ? gridDim.x - both.blocks : both.blocks;
   const int64_t all = a.total * a.words, step = (int64_t)blocks * kCopyThreads;
+  __shared__ u32 used[kTableGroups / 32];
   begin_after_predecessor();
+  const bool skips = both.skips == (int)second && both.weights > 1;
+  if (skips) {
+    for (int i = threadIdx.x; i < kTableGroups / 32; i += kCopyThreads) used[i] = 0;
+    __syncthreads();
+    for (int g = threadIdx.x; g < both.groups; g += kCopyThreads)
+      if (both.offsets[g] < both.offsets[g + 1]) atomicOr(&used[g % both.weights / 32], 1u << g % both.weights % 32);
+    __syncthreads();
+  }
   for (int64_t at = (int64_t)block * kCopyThreads + threadIdx.x; at < all; at += step) {
     const int64_t line = all >> 32 ? at / a.words : (u32)at / (u32)a.words;
     const int word = (int)(at - line * a.words);
-    const int64_t matrix = a.total == a.lines ? 0 : line / a.lines;
+    const int64_t matrix = a.total == a.lines ? 0 : a.total >> 31 ? line / a.lines : (u32)line / (u32)a.lines;
+    if (skips && !(used[matrix / 32] >> matrix % 32 & 1)) continue;
     const char* p = a.from + matrix * a.stride + (line - matrix * a.lines) * a.pitch + word * 16;
     const u32 skip = (u32)(uintptr_t)p & 15u;  // even
     const uint4* q = reinterpret_cast<const uint4*>(p - skip);
@@ -776,8 +793,13 @@ struct Copies {
     *ld = padded(cols);
     *stride = lines * *ld;
   }
-  int run(int sms, cudaStream_t s) {
+  // weights > 1: the operand added last is that many matrices, for the groups of `offsets`.
+  int run(const int64_t* offsets, int groups, int weights, int sms, cudaStream_t s) {
     if (!count) return REGTOPK_OK;
+    both.skips = count - 1;
+    both.offsets = offsets;
+    both.groups = groups;
+    both.weights = weights;
     unsigned blocks[2] = {0, 0};
     for (int i = 0; i < count; ++i) {
       const int64_t n = (both.c[i].total * both.c[i].words + kCopyThreads - 1) / kCopyThreads, most = (int64_t)sms * 16;
@@ -861,8 +883,9 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   Copies copies;
   copies.ws = static_cast<char*>(workspace);
   if (!direct(x, ldx, rows, 1, 0)) copies.add(&x, &ldx, rows, k, 1, &none);
-  if (!direct(w, ldw, lines, count, w_stride)) copies.add(&w, &ldw, lines, cols, count, &w_stride);
-  const int rc = copies.run(sms, s);
+  const bool copies_w = !direct(w, ldw, lines, count, w_stride);
+  if (copies_w) copies.add(&w, &ldw, lines, cols, count, &w_stride);
+  const int rc = copies.run(offsets, groups, copies_w ? count : 1, sms, s);
   if (rc != REGTOPK_OK) return rc;
 
   // The widest tile of tokens: as wide as a group has rows on average (a narrower one reads the weights again for
@@ -926,7 +949,7 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
     copies.ws = static_cast<char*>(workspace);
     if (!direct(dy, ld_dy, rows, 1, 0)) copies.add(&dy, &ld_dy, rows, m, 1, &none);
     if (!direct(x, ldx, rows, 1, 0)) copies.add(&x, &ldx, rows, k, 1, &none);
-    const int rc = copies.run(sms, s);
+    const int rc = copies.run(offsets, groups, 1, sms, s);
     if (rc != REGTOPK_OK) return rc;
     if (!make_map(&xm, x, type, k, rows, ldx, 0, 0, kDepth) || !make_map(&ym, dy, type, m, rows, ld_dy, 0, 0, kDepth)) return REGTOPK_ERR_CUDA;
   } else {
