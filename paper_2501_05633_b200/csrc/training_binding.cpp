@@ -137,6 +137,19 @@ regtopk_dropout_params drop_params(PyObject* p, PyObject* seed, PyObject* subseq
 Tensor empty(at::IntArrayRef size, at::ScalarType type, const Tensor& like) {
   return at::detail::empty_cuda(size, type, like.device(), std::nullopt);
 }
+// Two float32 tensors of one size in one allocation: they live and die together, and every allocation costs 0.7 us.
+std::pair<Tensor, Tensor> two_of(at::IntArrayRef size, const Tensor& like) {
+  int64_t n = 1;
+  for (const int64_t s : size) n *= s;
+  const Tensor whole = empty({2 * n}, at::kFloat, like);
+  const auto part = [&](int64_t at) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+    impl->set_storage_offset(at);
+    impl->set_sizes_contiguous(size);
+    return Tensor(std::move(impl));
+  };
+  return {part(0), part(n)};
+}
 void* stream_of(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.device().index()).stream(); }
 void* data(const Tensor* t) { return t ? t->data_ptr() : nullptr; }
 
@@ -170,7 +183,7 @@ PyObject* layer_norm(PyObject* const* a) {  // x, weight, bias, eps, residual, p
   const at::ScalarType stream_type = residual ? residual->scalar_type() : x.scalar_type();
   const c10::cuda::CUDAGuard guard(x.device());
   const Tensor y = empty(x.sizes(), x.scalar_type(), x), h = makes_h ? empty(x.sizes(), stream_type, x) : x;
-  const Tensor mean = empty(x.sizes().slice(0, x.dim() - 1), at::kFloat, x), rstd = empty(mean.sizes(), at::kFloat, x);
+  const auto [mean, rstd] = two_of(x.sizes().slice(0, x.dim() - 1), x);
   check(regtopk_layer_norm(x.data_ptr(), in.ld, data(residual), res.ld, weight, static_cast<const float*>(data(bias)),
                            static_cast<float>(number(a[3])), y.data_ptr(), in.cols, makes_h ? h.data_ptr() : nullptr, in.cols,
                            static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), in.rows, in.cols, type,
@@ -209,7 +222,7 @@ PyObject* layer_norm_backward(PyObject* const* a) {
   const c10::cuda::CUDAGuard guard(dy.device());
   Tensor made[2];
   if (!dw && !db) {
-    for (Tensor& t : made) t = empty({groups, in.cols}, at::kFloat, dy);
+    std::tie(made[0], made[1]) = two_of({groups, in.cols}, dy);
     dw = &made[0];
     db = &made[1];
   }
