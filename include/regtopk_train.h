@@ -95,11 +95,12 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
  * matrices [k][m], used as y[t] = x[t] w: with dy for x and the layer's own [m][k] matrices this is the gradient to the
  * tokens.  groups is a multiple of weights: groups sorted by (worker, expert) share the experts' matrices.
  * Products and sums are binary32 on the tensor cores; y is rounded once.  rows < 2^31; k, m < 2^31; k == 0 gives zeros.
- * workspace: 16-byte aligned, at least regtopk_grouped_matmul_workspace_bytes(...) bytes, which are 0 where x and w have
- * 16-byte aligned rows (base and leading dimension; for w the stride between matrices too) and otherwise hold a copy of
- * the one that has not.  Errors: INVALID_ARG, TOO_LARGE (groups), WORKSPACE_TOO_SMALL, NO_DEVICE, CUDA. */
+ * workspace: 16-byte aligned, at least regtopk_grouped_matmul_workspace_bytes(...) bytes, which hold a copy of
+ * x or w where it has no 16-byte aligned rows (base and leading dimension; for w the stride between matrices too), and partial
+ * sums where k is long and there are few rows; often 0.  Errors: INVALID_ARG, TOO_LARGE (groups), WORKSPACE_TOO_SMALL, NO_DEVICE, CUDA. */
 size_t regtopk_grouped_matmul_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride,
-                                              int32_t transposed, int32_t weights, int64_t rows, int64_t k, int64_t m);
+                                              int32_t transposed, int32_t weights, int32_t groups, int64_t rows, int64_t k,
+                                              int64_t m);
 int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride, int32_t transposed,
                            int32_t weights, void* y, int64_t ldy, const int64_t* offsets, int32_t groups, int64_t rows,
                            int64_t k, int64_t m, int32_t type, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -253,6 +253,9 @@ struct RowsArgs {
   int groups, weights, rows, k, m;
   int shared_weights;  // all matrices are the first one
   int pairs;           // two neighbouring elements of y may be written as one word
+  // The summed dimension is divided into `parts` of `part_k`, each a tile of its own whose sums go to partial [parts][rows][m].
+  int parts, part_k;
+  float* partial;
 };
 
 constexpr int kRowThreads = threads_of(kRowShare);
@@ -268,6 +271,7 @@ __device__ __forceinline__ int tile_rows(int count, int most) {
 // Each warp walks through them by additions.
 struct RowWalk {
   int token_tiles, feature_tiles, step_tokens, step_features;
+  int parts;                       // `in` counts parts of a tile of features
   int at, in, group;               // tile of tokens, tile of features; the former's group
   int row, count, feature;         // the tile: first token, tokens, first feature
   const int *before, *start, *end; // of each group in the table's order: tiles of tokens before it, its rows
@@ -277,8 +281,9 @@ struct RowWalk {
     const int step = tile_rows(end[group] - start[group], kMost);
     row = start[group] + (at - before[group]) * step;
     count = min(step, end[group] - row);
-    feature = in * (kCtas * kLanes);
+    feature = in / parts * (kCtas * kLanes);
   }
+  __device__ __forceinline__ int part() const { return in % parts; }
   template <int kMost, int kCtas> __device__ __forceinline__ void next() {
     at += step_tokens;
     in += step_features;
@@ -357,9 +362,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
     }
     __syncthreads();
   }
-  const int feature_tiles = (a.m + kCtas * kLanes - 1) / (kCtas * kLanes);
+  const int feature_tiles = (a.m + kCtas * kLanes - 1) / (kCtas * kLanes) * a.parts;
   const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas, tiles = before[a.groups];
-  RowWalk t{tiles, feature_tiles, pairs / feature_tiles, pairs % feature_tiles, pair / feature_tiles, pair % feature_tiles, 0, 0, 0, 0, before, start, end};
+  RowWalk t{tiles, feature_tiles, pairs / feature_tiles, pairs % feature_tiles, a.parts, pair / feature_tiles, pair % feature_tiles, 0, 0, 0, 0, before, start, end};
   t.find<kMost, kCtas>();
   volatile u32* quit = &sh.quit;
 
@@ -371,11 +376,12 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
       const int e = a.shared_weights ? 0 : t.group / (a.groups / a.weights);
       const int here = rounded<kCtas>(t.count) / kCtas, boxes = (here + kBoxRows - 1) / kBoxRows;  // this block's tokens
       const int feature = t.feature + (int)rank * kLanes, row = t.row + (int)rank * here;
-      for (int d = 0; d < a.k; d += kDepth) {
+      const int k0 = t.part() * a.part_k, k1 = min(a.k, k0 + a.part_k);
+      for (int d = k0; d < k1; d += kDepth) {
         ok = ok && bar_wait(smem_at(&sh.empty[s]), parity, quit);
         __syncwarp();
         if (elected() && ok) {
-          const int halves = a.k - d > kBox ? 2 : 1;
+          const int halves = k1 - d > kBox ? 2 : 1;
           const u32 at = tiles_at + s * kBytes, bar = full + s * 8;
           if (rank == 0)
             bar_expect(smem_at(&sh.full[s]), kCtas * ((kTransposed ? 2 : halves) * Stage::kHalfA + halves * boxes * kBoxRows * kBox * 2));
@@ -407,15 +413,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
         const u32 acc = sh.tmem + (n & 1) * kMost;
         ok = ok && bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit);
         tmem_fence_after();
-        for (int d = 0; d < a.k; d += kDepth) {
+        const int k0 = t.part() * a.part_k, k1 = min(a.k, k0 + a.part_k);
+        for (int d = k0; d < k1; d += kDepth) {
           ok = ok && bar_wait(smem_at(&sh.full[s]), parity, quit);
           __syncwarp();
           if (elected() && ok) {
             const u32 at = tiles_at + s * kBytes;
             multiply<kCtas, kTransposed, false>(acc, operand(at, kTransposed ? kBoxBytes : 0, 1024), Stage::kHalfA,
-                                                operand(at + kBytesA, 0, 1024), Stage::kHalfB, how, (min(kDepth, a.k - d) + 15) >> 4, d == 0);
+                                                operand(at + kBytesA, 0, 1024), Stage::kHalfB, how, (min(kDepth, k1 - d) + 15) >> 4, d == k0);
             mma_commit<kCtas>(smem_at(&sh.empty[s]));
-            if (d + kDepth >= a.k) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
+            if (d + kDepth >= k1) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
           }
           __syncwarp();
           if (++s == kStages) {
@@ -426,7 +433,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
       }
       if (elected() && !ok) settle<kCtas>(sh);
     }
-  } else if (warp == 3) {  // rows of no group
+  } else if (warp == 3 && a.parts == 1) {  // rows of no group
     const int64_t head = a.groups ? limited(a.offsets[0], a.rows) : a.rows, tail = limited(a.offsets[a.groups], a.rows);
     T* y = static_cast<T*>(a.y);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -451,7 +458,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
         tmem_read(v, sh.tmem + (n & 1) * kMost + c0 + ((u32)(part * 32) << 16));
         T* to = y + (int64_t)(t.row + c0) * a.ldy + f;
         const int left = f < a.m ? t.count - c0 : 0;
-        if (a.pairs) {  // lanes of a pair of features exchange halves of two tokens, and each writes one token's pair
+        if (a.parts > 1) {
+          float* sums = a.partial + ((int64_t)t.part() * a.rows + t.row + c0) * a.m + f;
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            if (c < left) *sums = v[c];
+            sums += a.m;
+          }
+        } else if (a.pairs) {  // lanes of a pair of features exchange halves of two tokens, and each writes one token's pair
           const int odd = lane & 1;
           to += odd * (a.ldy - 1);
 #pragma unroll
@@ -482,6 +496,9 @@ struct WeightsArgs {
   float* out;
   int64_t ld_out, inner_stride, outer_stride;
   int groups, inner, rows, k, m, accumulate;
+  // The rows of a group are divided into `parts`, each a tile of its own, whose matrices lie part_stride apart.
+  int parts;
+  int64_t part_stride;
 };
 
 // Tokens that one accumulator sums.  The tensor core cuts the running sum off at every step of sixteen products
@@ -500,17 +517,24 @@ template <int kCtas> struct WeightStage {  // the columns of dy are divided betw
 
 // The tiles of a pair (or a block), every `pairs`-th of all: for each group the tiles of its matrix.
 struct WeightWalk {
-  int groups, k_tiles, tiles, step_groups, step_tiles;  // tiles: of a matrix
+  int groups, k_tiles, tiles, step_groups, step_tiles;  // tiles: of a matrix, times `parts`
   int group, in;
   int row, count, k, m, columns;  // the tile: its group's rows; first column of x, first column and columns of dy
   const int2* rows;               // of each group: first row, number of rows
-  int all_m;
+  int all_m, parts;
+  __device__ __forceinline__ int part() const { return in % parts; }
   template <int kCtas> __device__ __forceinline__ void find() {
     if (group >= groups) return;
     row = rows[group].x;
     count = rows[group].y;
-    m = in / k_tiles * kWeightsMost;
-    k = in % k_tiles * (kCtas * kLanes);
+    if (parts > 1) {  // whole stages but for the last part
+      const int each = ((count + parts - 1) / parts + kDepth - 1) / kDepth * kDepth, before = min(count, part() * each);
+      row += before;
+      count = min(each, count - before);
+    }
+    const int tile = in / parts;
+    m = tile / k_tiles * kWeightsMost;
+    k = tile % k_tiles * (kCtas * kLanes);
     columns = min(kWeightsMost, all_m - m);
   }
   template <int kCtas> __device__ __forceinline__ void next() {
@@ -542,9 +566,9 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
     rows[g] = make_int2(lo, max(hi - lo, 0));
   }
   __syncthreads();
-  const int k_tiles = (a.k + kCtas * kLanes - 1) / (kCtas * kLanes), m_tiles = (a.m + kMost - 1) / kMost, matrix = k_tiles * m_tiles;
+  const int k_tiles = (a.k + kCtas * kLanes - 1) / (kCtas * kLanes), m_tiles = (a.m + kMost - 1) / kMost, matrix = k_tiles * m_tiles * a.parts;
   const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
-  WeightWalk t{a.groups, k_tiles, matrix, pairs / matrix, pairs % matrix, pair / matrix, pair % matrix, 0, 0, 0, 0, 0, rows, a.m};
+  WeightWalk t{a.groups, k_tiles, matrix, pairs / matrix, pairs % matrix, pair / matrix, pair % matrix, 0, 0, 0, 0, 0, rows, a.m, a.parts};
   t.find<kCtas>();
   volatile u32* quit = &sh.quit;
 
@@ -668,7 +692,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
       }
       if (k >= a.k || (a.accumulate && !t.count)) continue;
       float* to = a.out + (int64_t)(t.group / a.inner) * a.outer_stride + (int64_t)(t.group % a.inner) * a.inner_stride +
-                  (int64_t)(t.m + c0) * a.ld_out + k;
+                  (int64_t)(t.m + c0) * a.ld_out + k + t.part() * a.part_stride;
 #pragma unroll
       for (int c = 0; c < kOwn; c += 16) {
         float* next = to;
@@ -684,6 +708,41 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
     }
   }
   tear_down<kCtas>(sh, kTmem);
+}
+
+// ---- the sums of divided products --------------------------------------------------------------------------------------------
+// Where there are fewer tiles than places to compute them and the summed dimension is long, it is divided (parts_of) and the
+// parts are added here, the first to the last.
+constexpr int kJoinThreads = 256;
+
+// y = the sum of partial [parts][rows][m], rounded; zeros in rows of no group.
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) k_join_rows(const RowsArgs a) {
+  begin_after_predecessor();
+  const int64_t head = limited(a.offsets[0], a.rows), tail = limited(a.offsets[a.groups], a.rows), all = (int64_t)a.rows * a.m;
+  for (int64_t i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kJoinThreads) {
+    const int64_t row = all >> 32 ? i / a.m : (u32)i / (u32)a.m;
+    float s = 0.0f;
+    if (row >= head && row < tail) {
+#pragma unroll 4
+      for (int p = 0; p < a.parts; ++p) s += a.partial[p * all + i];
+    }
+    static_cast<T*>(a.y)[row * a.ldy + (i - row * a.m)] = from_float<T>(s);
+  }
+}
+
+// out (+)= the sum of the parts of each group's matrix; `a` describes out, parts those [parts][groups][m][k].
+__global__ void __launch_bounds__(kJoinThreads) k_join_weights(const WeightsArgs a, const float* parts) {
+  begin_after_predecessor();
+  const int64_t matrix = (int64_t)a.m * a.k, all = matrix * a.groups;
+  for (int64_t i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kJoinThreads) {
+    const int64_t line = all >> 32 ? i / a.k : (u32)i / (u32)a.k, g = all >> 32 ? line / a.m : (u32)line / (u32)a.m;
+    float s = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) s += parts[p * all + i];
+    float* to = a.out + g / a.inner * a.outer_stride + g % a.inner * a.inner_stride + (line - g * a.m) * a.ld_out + (i - line * a.k);
+    *to = a.accumulate ? *to + s : s;
+  }
 }
 
 // ---- copies of operands that TMA cannot read -------------------------------------------------------------------------------
@@ -831,18 +890,31 @@ int launch_rows(const CUtensorMap& w, const CUtensorMap& x, const RowsArgs& a, i
   constexpr auto k = k_rows<T, kMost, kTransposed, kCtas>;
   constexpr int smem = RowStage<kMost, kCtas>::kSmem;
   if (!allow_smem<k>(smem, dev)) return train_rc(cudaGetLastError());
-  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)), kRowThreads, smem, sms, s, w, x, a);
+  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)) * a.parts, kRowThreads, smem, sms, s, w, x, a);
 }
 
 template <typename T, int kCtas>
 int launch_weights(const CUtensorMap& x, const CUtensorMap& dy, const WeightsArgs& a, int dev, int sms, cudaStream_t s) {
   constexpr auto k = k_weights<T, kCtas>;
   if (!allow_smem<k>(WeightStage<kCtas>::kSmem, dev)) return train_rc(cudaGetLastError());
-  const int64_t tiles = (int64_t)a.groups * ((a.k + kCtas * kLanes - 1) / (kCtas * kLanes)) * ((a.m + kWeightsMost - 1) / kWeightsMost);
+  const int64_t tiles = (int64_t)a.groups * ((a.k + kCtas * kLanes - 1) / (kCtas * kLanes)) * ((a.m + kWeightsMost - 1) / kWeightsMost) * a.parts;
   return launch<kCtas>(k, tiles, kWeightThreads, WeightStage<kCtas>::kSmem, sms, s, x, dy, a);
 }
 
+// Into how many parts the summed dimension is divided: as many as there are places for (those of 148 SMs, whatever the device has,
+// since the workspace's size is asked for without one), but none shorter than 512.  One: not divided.
+int parts_of(int64_t tiles, int64_t places, int64_t summed) {
+  const int64_t most = tiles > 0 ? places / tiles : 1, parts = summed / 512;
+  return (int)(parts < most ? (parts < 1 ? 1 : parts) : most < 1 ? 1 : most);
+}
+constexpr int kPlaces = 148;
+
 constexpr int64_t kMostRows = 0x7FFFFF00;  // coordinates of a copy are 32-bit, and a tile may reach past the end
+
+struct RowPlan {
+  int most, parts, part_k;  // tokens of a tile; parts of the summed dimension and their length
+  int64_t tiles;            // of tokens, at most
+};
 
 bool good_sizes(int64_t rows, int64_t k, int64_t m, int32_t groups) {
   return rows >= 0 && k >= 0 && m >= 0 && rows <= kMostRows && k <= kMostRows && m <= kMostRows && groups >= 1;
@@ -853,12 +925,34 @@ bool is_short(int32_t type) { return type == REGTOPK_TYPE_BF16 || type == REGTOP
 
 extern "C" {
 
+static RowPlan row_plan(int64_t rows, int32_t groups, int64_t k, int64_t m) {
+  // The widest tile of tokens: as wide as a group has rows on average (a narrower one reads the weights again for nothing, a
+  // wider one holds fewer stages); pairs of blocks where they have 256 features to share.
+  RowPlan p;
+  const int64_t average = rows / groups;
+  p.most = average > 64 ? (m > kLanes ? 256 : 128) : average > 32 ? 64 : 32;
+  const int ctas = p.most == 256 ? 2 : 1;
+  p.tiles = rows / p.most + groups;
+  const int64_t all = p.tiles * ((m + ctas * kLanes - 1) / (ctas * kLanes));
+  p.parts = k >= 2048 ? parts_of(all, kPlaces / ctas, k) : 1;
+  p.part_k = p.parts > 1 ? (int)((k + p.parts - 1) / p.parts + kDepth - 1) / kDepth * kDepth : (int)k;
+  if (p.parts > 1) p.parts = (int)((k + p.part_k - 1) / p.part_k);
+  return p;
+}
+static size_t partial_bytes(int parts, int64_t elements) { return parts > 1 ? ((size_t)parts * elements * 4 + 255) / 256 * 256 : 0; }
+static int weight_parts(int64_t rows, int32_t groups, int64_t k, int64_t m) {
+  const int ctas = k > kLanes ? 2 : 1;
+  return parts_of(groups * ((k + ctas * kLanes - 1) / (ctas * kLanes)) * ((m + kWeightsMost - 1) / kWeightsMost), kPlaces / ctas, rows / groups);
+}
+
 size_t regtopk_grouped_matmul_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride,
-                                              int32_t transposed, int32_t weights, int64_t rows, int64_t k, int64_t m) {
-  if (!good_sizes(rows, k, m, 1) || weights < 1) return 0;
+                                              int32_t transposed, int32_t weights, int32_t groups, int64_t rows, int64_t k,
+                                              int64_t m) {
+  if (!good_sizes(rows, k, m, groups) || weights < 1) return 0;
   const int64_t lines = transposed ? k : m, cols = transposed ? m : k;
   const int count = w_stride ? weights : 1;
-  return (direct(x, ldx, rows, 1, 0) ? 0 : copy_bytes(rows, k, 1)) + (direct(w, ldw, lines, count, w_stride) ? 0 : copy_bytes(lines, cols, count));
+  return (direct(x, ldx, rows, 1, 0) ? 0 : copy_bytes(rows, k, 1)) + (direct(w, ldw, lines, count, w_stride) ? 0 : copy_bytes(lines, cols, count)) +
+         partial_bytes(row_plan(rows, groups, k, m).parts, rows * m);
 }
 
 int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t w_stride, int32_t transposed,
@@ -875,7 +969,7 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (k == 0) return train_rc(cudaMemset2DAsync(y, (size_t)(rows > 1 ? ldy : m) * 2, 0, (size_t)m * 2, (size_t)rows, s));
-  const size_t need = regtopk_grouped_matmul_workspace_bytes(x, ldx, w, ldw, w_stride, transposed, weights, rows, k, m);
+  const size_t need = regtopk_grouped_matmul_workspace_bytes(x, ldx, w, ldw, w_stride, transposed, weights, groups, rows, k, m);
   if (need && (!workspace || (uintptr_t)workspace % 16)) return REGTOPK_ERR_INVALID_ARG;
   if (workspace_bytes < need) return REGTOPK_ERR_WORKSPACE_TOO_SMALL;
   const int count = w_stride ? weights : 1;
@@ -888,10 +982,8 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   const int rc = copies.run(offsets, groups, copies_w ? count : 1, sms, s);
   if (rc != REGTOPK_OK) return rc;
 
-  // The widest tile of tokens: as wide as a group has rows on average (a narrower one reads the weights again for
-  // nothing, a wider one holds fewer stages), but narrow enough that every SM has a tile.
-  const int64_t average = rows / groups;
-  const int most = average > 64 ? (m > kLanes ? 256 : 128) : average > 32 ? 64 : 32;
+  const RowPlan plan = row_plan(rows, groups, k, m);
+  const int most = plan.most;
   CUtensorMap wm, xm;
   if (!make_map(&wm, w, type, cols, lines, ldw, count, w_stride, transposed ? kDepth : kLanes) ||
       !make_map(&xm, x, type, k, rows, ldx, 0, 0, most < 64 ? most : 64)) return REGTOPK_ERR_CUDA;
@@ -899,8 +991,10 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   a.offsets = offsets; a.y = y; a.ldy = ldy; a.groups = groups; a.weights = weights; a.rows = (int)rows; a.k = (int)k; a.m = (int)m;
   a.shared_weights = count == 1;
   a.pairs = m % 2 == 0 && (rows == 1 || ldy % 2 == 0) && (uintptr_t)y % 4 == 0;
-  const int64_t tiles = rows / most + groups;  // of tokens, at most
+  a.parts = plan.parts; a.part_k = plan.part_k; a.partial = reinterpret_cast<float*>(copies.ws);
+  const int64_t tiles = plan.tiles;
   if (tiles * ((m + kLanes - 1) / kLanes) > INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
+  auto launch_product = [&]() -> int {
 #define REGTOPK_ROWS(N, C)                                                                                 \
   case N:                                                                                                  \
     if (type == REGTOPK_TYPE_BF16)                                                                         \
@@ -916,12 +1010,20 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
     REGTOPK_ROWS(256, 2);
   }
 #undef REGTOPK_ROWS
+  };
+  const int done = launch_product();
+  if (done != REGTOPK_OK || a.parts == 1) return done;
+  const int64_t blocks = (rows * m + kJoinThreads - 1) / kJoinThreads, most_blocks = (int64_t)sms * 8;
+  const dim3 grid((unsigned)(blocks < most_blocks ? blocks : most_blocks));
+  return type == REGTOPK_TYPE_BF16 ? start(k_join_rows<__nv_bfloat16>, grid, kJoinThreads, 0, s, a)
+                                   : start(k_join_rows<__half>, grid, kJoinThreads, 0, s, a);
 }
 
 size_t regtopk_grouped_matmul_dw_workspace_bytes(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t groups,
                                                  int64_t rows, int64_t k, int64_t m) {
   if (!good_sizes(rows, k, m, groups)) return 0;
-  return (direct(dy, ld_dy, rows, 1, 0) ? 0 : copy_bytes(rows, m, 1)) + (direct(x, ldx, rows, 1, 0) ? 0 : copy_bytes(rows, k, 1));
+  return (direct(dy, ld_dy, rows, 1, 0) ? 0 : copy_bytes(rows, m, 1)) + (direct(x, ldx, rows, 1, 0) ? 0 : copy_bytes(rows, k, 1)) +
+         partial_bytes(weight_parts(rows, groups, k, m), groups * m * k);
 }
 
 int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, float* out, int64_t ld_out,
@@ -939,6 +1041,7 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
   if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   WeightsArgs a;
+  float* partial = nullptr;
   CUtensorMap xm, ym;
   if (rows > 0) {
     const size_t need = regtopk_grouped_matmul_dw_workspace_bytes(dy, ld_dy, x, ldx, groups, rows, k, m);
@@ -951,6 +1054,7 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
     if (!direct(x, ldx, rows, 1, 0)) copies.add(&x, &ldx, rows, k, 1, &none);
     const int rc = copies.run(offsets, groups, 1, sms, s);
     if (rc != REGTOPK_OK) return rc;
+    partial = reinterpret_cast<float*>(copies.ws);
     if (!make_map(&xm, x, type, k, rows, ldx, 0, 0, kDepth) || !make_map(&ym, dy, type, m, rows, ld_dy, 0, 0, kDepth)) return REGTOPK_ERR_CUDA;
   } else {
     memset(&xm, 0, sizeof xm);  // never used: no group has rows
@@ -959,10 +1063,21 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
   a.offsets = offsets; a.out = out; a.ld_out = ld_out; a.inner_stride = inner_stride; a.outer_stride = outer_stride;
   a.groups = groups; a.inner = inner; a.rows = (int)rows; a.k = (int)k; a.m = (int)m; a.accumulate = accumulate;
   if ((k + kLanes - 1) / kLanes * ((m + kWeightsMost - 1) / kWeightsMost) * groups > INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
+  a.parts = rows > 0 ? weight_parts(rows, groups, k, m) : 1;
+  a.part_stride = (int64_t)groups * m * k;
   const bool pairs = k > kLanes;
-  if (type == REGTOPK_TYPE_BF16)
-    return pairs ? launch_weights<__nv_bfloat16, 2>(xm, ym, a, dev, sms, s) : launch_weights<__nv_bfloat16, 1>(xm, ym, a, dev, sms, s);
-  return pairs ? launch_weights<__half, 2>(xm, ym, a, dev, sms, s) : launch_weights<__half, 1>(xm, ym, a, dev, sms, s);
+  const auto product = [&](const WeightsArgs& p) {
+    if (type == REGTOPK_TYPE_BF16)
+      return pairs ? launch_weights<__nv_bfloat16, 2>(xm, ym, p, dev, sms, s) : launch_weights<__nv_bfloat16, 1>(xm, ym, p, dev, sms, s);
+    return pairs ? launch_weights<__half, 2>(xm, ym, p, dev, sms, s) : launch_weights<__half, 1>(xm, ym, p, dev, sms, s);
+  };
+  if (a.parts == 1) return product(a);
+  WeightsArgs p = a;  // into the workspace
+  p.out = partial; p.ld_out = k; p.inner = groups; p.inner_stride = m * k; p.outer_stride = 0; p.accumulate = 0;
+  const int rc = product(p);
+  if (rc != REGTOPK_OK) return rc;
+  const int64_t blocks = (a.part_stride + kJoinThreads - 1) / kJoinThreads, most = (int64_t)sms * 8;
+  return start(k_join_weights, dim3((unsigned)(blocks < most ? blocks : most)), kJoinThreads, 0, s, a, partial);
 }
 
 int regtopk_train_status(void* cuda_stream) {

@@ -263,7 +263,7 @@ PyObject* grouped_matmul(PyObject* const* a) {  // x, w, offsets, out
   const int64_t ldy = given ? rows_of(y, "out").ld : m;
   const int32_t weights = static_cast<int32_t>(count);
   const int64_t stride = count > 1 ? w.stride(0) : ldw * (transposed ? k : m);
-  const size_t bytes = regtopk_grouped_matmul_workspace_bytes(x.data_ptr(), in.ld, w.data_ptr(), ldw, stride, transposed, weights, in.rows, k, m);
+  const size_t bytes = regtopk_grouped_matmul_workspace_bytes(x.data_ptr(), in.ld, w.data_ptr(), ldw, stride, transposed, weights, groups, in.rows, k, m);
   Tensor ws;
   if (bytes) ws = empty({static_cast<int64_t>(bytes)}, at::kByte, x);
   check(regtopk_grouped_matmul(x.data_ptr(), in.ld, w.data_ptr(), ldw, stride, transposed, weights, y.data_ptr(), ldy,

@@ -62,9 +62,9 @@ def test_c_entries_refuse():
     assert dw(out=p + 2) == -1 and dw(ldo=15) == -1 and dw(ld=15) == -1 and dw(dy=None) == -1 and dw(x=None) == -1
     assert dw(groups=4096) == -7 and dw(k=0) == 0 and dw(rows=0, acc=1) == 0
     size = lib.regtopk_grouped_matmul_workspace_bytes
-    assert size(p, 16, p, 16, 256, 0, 2, 8, 16, 16) == 0
-    assert size(p, 17, p, 16, 256, 0, 2, 8, 16, 16) >= 8 * 16 * 2 and size(p, 16, p, 17, 272, 0, 2, 8, 16, 16) >= 2 * 16 * 16 * 2
-    assert size(p, 16, p + 2, 16, 256, 0, 2, 8, 16, 16) > 0 and size(p, 16, p, 16, 260, 0, 2, 8, 16, 16) > 0
+    assert size(p, 16, p, 16, 256, 0, 2, 4, 8, 16, 16) == 0
+    assert size(p, 17, p, 16, 256, 0, 2, 4, 8, 16, 16) >= 8 * 16 * 2 and size(p, 16, p, 17, 272, 0, 2, 4, 8, 16, 16) >= 2 * 16 * 16 * 2
+    assert size(p, 16, p + 2, 16, 256, 0, 2, 4, 8, 16, 16) > 0 and size(p, 16, p, 16, 260, 0, 2, 4, 8, 16, 16) > 0
 
 
 # ---- on the GPU ----------------------------------------------------------------------------------------------------------
@@ -84,7 +84,8 @@ def cut(rows, groups, gen):
 SIZES = [  # rows, workers, experts, k, m
     (1, 1, 1, 1, 1), (5, 1, 2, 8, 8), (1, 1, 1, 64, 128), (33, 1, 3, 64, 128), (40, 2, 2, 72, 136), (100, 2, 4, 17, 130),
     (257, 1, 2, 128, 130), (300, 1, 5, 65, 257), (64, 4, 16, 40, 24), (1000, 1, 3, 200, 384), (513, 1, 1, 1000, 72),
-    (2000, 2, 2, 136, 264), (700, 1, 1, 31, 600), (4500, 1, 2, 264, 1100)]
+    (2000, 2, 2, 136, 264), (700, 1, 1, 31, 600), (4500, 1, 2, 264, 1100), (40, 1, 2, 2200, 130), (5, 2, 2, 4100, 60), (90, 1, 1, 2049, 300),
+    (3000, 1, 1, 72, 100)]
 
 
 @pytest.mark.gpu

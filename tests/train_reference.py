@@ -87,7 +87,7 @@ def c_library():
             ("regtopk_layer_norm_backward_workspace_bytes", [i64, i64, i32], size),
             ("regtopk_layer_norm_backward", [p, i64, p, i64, p, p, p, p, i64, p, i64, p, i64, p, i64, p, i64, p, i32, i32, i64, i64,
                                              i32, i32, drop, p, size, p], i32),
-            ("regtopk_grouped_matmul_workspace_bytes", [p, i64, p, i64, i64, i32, i32, i64, i64, i64], size),
+            ("regtopk_grouped_matmul_workspace_bytes", [p, i64, p, i64, i64, i32, i32, i32, i64, i64, i64], size),
             ("regtopk_grouped_matmul", [p, i64, p, i64, i64, i32, i32, p, i64, p, i32, i64, i64, i64, i32, p, size, p], i32),
             ("regtopk_grouped_matmul_dw_workspace_bytes", [p, i64, p, i64, i32, i64, i64, i64], size),
             ("regtopk_grouped_matmul_dw", [p, i64, p, i64, p, i64, i64, i64, i32, i32, p, i32, i64, i64, i64, i32, p, size, p], i32),
