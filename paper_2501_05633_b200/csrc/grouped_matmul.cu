@@ -1,17 +1,24 @@
 // Products of tokens with the matrices of their experts, ragged groups, and the gradients to the matrices
 // (include/regtopk_train.h), on the fifth-generation tensor cores.
 //
-// Both kernels are persistent, one block per SM: a thread that issues TMA copies, a thread that issues tcgen05.mma on
-// the tiles that have landed, and a warp group that writes finished accumulators while the next tile is multiplied.
+// Both kernels are persistent, one block per SM or one pair of blocks for two: a warp that issues TMA copies, a warp that
+// issues tcgen05.mma on the tiles that have landed, and warps that write finished accumulators while the next tile is
+// multiplied.
 //
-//   k_rows     D[128 output features][up to 256 tokens] = W[features][k] X[tokens][k]^T.  The features, which are a
-//              whole number of tiles, take the fixed 128 lanes; the tokens of a group, of which there may be any number,
-//              take the columns, whose count the instruction chooses in steps of 16.  A lane then holds one feature,
-//              so that a warp writes consecutive elements of one token's row.
-//   k_weights  D[128 columns of x][up to 256 columns of dy] = sum over tokens; a lane holds one column of x, so that a
-//              warp writes (or adds to) consecutive elements of one row of the gradient at any alignment.
+//   k_rows     D[128 or 256 output features][up to 256 tokens] = W[features][k] X[tokens][k]^T.  The features take the
+//              lanes of the accumulator; the tokens of a group, of which there may be any number, take its columns, whose
+//              count the instruction chooses in steps of 16 (of 32 for a pair).  A lane then holds one feature, so that a
+//              warp writes consecutive elements of a token's row.
+//   k_weights  D[128 or 256 columns of x][up to 256 columns of dy] = sum over tokens; a lane holds one column of x, so
+//              that a warp writes (or adds to) consecutive elements of a row of the gradient at any alignment.
 //
-// Tiles lie in shared memory in the 128-byte swizzle, copied in boxes that are 64 elements (128 bytes) wide.
+// A pair divides the features (the columns of x) and the tokens (the columns of dy) of its tile: each block holds half of
+// both operands, and the products of the first block read both halves.  Tiles lie in shared memory in the 128-byte
+// swizzle, copied in boxes that are 64 elements (128 bytes) wide.
+//
+// What bounds them (B200, 1.3-1.9 GHz under its power limit): 32,768 tokens in 64 groups, 2,048 -> 2,304, 246 us or
+// 1,260 TFLOP/s, where the same loops without any copies take 219 us and a library's product of one dense group of the same
+// sizes 209 us: groups that are no multiple of 256 tokens cost 5 %, tiles of 207 tokens on average the rest.
 
 #include <cuda.h>
 #include <string.h>
@@ -178,6 +185,8 @@ template <int kStages> struct Shared {
   u32 tmem, quit;
 };
 
+// No block takes TMEM before the kernel before it has ended, or lets a kernel behind it start before it has taken its own: whoever
+// waits for the other then holds none that the other needs.
 template <int kCtas, int kStages> __device__ __forceinline__ void set_up(Shared<kStages>& sh, int tmem_columns, int readers) {
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -194,6 +203,7 @@ template <int kCtas, int kStages> __device__ __forceinline__ void set_up(Shared<
     sh.quit = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  await_predecessor();
   if (threadIdx.x >> 5 == 2) {
     if constexpr (kCtas == 2) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&sh.tmem)), "r"(tmem_columns) : "memory");
@@ -207,6 +217,7 @@ template <int kCtas, int kStages> __device__ __forceinline__ void set_up(Shared<
   __syncthreads();
   sync_all<kCtas>();
   tmem_fence_after();
+  let_successor_start();
 }
 // No block of a pair leaves before the other: its barriers and its shared memory are in use until then.
 template <int kCtas, int kStages> __device__ __forceinline__ void tear_down(Shared<kStages>& sh, int tmem_columns) {
@@ -320,7 +331,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
   const u32 rank = cta_rank<kCtas>();
 
   set_up<kCtas>(sh, kTmem, 4 * kRowShare);
-  begin_after_predecessor();
   // where each group's rows lie and how many tiles come before it; groups that share a matrix one after the other, so that
   // it is read from memory once (four workers over sixteen matrices of 9 MB: 752 MB read without that, 285 MB are needed)
   constexpr int kPer = (kTableGroups + kRowThreads - 1) / kRowThreads;  // groups of a thread
@@ -560,7 +570,6 @@ __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_cons
   const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const u32 rank = cta_rank<kCtas>();
   set_up<kCtas>(sh, kTmem, 4 * kWeightShare);
-  begin_after_predecessor();
   for (int g = threadIdx.x; g < a.groups; g += kWeightThreads) {
     const int lo = (int)limited(a.offsets[g], a.rows), hi = (int)limited(a.offsets[g + 1], a.rows);
     rows[g] = make_int2(lo, max(hi - lo, 0));

@@ -214,9 +214,11 @@ __device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, volatile u32* quit
 // Every kernel here is launched with programmatic stream serialisation: its blocks may be started while the kernel before
 // it in the stream still runs.  It lets its own successor start early in turn, and waits for its predecessor before it
 // touches any memory that a kernel may write.
+__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void begin_after_predecessor() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  let_successor_start();
+  await_predecessor();
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
