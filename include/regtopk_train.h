@@ -118,9 +118,9 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
                               const int64_t* offsets, int32_t groups, int64_t rows, int64_t k, int64_t m, int32_t type,
                               void* workspace, size_t workspace_bytes, void* cuda_stream);
 
-/* Synchronises the stream.  REGTOPK_OK, REGTOPK_ERR_CUDA, or REGTOPK_ERR_INTERNAL if a product's kernel on the current
- * device ever gave up waiting for its own copies or tensor core work (every such wait ends after four billion cycles; the
- * outputs of that call are then incomplete).  The internal error stays set until the process ends. */
+/* Synchronises the stream.  REGTOPK_OK, REGTOPK_ERR_CUDA, or REGTOPK_ERR_INTERNAL if a kernel of the norms or the products on
+ * the current device ever gave up waiting for its own copies or tensor core work (every such wait ends after four billion
+ * cycles; the outputs of that call are then incomplete).  The internal error stays set until the process ends. */
 int regtopk_train_status(void* cuda_stream);
 
 #ifdef __cplusplus

@@ -89,6 +89,6 @@ def grouped_matmul_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, 
 
 
 def training_status(device=None):
-    """Synchronises the device's current stream; raises if a product's kernel there ever gave up waiting (a bug)."""
+    """Synchronises the device's current stream; raises if one of these kernels there ever gave up waiting (a bug)."""
     with torch.cuda.device(device):
         (_native or _load()).status(torch.cuda.current_stream().cuda_stream)
