@@ -1,9 +1,10 @@
 // Dropout and layer norm with their gradients (include/regtopk_train.h).
 //
-// All of them are bound by memory traffic: a few operations per element and one read and one write of each array.
+// All of them have memory traffic for their floor: a few operations per element and one read and one write of each array.
 // So each kernel reads every input once, keeps many copies under way, and draws the dropout mask again wherever it is
 // needed instead of storing it (one Philox call for eight columns costs less issue time than a byte of mask costs
-// bandwidth).
+// bandwidth).  Dropout reaches that floor; the norms spend 1.2 to 1.4 instructions of a lane on a value and are bound by
+// their issue.
 
 #include "train_common.cuh"
 
@@ -84,7 +85,8 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
   }
 }
 
-// Any other layout: a warp takes 256 columns of a row.
+// Any other layout: a warp takes 256 columns of a row, element by element (8,192 x 2,047 bfloat16: 25 us, where the layout
+// with 2,048 columns takes 13.6 us in the kernel above; aligned words shifted together took 42 us).
 template <typename T>
 __global__ void __launch_bounds__(kDropThreads) k_dropout_any(const DropoutArgs a) {
   const T* x = static_cast<const T*>(a.x);
@@ -333,6 +335,8 @@ struct NormArgs {
 // team by the rule for joining two samples (Chan, Golub, LeVeque 1979): nothing is lost when the mean is large beside the
 // deviation, and one exchange a row is enough.
 // RING false: every team has one row at most and reads it, and the vectors, where they are.
+// 32,768 rows of 1,024 bfloat16 columns with dropout beside a binary32 stream, 403 MB: 70 to 76 us, 5.3 to 5.8 TB/s, with 54 %
+// of the issue slots busy.
 template <typename T, typename S, bool VEC, int U, bool RING>
 __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ NormArgs a) {
   extern __shared__ __align__(16) char smem[];
@@ -459,6 +463,8 @@ __device__ __forceinline__ int group_of(const int64_t* offsets, int groups, int6
 // gradients in registers; where the range meets the end of a group the sums so far go to the slot (block + group) of
 // the partial sums.  With ascending groups no two blocks share a slot: a later block's groups are not lower, so
 // block + group only grows.
+// 32,768 rows of 1,024 bfloat16 columns with dropout, 336 MB: 83 us with the sum after it, 4.0 TB/s.  58 % of the issue slots
+// are busy with eight warps a block, whose 128 registers a thread leave no room for more of them.
 template <typename T, typename S, bool VEC, int U, bool RING>
 __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_constant__ NormBackArgs a) {
   extern __shared__ __align__(16) char smem[];
@@ -624,7 +630,9 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
   }
 }
 
-// The weight gradients: for each group the sum of its blocks' partial sums, kRuns runs of them side by side.
+// The weight gradients: for each group the sum of its blocks' partial sums, kRuns runs of them side by side.  Always the
+// same runs in the same order, so that the sums do not change from call to call.  Latency bounds it: 8 us for eight groups of
+// 1,024 columns and 293 blocks, 2.4 MB, from memory.
 struct NormSumArgs {
   const float* partial;
   float *dweight, *dbias;
