@@ -87,11 +87,13 @@ Rows rows_of(const Tensor& t, const char* name) {
   for (int64_t i = 0; i < n - 1; ++i) r.rows *= size[i];
   if (r.rows == 0 || r.cols == 0) return r;
   if (r.cols > 1 && stride[n - 1] != 1) value_error(std::string(name) + ": the elements of a row must be contiguous");
-  int64_t span = 0;  // what one step of the dimension to the left has to be; 0: no row distance known yet
+  int64_t span = 0;  // what one step of the dimension to the left has to be
+  bool known = false;  // whether a dimension has given the row distance (0 too: an expanded one repeats its rows, and is refused)
   for (int64_t i = n - 2; i >= 0; --i) {
     if (size[i] == 1) continue;
-    if (span == 0) r.ld = stride[i];
+    if (!known) r.ld = stride[i];
     else if (stride[i] != span) value_error(std::string(name) + ": no single distance leads from row to row (make it contiguous)");
+    known = true;
     span = stride[i] * size[i];
   }
   if (r.ld < r.cols) value_error(std::string(name) + ": rows overlap");
