@@ -109,7 +109,7 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
  *   out[g] (+)= sum over the rows t of group g of dy[t] x[t]^T, an [m][k] matrix; a group without rows gives zeros.
  * dy [rows][m] and x [rows][k] of `type` (BF16 or F16); out binary32, element (i, j) of group g = n * inner + e at
  * out[n * outer_stride + e * inner_stride + i * ld_out + j]: with inner experts and groups sorted by (worker, expert) this is
- * each worker's own row of a flat gradient.  accumulate != 0 adds to what out holds, one rounded addition per element.
+ * each worker's own row of a flat gradient.  No two rows of out may overlap (INVALID_ARG: blocks write them at once).  accumulate != 0 adds to what out holds, one rounded addition per element.
  * workspace as above, by regtopk_grouped_matmul_dw_workspace_bytes.  Errors as above. */
 size_t regtopk_grouped_matmul_dw_workspace_bytes(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t groups,
                                                  int64_t rows, int64_t k, int64_t m);

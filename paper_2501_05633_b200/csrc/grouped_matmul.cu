@@ -24,6 +24,7 @@
 #include <string.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "train_common.cuh"
 
@@ -933,6 +934,21 @@ struct RowPlan {
 bool good_sizes(int64_t rows, int64_t k, int64_t m, int32_t groups) {
   return rows >= 0 && k >= 0 && m >= 0 && rows <= kMostRows && k <= kMostRows && m <= kMostRows && groups >= 1;
 }
+// Whether no element of [outer][inner][m] rows of k elements lies in two of them: each distance passes what the smaller ones span.
+// Blocks write (and add to) rows on their own, so that rows that overlap would be a race.
+bool rows_apart(int64_t k, int64_t m, int64_t ld, int64_t inner, int64_t inner_stride, int64_t outer, int64_t outer_stride) {
+  struct { int64_t count, stride; } d[3] = {{m, ld}, {inner, inner_stride}, {outer, outer_stride}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (d[j].stride > d[j + 1].stride) std::swap(d[j], d[j + 1]);
+  __int128 span = k;
+  for (const auto& e : d) {
+    if (e.count <= 1) continue;
+    if (e.stride < span) return false;
+    span += (__int128)(e.count - 1) * e.stride;
+  }
+  return true;
+}
 bool is_short(int32_t type) { return type == REGTOPK_TYPE_BF16 || type == REGTOPK_TYPE_F16; }
 
 }  // namespace
@@ -1048,7 +1064,7 @@ int regtopk_grouped_matmul_dw(const void* dy, int64_t ld_dy, const void* x, int6
       inner_stride < 0 || outer_stride < 0) return REGTOPK_ERR_INVALID_ARG;
   if (groups > REGTOPK_MATMUL_MAX_GROUPS) return REGTOPK_ERR_TOO_LARGE;
   if (k == 0 || m == 0) return REGTOPK_OK;
-  if (!good_matrix(out, ld_out, m, k, 4)) return REGTOPK_ERR_INVALID_ARG;
+  if (!good_matrix(out, ld_out, m, k, 4) || !rows_apart(k, m, ld_out, inner, inner_stride, groups / inner, outer_stride)) return REGTOPK_ERR_INVALID_ARG;
   if (rows > 0 && (!good_matrix(dy, ld_dy, rows, m, 2) || !good_matrix(x, ldx, rows, k, 2))) return REGTOPK_ERR_INVALID_ARG;
   if (rows == 0 && accumulate) return REGTOPK_OK;
   int dev, sms;

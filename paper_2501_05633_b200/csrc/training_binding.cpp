@@ -15,6 +15,11 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <string>
+#include <utility>
+#include <vector>
+
 #include "regtopk_train.h"
 
 namespace {
@@ -98,6 +103,20 @@ Rows rows_of(const Tensor& t, const char* name) {
   }
   if (r.ld < r.cols) value_error(std::string(name) + ": rows overlap");
   return r;
+}
+
+// Whether no two elements of a tensor lie in one place, for certain: sorted, each distance passes what the smaller ones span.
+bool elements_apart(const Tensor& t) {
+  std::vector<std::pair<int64_t, int64_t>> d;  // distance, count
+  for (int64_t i = 0; i < t.dim(); ++i)
+    if (t.size(i) > 1) d.emplace_back(t.stride(i), t.size(i));
+  std::sort(d.begin(), d.end());
+  int64_t span = 1;
+  for (const auto& [stride, count] : d) {
+    if (stride < span) return false;
+    span += stride * (count - 1);
+  }
+  return true;
 }
 
 void same_shape(const Tensor& t, const Tensor& x, const char* name, bool or_float = false) {
@@ -295,6 +314,7 @@ PyObject* grouped_matmul_dw(PyObject* const* a) {  // dy, x, offsets, out, accum
                "], or with the groups split into [workers, experts], on dy's device");
   const int64_t ld = m > 1 ? out.stride(n - 2) : k;
   if ((k > 1 && out.stride(n - 1) != 1) || ld < k) value_error("out: the elements of a row must be contiguous and rows must not overlap");
+  if (out.numel() && !elements_apart(out)) value_error("out: matrices overlap");
   const int32_t inner = n == 3 ? groups : static_cast<int32_t>(out.size(1));
   const int64_t inner_stride = out.stride(n - 3), outer_stride = n == 3 ? 0 : out.stride(0);
   const size_t bytes = regtopk_grouped_matmul_dw_workspace_bytes(dy.data_ptr(), up.ld, x.data_ptr(), in.ld, groups, up.rows, k, m);

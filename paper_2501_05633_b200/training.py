@@ -83,8 +83,8 @@ def grouped_matmul_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, 
     """The gradient of grouped_matmul to the matrices, for every group on its own: out[g] = sum of dy[t] x[t]^T over
     the rows t of group g, float32 [groups, m, k].
 
-    out may be given, as [groups, m, k] or [workers, experts, m, k] with any strides but contiguous rows (a view of an
-    accumulator's columns, say), and is added to if `accumulate`."""
+    out may be given, as [groups, m, k] or [workers, experts, m, k] with contiguous rows of which no two
+    overlap (a view of an accumulator's columns, say), and is added to if `accumulate`."""
     return (_native or _load()).grouped_matmul_dw(dy, x, offsets, out, accumulate)
 
 

@@ -29,3 +29,35 @@ def test_rows_that_repeat_are_refused():
     one = x[:1].as_strided((1, 5, 16), (0, 16, 1))
     assert torch.equal(rt.layer_norm(one, w)[0], y[:1])
     assert torch.equal(rt.layer_norm(x[:, :1].as_strided((4, 1, 16), (80, 0, 1)), w)[0], y[:, :1])
+
+
+def test_c_matrices_that_overlap():
+    """Before anything is launched (the pointer is never followed): distances that let two rows of the gradient meet."""
+    lib = ref.c_library()
+
+    def dw(ld=16, inner=2, inner_stride=384, outer_stride=768, groups=4, m=24):
+        p = 4096
+        return lib.regtopk_grouped_matmul_dw(p, 24, p, 16, p, ld, inner_stride, outer_stride, inner, 0, p, groups, 0, 16, m, 1, None, 0, None)
+    assert dw(inner_stride=0) == -1 and dw(inner_stride=383) == -1 and dw(outer_stride=0) == -1 and dw(outer_stride=767) == -1
+    assert dw(ld=17) == -1 and dw(inner=4, inner_stride=383) == -1 and dw(ld=32, inner_stride=15, outer_stride=768) == -1
+    assert dw(inner_stride=2**62, outer_stride=2**62) == -1
+
+
+@pytest.mark.gpu
+def test_matrices_that_overlap_are_refused():
+    gen = torch.Generator().manual_seed(3)
+    dy, x = torch.randn(40, 24, generator=gen).to(BF).cuda(), torch.randn(40, 16, generator=gen).to(BF).cuda()
+    off = torch.tensor([0, 3, 8, 30, 40], device="cuda")
+    flat = torch.zeros(4 * 24 * 16, device="cuda")
+    for out in (flat[:384].view(1, 24, 16).expand(4, 24, 16), flat[:768].view(2, 1, 24, 16).expand(2, 2, 24, 16),
+                flat[:768].view(1, 2, 24, 16).expand(2, 2, 24, 16), flat.as_strided((4, 24, 16), (383, 16, 1)),
+                flat.as_strided((4, 24, 16), (15, 64, 1)), flat.as_strided((2, 2, 24, 16), (384, 384, 16, 1))):
+        for accumulate in (False, True):
+            with pytest.raises(ValueError):
+                rt.grouped_matmul_dw(dy, x, off, out=out, accumulate=accumulate)
+    assert not flat.any()
+    want = rt.grouped_matmul_dw(dy, x, off)
+    for out in (torch.zeros(24, 4, 16, device="cuda").transpose(0, 1), torch.zeros(24, 2, 2, 16, device="cuda").permute(2, 1, 0, 3),
+                torch.zeros(4, 24, 21, device="cuda")[:, :, :16]):
+        rt.grouped_matmul_dw(dy, x, off, out=out, accumulate=True)
+        assert torch.equal(out.reshape(4, 24, 16), want), "rows that lie between one another do not overlap"
