@@ -56,7 +56,8 @@ constexpr int kDropStep = 2;  // loads under way per thread
 
 // Aligned rows of a multiple of eight columns, fewer than 2^31 groups of eight: a thread takes kDropStep groups at a
 // time.  The row of a group is found by a multiplication (Granlund and Montgomery 1994): with 2^(s-1) < d <= 2^s and
-// magic = floor(2^(31+s) / d) + 1, floor(n / d) = floor(n magic / 2^(31+s)) for every n < 2^31.
+// magic = floor(2^(31+s) / d) + 1, floor(n / d) = floor(n magic / 2^(31+s)) for every n < 2^31.  For d = 1 there is no such
+// number of 32 bits.
 template <typename T>
 __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs a) {
   const T* x = static_cast<const T*>(a.x);
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
 #pragma unroll
   for (int i = 0; i < kDropStep; ++i) {
     const u32 at = first + i * kDropThreads + threadIdx.x;
-    row[i] = __umulhi(at, a.magic) >> a.shift;
+    row[i] = a.groups == 1 ? at : __umulhi(at, a.magic) >> a.shift;
     group[i] = at - row[i] * a.groups;
     if (at < a.total) v[i].fetch(x + row[i] * a.ldx + group[i] * 8);
   }

@@ -10,6 +10,33 @@ from tests import train_reference as ref
 BF, HF, F = torch.bfloat16, torch.float16, torch.float32
 
 
+def padded(rows, cols, dtype, gen, pad, shift=0, fill=0.0):
+    """(a [rows, cols] tensor with `pad` more columns behind each row, beginning `shift` elements into its storage, which is `fill`
+    otherwise; the storage's whole rows)."""
+    flat = torch.full((rows * (cols + pad) + shift,), fill, dtype=dtype, device="cuda")
+    whole = flat[shift:].view(rows, cols + pad)
+    whole[:, :cols] = torch.randn(rows, cols, generator=gen).to(dtype)
+    return whole[:, :cols], whole
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("rows,cols", [(2, 8), (300, 8), (4099, 8), (300, 16), (129, 24), (65, 520)])
+def test_dropout_of_short_rows(rows, cols, dtype):
+    """Rows of one group of eight columns and of a few: each row has its own mask and stays in its place, contiguous or a view of
+    wider rows, aligned or not, and the columns behind it keep what they hold."""
+    gen = torch.Generator().manual_seed(rows + cols)
+    keep, factor = ref.keep_mask(rows, cols, 0.4, 2**63 + 5, 31)
+    for pad, out_pad, shift in ((0, 0, 0), (16, 0, 0), (0, 8, 0), (8, 24, 0), (8, 8, 1), (0, 0, 3)):
+        x, _ = padded(rows, cols, dtype, gen, pad, shift)
+        out, whole = padded(rows, cols, dtype, gen, out_pad, shift, fill=3.0)
+        want = torch.where(torch.from_numpy(keep), x.cpu().float() * torch.tensor(factor, dtype=F), 0.0).to(dtype)
+        assert torch.equal(rt.dropout(x, 0.4, 2**63 + 5, 31).cpu(), want), (pad, shift)
+        rt.dropout(x, 0.4, 2**63 + 5, 31, out=out)
+        assert torch.equal(out.cpu(), want), (pad, out_pad, shift)
+        assert (whole[:, cols:] == 3).all()
+
+
 @pytest.mark.gpu
 def test_rows_that_repeat_are_refused():
     """An expanded dimension between others has distance 0, which is no distance from row to row: such a tensor (the gradient of
