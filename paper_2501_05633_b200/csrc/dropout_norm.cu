@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
     const u32 at = first + i * kDropThreads + threadIdx.x;
     row[i] = a.groups == 1 ? at : __umulhi(at, a.magic) >> a.shift;
     group[i] = at - row[i] * a.groups;
-    if (at < a.total) v[i].fetch(x + row[i] * a.ldx + group[i] * 8);
+    if (at < a.total) v[i].fetch(x + row[i] * a.ldx + (int64_t)group[i] * 8);
   }
 #pragma unroll
   for (int i = 0; i < kDropStep; ++i) {
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
       Numbers(a.drop, row[i], group[i]).drop(f, a.drop);
       v[i].put(f);
     }
-    if (at < a.total) v[i].store(y + row[i] * a.ldy + group[i] * 8);
+    if (at < a.total) v[i].store(y + row[i] * a.ldy + (int64_t)group[i] * 8);
   }
 }
 

@@ -1,6 +1,7 @@
 """The training operators at the edges of what they take: layouts, lengths and values at which the arithmetic of addresses,
 counters and sums could go wrong, against the definitions in 64 bits where there is a result."""
 import numpy as np
+import numpy as np
 import pytest
 import torch
 
@@ -35,6 +36,31 @@ def test_dropout_of_short_rows(rows, cols, dtype):
         rt.dropout(x, 0.4, 2**63 + 5, 31, out=out)
         assert torch.equal(out.cpu(), want), (pad, out_pad, shift)
         assert (whole[:, cols:] == 3).all()
+
+
+def keep_of_groups(groups, p, seed, subsequence):
+    """The mask of row 0 in the groups of eight columns that are numbered here."""
+    words = ref.philox([np.asarray(groups, np.uint64), 0, 0, subsequence], (seed & 0xFFFFFFFF, seed >> 32))
+    numbers = np.stack([(w >> np.uint64(s)) & np.uint64(0xFFFF) for w in words for s in (0, 16)], -1)
+    return (numbers >= int(round(65536 * p))).reshape(-1)
+
+
+def test_mask_of_groups():
+    assert np.array_equal(keep_of_groups(range(40), 0.3, 12345678901, 8), ref.keep_mask(1, 320, 0.3, 12345678901, 8)[0][0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("extra", [4104, 4103])
+def test_dropout_of_a_row_past_32_bits(extra):
+    """One row of more than 2^32 columns, in place, a multiple of eight columns and not: the start, what lies on both sides of
+    column 2^32 and the end."""
+    cols = 2**32 + extra
+    x = torch.ones(cols, dtype=BF, device="cuda")
+    rt.dropout(x, 0.25, 5, 6, out=x)
+    for first in (0, 2**31 - 4096, 2**32 - 4096, 2**32):
+        here = x[first: first + 8192]
+        want = keep_of_groups(range(first // 8, first // 8 + 1024), 0.25, 5, 6)[: here.numel()]
+        assert np.array_equal(here.float().cpu().numpy() != 0, want), first
 
 
 @pytest.mark.gpu
