@@ -1,7 +1,6 @@
 """The training operators at the edges of what they take: layouts, lengths and values at which the arithmetic of addresses,
 counters and sums could go wrong, against the definitions in 64 bits where there is a result."""
 import numpy as np
-import numpy as np
 import pytest
 import torch
 
@@ -114,3 +113,40 @@ def test_matrices_that_overlap_are_refused():
                 torch.zeros(4, 24, 21, device="cuda")[:, :, :16]):
         rt.grouped_matmul_dw(dy, x, off, out=out, accumulate=True)
         assert torch.equal(out.reshape(4, 24, 16), want), "rows that lie between one another do not overlap"
+
+
+def check_back(dy, h, mean, rstd, weight, dh=None, offsets=None, p=0.0):
+    """layer_norm_backward against the formula in 64 bits for the mean and rstd given.
+
+    Tolerance: h - mean is rounded once, and exact where the two are within a factor of two; with the product by rstd the
+    normalised value u is off by 2 * 2^-24 of itself, however large the mean.  A sum over a row in a tree of at most 8*4 + 5 + 16
+    steps adds 53 * 2^-24 of the sum of magnitudes, and each further step 2^-24 of what it handles: 2^-17 covers the chain, applied
+    to the terms rstd |g|, rstd mean|g| and rstd |u| mean|g u|.  The sums over rows take at most 256 steps in a row here: 2^-16."""
+    at = [0, len(dy)] if offsets is None else offsets
+    dev = None if offsets is None else torch.tensor(offsets, device="cuda")
+    dx, dres, dw, db = rt.layer_norm_backward(dy, h, mean, rstd, weight, dh=dh, p=p, seed=4, subsequence=9, offsets=dev)
+    d = [ref.host(t) for t in (dy, h, mean, rstd, weight)]
+    wx, wr, ww, wb = ref.layer_norm_backward(*d, None if dh is None else ref.host(dh), p, 4, 9, at)
+    unit, g = np.abs(d[1] - d[2][:, None]) * d[3][:, None], np.abs(d[0] * d[4])
+    slack = 2.0 ** -17 * (d[3][:, None] * (g + g.mean(1)[:, None] + unit * (g * unit).mean(1)[:, None])
+                          + (0 if dh is None else np.abs(ref.host(dh))))
+    ref.assert_close(dx, wx, slack * 65536 / (65536 - round(65536 * p)), dy.dtype, "dx")
+    ref.assert_close(dres, wr, slack, h.dtype, "dresidual")
+    for got, want, size, name in ((dw, ww, np.abs(d[0]) * unit, "dweight"), (db, wb, np.abs(d[0]), "dbias")):
+        ref.assert_close(got, want, 2.0 ** -16 * np.stack([size[a:b].sum(0) for a, b in zip(at, at[1:])]), F, name)
+    return dx, dres, dw, db
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,stream", [(F, F), (BF, F), (BF, BF), (HF, HF)])
+@pytest.mark.parametrize("rows,cols", [(60, 1024), (9, 1001), (2500, 768), (2500, 333), (200, 8192)])
+def test_norm_gradient_with_a_large_mean(rows, cols, dtype, stream):
+    """Rows whose mean is 0 to 10,000 times their deviation, and constant rows, whose normalised values are zeros."""
+    gen = torch.Generator().manual_seed(rows + cols)
+    means = 10.0 ** torch.randint(-1, 5, (rows, 1), generator=gen).float()
+    h = (torch.randn(rows, cols, generator=gen) + means).to(stream).cuda()
+    dy, weight = torch.randn(rows, cols, generator=gen).to(dtype).cuda(), torch.randn(cols, generator=gen).cuda()
+    _, _, mean, rstd = rt.layer_norm(h, weight)
+    check_back(dy, h, mean, rstd, weight, offsets=[0, rows // 3, rows])
+    _, _, dw, _ = rt.layer_norm_backward(dy, torch.full_like(h, 100.0), torch.full_like(mean, 100.0), torch.full_like(rstd, 316.0), weight)
+    assert not dw.any()
