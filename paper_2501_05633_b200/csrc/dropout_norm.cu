@@ -56,8 +56,7 @@ constexpr int kDropStep = 2;  // loads under way per thread
 
 // Aligned rows of a multiple of eight columns, fewer than 2^31 groups of eight: a thread takes kDropStep groups at a
 // time.  The row of a group is found by a multiplication (Granlund and Montgomery 1994): with 2^(s-1) < d <= 2^s and
-// magic = floor(2^(31+s) / d) + 1, floor(n / d) = floor(n magic / 2^(31+s)) for every n < 2^31.  For d = 1 there is no such
-// number of 32 bits.
+// magic = floor(2^(31+s) / d) + 1, which has 32 bits, floor(n / d) = floor(2n magic / 2^(32+s)) for every n < 2^31.
 template <typename T>
 __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs a) {
   const T* x = static_cast<const T*>(a.x);
@@ -69,9 +68,9 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
 #pragma unroll
   for (int i = 0; i < kDropStep; ++i) {
     const u32 at = first + i * kDropThreads + threadIdx.x;
-    row[i] = a.groups == 1 ? at : __umulhi(at, a.magic) >> a.shift;
+    row[i] = __umulhi(2 * at, a.magic) >> a.shift;
     group[i] = at - row[i] * a.groups;
-    if (at < a.total) v[i].fetch(x + row[i] * a.ldx + (int64_t)group[i] * 8);
+    if (at < a.total) v[i].fetch(x + (row[i] * a.ldx + (uint64_t)group[i] * 8));
   }
 #pragma unroll
   for (int i = 0; i < kDropStep; ++i) {
@@ -82,7 +81,7 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_vec(const DropoutArgs 
       Numbers(a.drop, row[i], group[i]).drop(f, a.drop);
       v[i].put(f);
     }
-    if (at < a.total) v[i].store(y + row[i] * a.ldy + (int64_t)group[i] * 8);
+    if (at < a.total) v[i].store(y + (row[i] * a.ldy + (uint64_t)group[i] * 8));
   }
 }
 
@@ -113,8 +112,8 @@ int launch_dropout(DropoutArgs& a, bool vec, int sms, cudaStream_t s) {
     while (((int64_t)1 << s31) < groups) ++s31;
     a.groups = (u32)groups;
     a.total = (u32)(a.rows * groups);
-    a.magic = groups == 1 ? 0u : (u32)(((uint64_t)1 << (31 + s31)) / (uint64_t)groups + 1);
-    a.shift = groups == 1 ? 0u : (u32)(s31 - 1);
+    a.magic = (u32)(((uint64_t)1 << (31 + s31)) / (uint64_t)groups + 1);
+    a.shift = (u32)s31;
     return start(k_dropout_vec<T>, (a.total + kDropThreads * kDropStep - 1) / (kDropThreads * kDropStep), kDropThreads, 0, s, a);
   } else {
     const int64_t tasks = (a.rows * ((a.cols + 255) >> 8) + kDropThreads / 32 - 1) / (kDropThreads / 32), most = (int64_t)sms * 8;
