@@ -313,8 +313,9 @@ __device__ __forceinline__ float quotient(float a, float b, float reciprocal) {
   return better == better ? better : q;  // infinity
 }
 // 1 / sqrt(x) by the approximation and one step of Newton's method; where that has no value (0, infinity), the approximation.
+// x is not halved: half of the smallest number is 0.
 __device__ __forceinline__ float inverse_root(float x) {
-  const float y = rsqrtf(x), better = y * fmaf(-0.5f * x * y, y, 1.5f);
+  const float y = rsqrtf(x), better = fmaf(0.5f * y, fmaf(-x * y, y, 1.0f), y);
   return better == better ? better : y;
 }
 

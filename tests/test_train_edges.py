@@ -150,3 +150,32 @@ def test_norm_gradient_with_a_large_mean(rows, cols, dtype, stream):
     check_back(dy, h, mean, rstd, weight, offsets=[0, rows // 3, rows])
     _, _, dw, _ = rt.layer_norm_backward(dy, torch.full_like(h, 100.0), torch.full_like(mean, 100.0), torch.full_like(rstd, 316.0), weight)
     assert not dw.any()
+
+
+@pytest.mark.gpu
+def test_norm_statistics_over_the_range():
+    """The division behind the mean and the reciprocal root behind rstd, from the smallest values to the largest.
+
+    Rows [a, -a, 0, 0] with a a power of two have mean 0 and the variance a^2 / 2 without a rounding, down to the smallest
+    number that binary32 has (a = 2^-74); the root of Newton's step is within 2^-22.  Rows with a single value v have the sum v
+    without a rounding: the mean is off by three roundings at most, each 2^-24 of it or half the smallest number."""
+    power = torch.arange(-74, 63)
+    a = torch.ldexp(torch.ones(len(power)), power)
+    x = torch.stack([a, -a, 0 * a, 0 * a], 1).cuda()
+    _, _, mean, rstd = rt.layer_norm(x, torch.ones(4, device="cuda"), eps=0.0)
+    want = 2.0 ** (0.5 - power.double().numpy())
+    assert not mean.any()
+    off = np.abs(ref.host(rstd) / want - 1)
+    assert (off < 2.0 ** -22).all(), (power[int(off.argmax())], off.max())
+    assert torch.isinf(rt.layer_norm(torch.zeros(2, 4, device="cuda"), torch.ones(4, device="cuda"), eps=0.0)[3]).all()
+    v = torch.ldexp(1 + torch.rand(3000, generator=torch.Generator().manual_seed(1)), torch.randint(-149, 128, (3000,), generator=torch.Generator().manual_seed(2)))
+    v[:4] = torch.tensor([2.0**-149, 3 * 2.0**-149, 2.0**-126, torch.finfo(F).max])
+    for cols in (1, 3, 7, 96, 511, 1000, 3001):
+        x = torch.zeros(3000, cols)
+        x[torch.arange(3000), torch.arange(3000) % cols] = v
+        mean = ref.host(rt.layer_norm(x.cuda(), torch.ones(cols, device="cuda"))[2])
+        want = v.double().numpy() / cols
+        assert (np.abs(mean - want) <= 3 * (2.0 ** -24 * want + 2.0 ** -150)).all(), cols
+    whole = torch.randint(-1000, 1001, (500, 37), generator=torch.Generator().manual_seed(3)).float()
+    whole[:, 0] -= whole.sum(1) % 37
+    assert torch.equal(rt.layer_norm(whole.cuda(), torch.ones(37, device="cuda"))[2].cpu(), whole.sum(1) / 37), "whole means are exact"
