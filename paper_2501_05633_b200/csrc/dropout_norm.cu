@@ -11,10 +11,10 @@
 namespace {
 
 // ---- eight columns of a row ------------------------------------------------------------------------------------------
-// This lane's columns of the unit that begins at column c0; zeros past the end of the row.  SHARED: the row is in shared
-// memory, otherwise in global.
+// This lane's columns of the unit that begins at column c0; past the end of the row zeros if VEC, `past` if not.  SHARED: the row is
+// in shared memory, otherwise in global.
 template <typename T, bool VEC, bool SHARED, typename Column>
-__device__ __forceinline__ void read_eight(Octet& f, const T* row, Column c0, int lane, Column cols) {
+__device__ __forceinline__ void read_eight(Octet& f, const T* row, Column c0, int lane, Column cols, float past = 0.0f) {
   if (VEC) {
     Eight<T> v;
     if (c0 + lane * 8 >= cols) v.clear();
@@ -24,7 +24,7 @@ __device__ __forceinline__ void read_eight(Octet& f, const T* row, Column c0, in
   } else {
     float e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = c0 + lane_col<false>(lane, j) < cols ? to_float(row[c0 + lane_col<false>(lane, j)]) : 0.0f;
+    for (int j = 0; j < 8; ++j) e[j] = c0 + lane_col<false>(lane, j) < cols ? to_float(row[c0 + lane_col<false>(lane, j)]) : past;
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = make_float2(e[2 * i], e[2 * i + 1]);
   }
@@ -527,16 +527,18 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
         const int c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
         Octet &d = kept_d[u % kKept], &v = kept_v[u % kKept], &w = kept_w[u % kKept];
-        read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);  // zeros past the end, so nothing is added there
-        read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
+        read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);  // zeros past the end, so finite values add nothing there
+        read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols, mean);
         if (RING) read_vector<VEC>(w, weight, c0, t.lane);
         else load_vector<VEC>(w, a.weight, a.wide, c0, t.lane, a.cols);
+        // The difference first, which takes an instruction more than h rstd + (-mean rstd), 1 to 3 % of the time, but is exact
+        // where the two are close: with a mean a thousand times the deviation dweight was off by 2e-5 of its largest value, now
+        // as without a mean by 1e-7.  Past the end it is made 0: -mean there, times rstd, may be an infinity.
+        const float centre = VEC && c0 + t.lane * 8 >= a.cols ? 0.0f : mean;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = add2(v[i], both(-centre));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // The difference first, which takes an instruction more than h rstd + (-mean rstd), 1 to 3 % of the time, but is exact
-          // where the two are close: with a mean a thousand times the deviation dweight was off by 2e-5 of its largest value, now
-          // as without a mean by 1e-7.
-          v[i] = add2(v[i], both(-mean));
           const float2 unit = mul2(v[i], both(rstd)), p = mul2(d[i], w[i]);
           s1 = add2(s1, p);
           s2 = fma2(p, unit, s2);

@@ -179,3 +179,16 @@ def test_norm_statistics_over_the_range():
     whole = torch.randint(-1000, 1001, (500, 37), generator=torch.Generator().manual_seed(3)).float()
     whole[:, 0] -= whole.sum(1) % 37
     assert torch.equal(rt.layer_norm(whole.cuda(), torch.ones(37, device="cuda"))[2].cpu(), whole.sum(1) / 37), "whole means are exact"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [8, 20, 300, 520, 1000, 1023])
+@pytest.mark.parametrize("rows", [7, 3000])
+def test_norm_gradient_of_huge_rows(rows, cols):
+    """A mean whose product with rstd passes binary32's range: what lies past the end of a row, where nothing is, must not
+    reach the sums over the row.  The rows here are constant, so that dx = rstd (g - mean(g)), and dweight is 0."""
+    gen = torch.Generator().manual_seed(cols)
+    dy, weight = torch.randn(rows, cols, generator=gen).cuda(), torch.randn(cols, generator=gen).cuda()
+    h, mean, rstd = (torch.full(s, v, device="cuda") for s, v in (((rows, cols), 3e37), ((rows,), 3e37), ((rows,), 316.0)))
+    _, _, dw, _ = check_back(dy, h, mean, rstd, weight)
+    assert not dw.any()
