@@ -15,7 +15,7 @@
  *   - Calls enqueue work on cuda_stream (a cudaStream_t of the current device, NULL = default stream) and return
  *     without synchronising.  Return value: REGTOPK_OK or a negative REGTOPK_ERR_* code of regtopk.h.  Nothing aborts,
  *     throws or traps.
- *   - Statistics, sums and weight gradients are binary32, and each output is rounded once.  Results do not depend on
+ *   - Statistics, sums and weight gradients are binary32 (the products' say how), and each output is rounded once.  Results do not depend on
  *     the order in which blocks run: equal calls give equal bits.
  *   - offsets arrays are int64 on the device, `groups` + 1 ascending values: group g is the rows
  *     [offsets[g], offsets[g+1]), which may be none.  The values are the caller's data and not trusted: they are
@@ -94,7 +94,9 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
  * w[e * w_stride + i * ldw + j].  transposed == 0: matrices [m][k], as a linear layer keeps them.  transposed != 0:
  * matrices [k][m], used as y[t] = x[t] w: with dy for x and the layer's own [m][k] matrices this is the gradient to the
  * tokens.  groups is a multiple of weights: groups sorted by (worker, expert) share the experts' matrices.
- * Products and sums are binary32 on the tensor cores; y is rounded once.  rows < 2^31; k, m < 2^31; k == 0 gives zeros.
+ * Products are exact and sums binary32 on the tensor cores, which cut the running sum off where an addition would round: sums of up to
+ * 4,096 terms are some 3e-5 of the sum of magnitudes too small at most, and longer ones are joined from such by rounded additions.  y is
+ * rounded once.  rows < 2^31; k, m < 2^31; k == 0 gives zeros.
  * workspace: 16-byte aligned, at least regtopk_grouped_matmul_workspace_bytes(...) bytes, which hold a copy of
  * x or w where it has no 16-byte aligned rows (base and leading dimension; for w the stride between matrices too), and partial
  * sums where k is long and there are few rows; often 0.  Errors: INVALID_ARG, TOO_LARGE (groups), WORKSPACE_TOO_SMALL, NO_DEVICE, CUDA. */
@@ -109,7 +111,9 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
  *   out[g] (+)= sum over the rows t of group g of dy[t] x[t]^T, an [m][k] matrix; a group without rows gives zeros.
  * dy [rows][m] and x [rows][k] of `type` (BF16 or F16); out binary32, element (i, j) of group g = n * inner + e at
  * out[n * outer_stride + e * inner_stride + i * ld_out + j]: with inner experts and groups sorted by (worker, expert) this is
- * each worker's own row of a flat gradient.  No two rows of out may overlap (INVALID_ARG: blocks write them at once).  accumulate != 0 adds to what out holds, one rounded addition per element.
+ * each worker's own row of a flat gradient.  No two rows of out may overlap (INVALID_ARG: blocks write them at once).
+ * accumulate != 0 adds to what out holds, one rounded addition per element.  The tensor cores' sums of up to 512 rows are joined by
+ * rounded additions: 2 to 5e-7 of the result off.
  * workspace as above, by regtopk_grouped_matmul_dw_workspace_bytes.  Errors as above. */
 size_t regtopk_grouped_matmul_dw_workspace_bytes(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t groups,
                                                  int64_t rows, int64_t k, int64_t m);

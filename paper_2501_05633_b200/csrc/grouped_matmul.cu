@@ -270,7 +270,15 @@ struct RowsArgs {
   float* partial;
 };
 
-constexpr int kRowThreads = threads_of(kRowShare);
+// Terms that one accumulator of k_rows sums before the sum moves on to registers (kWeightsChain, below, says why).  Outputs are rounded
+// to 16 bits, so that this may be more than for the weight gradients: 4,096 terms of one sign come out 2.6e-5 too small, a tenth of half
+// a step of float16 and less of bfloat16; without a limit 65,536 terms came out 4e-4 too small, nearly half a step.  Up to here a kernel
+// without those registers does it; longer sums take 0 to 4 % more time than they would in it (8,192 tokens over 16 matrices of 2304 x 8192: 312 us against
+// 308 us; with 2,048 terms 1 % more, and sums of 2,144 over 91 groups of 16 tokens in all 13.5 us in place of 12.1 us).
+constexpr int kRowsChain = 4096;
+// Writing warps for each quarter of the lanes: twice as many share the sums in registers.
+template <bool kLong> constexpr int kRowShareOf = kLong ? 2 * kRowShare : kRowShare;
+template <bool kLong> constexpr int kRowThreadsOf = threads_of(kRowShareOf<kLong>);
 constexpr int kTableGroups = REGTOPK_MATMUL_MAX_GROUPS;
 
 // How a group's rows are cut: as many tiles as the widest allows, all of one size but the last.
@@ -315,12 +323,13 @@ template <int kMost, int kCtas> struct RowStage {
   static constexpr int kSmem = kCount * kBytes + 1024;
 };
 
-template <typename T, int kMost, bool kTransposed, int kCtas>
-__global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const RowsArgs a) {
+// kLong: for sums of more than kRowsChain terms.
+template <typename T, int kMost, bool kTransposed, int kCtas, bool kLong>
+__global__ void __launch_bounds__(kRowThreadsOf<kLong>, 1) k_rows(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const RowsArgs a) {
   typedef RowStage<kMost, kCtas> Stage;
   constexpr int kStages = Stage::kCount, kBytesA = Stage::kBytesA, kBytes = Stage::kBytes;
   constexpr int kBoxRows = Stage::kTokens < 64 ? Stage::kTokens : 64;  // tokens of one copy
-  constexpr int kTmem = 2 * kMost;
+  constexpr int kTmem = 2 * kMost, kShare = kRowShareOf<kLong>, kRowThreads = kRowThreadsOf<kLong>;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ uint8_t raw[];
   __shared__ Shared<kStages> sh;
@@ -331,7 +340,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
 
   const u32 rank = cta_rank<kCtas>();
 
-  set_up<kCtas>(sh, kTmem, 4 * kRowShare);
+  set_up<kCtas>(sh, kTmem, 4 * kShare);
   // where each group's rows lie and how many tiles come before it; groups that share a matrix one after the other, so that
   // it is read from memory once (four workers over sixteen matrices of 9 MB: 752 MB read without that, 285 MB are needed)
   constexpr int kPer = (kTableGroups + kRowThreads - 1) / kRowThreads;  // groups of a thread
@@ -419,23 +428,34 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
     if (rank == 0) {
       u32 s = 0, parity = 0, n = 0;
       bool ok = true;
-      for (; t.at < tiles; t.next<kMost, kCtas>(), ++n) {
-        const u32 how = instruction<kCtas>(kBf16, kTransposed, false, rounded<kCtas>(t.count));
-        const u32 acc = sh.tmem + (n & 1) * kMost;
+      const auto take_accumulator = [&] {
         ok = ok && bar_wait(smem_at(&sh.free_[n & 1]), ((n >> 1) & 1) ^ 1, quit);
         tmem_fence_after();
+      };
+      for (; t.at < tiles; t.next<kMost, kCtas>(), ++n) {
+        const u32 how = instruction<kCtas>(kBf16, kTransposed, false, rounded<kCtas>(t.count));
+        u32 acc = sh.tmem + (n & 1) * kMost;
+        take_accumulator();
         const int k0 = t.part() * a.part_k, k1 = min(a.k, k0 + a.part_k);
+        bool begins = true;
         for (int d = k0; d < k1; d += kDepth) {
           ok = ok && bar_wait(smem_at(&sh.full[s]), parity, quit);
           __syncwarp();
+          const bool ends = d + kDepth >= k1, moves = kLong && !ends && (d - k0 + kDepth) % kRowsChain == 0;
           if (elected() && ok) {
             const u32 at = tiles_at + s * kBytes;
             multiply<kCtas, kTransposed, false>(acc, operand(at, kTransposed ? kBoxBytes : 0, 1024), Stage::kHalfA,
-                                                operand(at + kBytesA, 0, 1024), Stage::kHalfB, how, (min(kDepth, k1 - d) + 15) >> 4, d == k0);
+                                                operand(at + kBytesA, 0, 1024), Stage::kHalfB, how, (min(kDepth, k1 - d) + 15) >> 4, kLong ? begins : d == k0);
             mma_commit<kCtas>(smem_at(&sh.empty[s]));
-            if (d + kDepth >= k1) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
+            if (ends || moves) mma_commit<kCtas>(smem_at(&sh.done[n & 1]));
           }
           __syncwarp();
+          begins = moves;
+          if (moves) {  // on to the other accumulator
+            ++n;
+            acc = sh.tmem + (n & 1) * kMost;
+            take_accumulator();
+          }
           if (++s == kStages) {
             s = 0;
             parity ^= 1;
@@ -459,43 +479,81 @@ __global__ void __launch_bounds__(kRowThreads, 1) k_rows(const __grid_constant__
     const int part = warp & 3, first = ((warp >> 2) - 1) * 32;  // the lanes that this warp may read, and its first columns
     const u32 swap = (lane & 1) ? 0x3276 : 0x5410;
     T* y = static_cast<T*>(a.y);
-    for (; t.at < tiles; t.next<kMost, kCtas>(), ++n) {
+    const auto write = [&](const float (&v)[32], int f, int c0) {
+      T* to = y + (int64_t)(t.row + c0) * a.ldy + f;
+      const int left = f < a.m ? t.count - c0 : 0;
+      if (a.parts > 1) {
+        float* sums = a.partial + ((int64_t)t.part() * a.rows + t.row + c0) * a.m + f;
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          if (c < left) *sums = v[c];
+          sums += a.m;
+        }
+      } else if (a.pairs) {  // lanes of a pair of features exchange halves of two tokens, and each writes one token's pair
+        const int odd = lane & 1;
+        to += odd * (a.ldy - 1);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const u32 own = packed(v[c], v[c + 1], T()), other = __shfl_xor_sync(kAll, own, 1);
+          if (c + odd < left) *reinterpret_cast<u32*>(to) = __byte_perm(own, other, swap);
+          to += 2 * a.ldy;
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          if (c < left) *to = from_float<T>(v[c]);
+          to += a.ldy;
+        }
+      }
+    };
+    const auto await_sum = [&] {
       bar_wait(smem_at(&sh.done[n & 1]), (n >> 1) & 1, quit);  // given up: go on with what there is
       __syncwarp();
       tmem_fence_after();
-      const int f = t.feature + (int)rank * kLanes + part * 32 + lane;
-      for (int c0 = first; c0 < t.count; c0 += 32 * kRowShare) {
-        float v[32];
-        tmem_read(v, sh.tmem + (n & 1) * kMost + c0 + ((u32)(part * 32) << 16));
-        T* to = y + (int64_t)(t.row + c0) * a.ldy + f;
-        const int left = f < a.m ? t.count - c0 : 0;
-        if (a.parts > 1) {
-          float* sums = a.partial + ((int64_t)t.part() * a.rows + t.row + c0) * a.m + f;
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            if (c < left) *sums = v[c];
-            sums += a.m;
-          }
-        } else if (a.pairs) {  // lanes of a pair of features exchange halves of two tokens, and each writes one token's pair
-          const int odd = lane & 1;
-          to += odd * (a.ldy - 1);
-#pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const u32 own = packed(v[c], v[c + 1], T()), other = __shfl_xor_sync(kAll, own, 1);
-            if (c + odd < left) *reinterpret_cast<u32*>(to) = __byte_perm(own, other, swap);
-            to += 2 * a.ldy;
-          }
-        } else {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            if (c < left) *to = from_float<T>(v[c]);
-            to += a.ldy;
-          }
-        }
-      }
+    };
+    const auto pass_sum = [&] {
       tmem_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive_first<kCtas, false>(smem_at(&sh.free_[n & 1]));
+    };
+    for (; t.at < tiles; t.next<kMost, kCtas>()) {
+      const int f = t.feature + (int)rank * kLanes + part * 32 + lane;
+      if constexpr (kLong) {
+        constexpr int kChunks = (kMost + 32 * kShare - 1) / (32 * kShare);
+        float sum[kChunks][32];
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+          for (int c = 0; c < 32; ++c) sum[i][c] = 0.0f;
+        const int summed = min(a.part_k, a.k - t.part() * a.part_k);
+        for (int d = 0; d < summed; d += kRowsChain, ++n) {
+          await_sum();
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+            for (int c0 = 0; c0 < 32; c0 += 16) {
+              const int at = first + i * 32 * kShare + c0;
+              if (at >= t.count) continue;
+              float v[16];
+              tmem_read16(v, sh.tmem + (n & 1) * kMost + at + ((u32)(part * 32) << 16));
+#pragma unroll
+              for (int c = 0; c < 16; ++c) sum[i][c0 + c] += v[c];
+            }
+          pass_sum();
+        }
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i)
+          if (first + i * 32 * kShare < t.count) write(sum[i], f, first + i * 32 * kShare);
+      } else {
+        await_sum();
+        for (int c0 = first; c0 < t.count; c0 += 32 * kShare) {
+          float v[32];
+          tmem_read(v, sh.tmem + (n & 1) * kMost + c0 + ((u32)(part * 32) << 16));
+          write(v, f, c0);
+        }
+        pass_sum();
+        ++n;
+      }
     }
   }
   tear_down<kCtas>(sh, kTmem);
@@ -900,12 +958,12 @@ int launch(K kernel, int64_t tiles, int threads, int smem, int sms, cudaStream_t
   return start<kCtas>(kernel, (unsigned)(tiles < most ? tiles : most) * kCtas, threads, smem, s, args...);
 }
 
-template <typename T, int kMost, bool kTransposed, int kCtas>
+template <typename T, int kMost, bool kTransposed, int kCtas, bool kLong>
 int launch_rows(const CUtensorMap& w, const CUtensorMap& x, const RowsArgs& a, int64_t token_tiles, int dev, int sms, cudaStream_t s) {
-  constexpr auto k = k_rows<T, kMost, kTransposed, kCtas>;
+  constexpr auto k = k_rows<T, kMost, kTransposed, kCtas, kLong>;
   constexpr int smem = RowStage<kMost, kCtas>::kSmem;
   if (!allow_smem<k>(smem, dev)) return train_rc(cudaGetLastError());
-  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)) * a.parts, kRowThreads, smem, sms, s, w, x, a);
+  return launch<kCtas>(k, token_tiles * ((a.m + kCtas * kLanes - 1) / (kCtas * kLanes)) * a.parts, kRowThreadsOf<kLong>, smem, sms, s, w, x, a);
 }
 
 template <typename T, int kCtas>
@@ -1025,20 +1083,22 @@ int regtopk_grouped_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
   const int64_t tiles = plan.tiles;
   if (tiles * ((m + kLanes - 1) / kLanes) > INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
   auto launch_product = [&]() -> int {
-#define REGTOPK_ROWS(N, C)                                                                                 \
-  case N:                                                                                                  \
-    if (type == REGTOPK_TYPE_BF16)                                                                         \
-      return transposed ? launch_rows<__nv_bfloat16, N, true, C>(wm, xm, a, tiles, dev, sms, s)            \
-                        : launch_rows<__nv_bfloat16, N, false, C>(wm, xm, a, tiles, dev, sms, s);          \
-    return transposed ? launch_rows<__half, N, true, C>(wm, xm, a, tiles, dev, sms, s)                     \
-                      : launch_rows<__half, N, false, C>(wm, xm, a, tiles, dev, sms, s)
-  switch (most) {
-    REGTOPK_ROWS(32, 1);
-    REGTOPK_ROWS(64, 1);
-    REGTOPK_ROWS(128, 1);
-    default:
-    REGTOPK_ROWS(256, 2);
-  }
+#define REGTOPK_ROWS(N, C, L)                                                                        \
+  return type == REGTOPK_TYPE_BF16                                                                   \
+             ? (transposed ? launch_rows<__nv_bfloat16, N, true, C, L>(wm, xm, a, tiles, dev, sms, s)  \
+                           : launch_rows<__nv_bfloat16, N, false, C, L>(wm, xm, a, tiles, dev, sms, s)) \
+             : (transposed ? launch_rows<__half, N, true, C, L>(wm, xm, a, tiles, dev, sms, s)         \
+                           : launch_rows<__half, N, false, C, L>(wm, xm, a, tiles, dev, sms, s))
+#define REGTOPK_ROWS_OF(N, C)               \
+  if (a.part_k > kRowsChain) REGTOPK_ROWS(N, C, true); \
+  REGTOPK_ROWS(N, C, false)
+    switch (most) {
+      case 32: REGTOPK_ROWS_OF(32, 1);
+      case 64: REGTOPK_ROWS_OF(64, 1);
+      case 128: REGTOPK_ROWS_OF(128, 1);
+      default: REGTOPK_ROWS_OF(256, 2);
+    }
+#undef REGTOPK_ROWS_OF
 #undef REGTOPK_ROWS
   };
   const int done = launch_product();

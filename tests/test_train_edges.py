@@ -192,3 +192,28 @@ def test_norm_gradient_of_huge_rows(rows, cols):
     h, mean, rstd = (torch.full(s, v, device="cuda") for s, v in (((rows, cols), 3e37), ((rows,), 3e37), ((rows,), 316.0)))
     _, _, dw, _ = check_back(dy, h, mean, rstd, weight)
     assert not dw.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [HF, BF])
+@pytest.mark.parametrize("rows,groups,k,m,transposed", [
+    (2400, 150, 16384, 128, False), (2400, 150, 65536, 128, False), (3300, 75, 12345, 140, True), (5000, 20, 9000, 300, False),
+    (9000, 3, 8192, 1030, True), (9000, 40, 6001, 90, False), (40, 2, 65536, 300, False), (3000, 60, 4097, 264, True)])
+def test_long_products(rows, groups, k, m, transposed, dtype):
+    """Sums of thousands of values of one sign, in tiles of every width.  The tensor core cuts its running sum off at every step
+    of sixteen terms, always to the same side, so that the error grows with the steps of one accumulator.
+
+    Tolerance: half a step of the output's type, and for an accumulator of up to 4,096 terms 256 steps of at most twice 2^-23 of the
+    sum, 2^-14 in all; accumulators are joined with one rounding of 2^-24 each."""
+    gen = torch.Generator(device="cuda").manual_seed(rows + k)
+    made = lambda *s: (1 + 0.1 * torch.randn(*s, generator=gen, device="cuda")).to(dtype)  # noqa: E731
+    x, w = made(rows, k), 2.0 ** -8 * made(2, k, m).transpose(1, 2) if transposed else 2.0 ** -8 * made(2, m, k)
+    at = [0, *sorted(int(i) for i in torch.randint(0, rows + 1, (2 * groups - 1,), generator=gen, device="cuda")), rows]
+    got = rt.grouped_matmul(x, w, torch.tensor(at, device="cuda")).double()
+    half, most = 2.0 ** -11 if dtype == HF else 2.0 ** -8, 0.0
+    for g, (lo, hi) in enumerate(zip(at, at[1:])):
+        if lo < hi:
+            want = x[lo:hi].double() @ w[g % 2].double().T
+            most = max(most, float(((got[lo:hi] - want).abs() / want).max()))
+    assert most < half + 2.0 ** -14 + (k // 4096 + 1) * 2.0 ** -24, most
+    rt.training_status()
