@@ -11,6 +11,7 @@ import shutil
 import subprocess
 import sysconfig
 import tempfile
+import warnings
 from typing import Optional, Tuple
 
 import torch
@@ -63,6 +64,26 @@ def _stale(made: str, sources) -> bool:
     return not os.path.exists(made) or os.path.getmtime(made) < max(os.path.getmtime(f) for f in sources)
 
 
+def _missing_for_module() -> Optional[str]:
+    """What the marshalling module of the training operators needs and this machine lacks: a host compiler, Python's and torch's
+    headers.  The CUDA libraries need none of them but nvcc and what nvcc calls."""
+    if not shutil.which("g++"):
+        return "g++"
+    for where, header in ((sysconfig.get_paths()["include"], "Python.h"),
+                          (os.path.join(os.path.dirname(torch.__file__), "include"), os.path.join("torch", "csrc", "autograd", "python_variable.h"))):
+        if not os.path.exists(os.path.join(where, header)):
+            return os.path.join(where, header)
+    return None
+
+
+def _wait(runs) -> None:
+    for run in runs:
+        run.wait()
+    for run in runs:
+        if run.returncode:
+            raise subprocess.CalledProcessError(run.returncode, run.args)
+
+
 def build_training(force: bool = False, verbose: bool = False) -> str:
     """Compile the training operators for sm_100a into libregtopk_train.so, source by source side by side, and the Python
     module that marshals into it."""
@@ -72,16 +93,14 @@ def build_training(force: bool = False, verbose: bool = False) -> str:
             if verbose:
                 flags.insert(0, "-Xptxas=-v")
             objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in _TRAIN_SRC]
-            runs = [subprocess.Popen(["nvcc", *flags, "-c", "-o", o, f]) for f, o in zip(_TRAIN_SRC, objects)]
-            for run in runs:
-                run.wait()
-            for run in runs:
-                if run.returncode:
-                    raise subprocess.CalledProcessError(run.returncode, run.args)
+            _wait([subprocess.Popen(["nvcc", *flags, "-c", "-o", o, f]) for f, o in zip(_TRAIN_SRC, objects)])
             made = os.path.join(tmp, os.path.basename(_TRAIN_LIB))
             subprocess.run(["nvcc", *flags, "--shared", "-o", made, *objects], check=True)
             shutil.move(made, _TRAIN_LIB)
         if force or _stale(_TRAIN_MODULE, [_TRAIN_BINDING, *_TRAIN_DEPS[1:]]):
+            missing = _missing_for_module()
+            if missing:
+                raise RuntimeError(f"the Python module of the training operators cannot be built without {missing}")
             root = os.path.dirname(torch.__file__)
             cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc"))))
             made = os.path.join(tmp, os.path.basename(_TRAIN_MODULE))
@@ -96,16 +115,23 @@ def build_training(force: bool = False, verbose: bool = False) -> str:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile csrc/regtopk.cu for sm_100a into the package directory (nvcc cross-compiles without a GPU), and the
-    training operators beside it."""
-    build_training(force, verbose)
-    if not force and os.path.exists(_LIB) and os.path.getmtime(_LIB) >= max(
-            os.path.getmtime(_SRC), os.path.getmtime(os.path.join(_INC, "regtopk.h"))):
-        return _LIB
-    cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-I", _INC, "--shared", "-Xcompiler", "-fPIC", "-o", _LIB, _SRC]
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    subprocess.run(cmd, check=True)
+    training operators beside it.
+
+    Whatever becomes of the latter, the former is built; where only their Python module cannot be, because the machine lacks
+    what it needs and the sparsifier does not, this warns and goes on, and their calls raise."""
+    runs = []
+    if force or _stale(_LIB, [_SRC, os.path.join(_INC, "regtopk.h")]):
+        cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+               "-I", _INC, "--shared", "-Xcompiler", "-fPIC", "-o", _LIB, _SRC]
+        if verbose:
+            cmd.insert(1, "-Xptxas=-v")
+        runs.append(subprocess.Popen(cmd))
+    try:
+        build_training(force, verbose)
+    except RuntimeError as e:
+        warnings.warn(f"{e}; the sparsifier is not affected")
+    finally:
+        _wait(runs)
     return _LIB
 
 
