@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -124,6 +125,12 @@ void same_shape(const Tensor& t, const Tensor& x, const char* name, bool or_floa
       !(t.scalar_type() == x.scalar_type() || (or_float && t.scalar_type() == at::kFloat)))
     type_error(std::string(name) + " must match the input's shape, device and dtype" + (or_float ? " (or be float32)" : ""));
 }
+// A tensor that a call writes.  As with torch's own `out` arguments, one that autograd would have to follow is refused while it
+// records, and its version goes up, so that a backward pass that has saved it for its own use notices.
+void written(const Tensor& t, const char* name) {
+  if (at::GradMode::is_enabled() && t.requires_grad()) value_error(std::string(name) + " requires a gradient, but autograd does not see this call (use torch.no_grad())");
+  t.unsafeGetTensorImpl()->bump_version();
+}
 const float* vector_of(const Tensor& t, int64_t n, const Tensor& x, const char* name) {
   if (t.device() != x.device() || t.scalar_type() != at::kFloat || t.numel() != n || !t.is_contiguous())
     type_error(std::string(name) + " must be " + std::to_string(n) + " contiguous float32 values on the input's device");
@@ -185,6 +192,7 @@ PyObject* dropout(PyObject* const* a) {  // x, p, seed, subsequence, out
   if (given) same_shape(*given, x, "out");
   const Tensor out = given ? *given : empty(x.sizes(), x.scalar_type(), x);
   const Rows to = given ? rows_of(out, "out") : Rows{in.rows, in.cols, in.cols};
+  if (given) written(out, "out");
   check(regtopk_dropout(x.data_ptr(), in.ld, out.data_ptr(), to.ld, in.rows, in.cols, type, &drop, stream_of(x)), "regtopk_dropout");
   return THPVariable_Wrap(out);
 }
@@ -240,6 +248,8 @@ PyObject* layer_norm_backward(PyObject* const* a) {
     ld[i] = rows_of(*t, names[i]).ld;
   }
   if (accumulate && !dw && !db) value_error("accumulate needs dweight or dbias to add to");
+  if (dw) written(*dw, "dweight");
+  if (db) written(*db, "dbias");
   const c10::cuda::CUDAGuard guard(dy.device());
   Tensor made[2];
   if (!dw && !db) {
@@ -282,6 +292,7 @@ PyObject* grouped_matmul(PyObject* const* a) {  // x, w, offsets, out
     type_error("out must be [" + std::to_string(in.rows) + ", " + std::to_string(m) + "] of x's dtype on x's device");
   const Tensor y = given ? *given : empty({in.rows, m}, x.scalar_type(), x);
   const int64_t ldy = given ? rows_of(y, "out").ld : m;
+  if (given) written(y, "out");
   const int32_t weights = static_cast<int32_t>(count);
   const int64_t stride = count > 1 ? w.stride(0) : ldw * (transposed ? k : m);
   const size_t bytes = regtopk_grouped_matmul_workspace_bytes(x.data_ptr(), in.ld, w.data_ptr(), ldw, stride, transposed, weights, groups, in.rows, k, m);
@@ -315,6 +326,7 @@ PyObject* grouped_matmul_dw(PyObject* const* a) {  // dy, x, offsets, out, accum
   const int64_t ld = m > 1 ? out.stride(n - 2) : k;
   if ((k > 1 && out.stride(n - 1) != 1) || ld < k) value_error("out: the elements of a row must be contiguous and rows must not overlap");
   if (out.numel() && !elements_apart(out)) value_error("out: matrices overlap");
+  if (given) written(out, "out");
   const int32_t inner = n == 3 ? groups : static_cast<int32_t>(out.size(1));
   const int64_t inner_stride = out.stride(n - 3), outer_stride = n == 3 ? 0 : out.stride(0);
   const size_t bytes = regtopk_grouped_matmul_dw_workspace_bytes(dy.data_ptr(), up.ld, x.data_ptr(), in.ld, groups, up.rows, k, m);

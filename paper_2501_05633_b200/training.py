@@ -5,7 +5,8 @@ int64 device tensor, says where each group of rows begins and where the last one
 and come per group; they may be written, or added, straight into views of RegTopK.accumulator().
 
 Everything runs on the current torch stream of the tensors' device and is asynchronous like any torch CUDA op; autograd
-does not see it, the gradients are calls of their own.  There is no CPU path: if the library is missing or a tensor is
+does not see it, the gradients are calls of their own.  A tensor given to be written must not require a gradient while autograd
+records; its version goes up as with torch's in-place operations.  There is no CPU path: if the library is missing or a tensor is
 not on a CUDA device, the calls raise.  Wrong types, shapes and devices raise TypeError, wrong values and strides
 ValueError, and what the library refuses or fails at RegTopKError.
 """

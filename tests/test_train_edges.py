@@ -217,3 +217,38 @@ def test_long_products(rows, groups, k, m, transposed, dtype):
             most = max(most, float(((got[lo:hi] - want).abs() / want).max()))
     assert most < half + 2.0 ** -14 + (k // 4096 + 1) * 2.0 ** -24, most
     rt.training_status()
+
+
+@pytest.mark.gpu
+def test_autograd_notices_what_is_written():
+    """A tensor that a call writes: its version goes up (so that a backward pass that saved it refuses to use it), and while
+    autograd records it must not require a gradient."""
+    x, w = torch.randn(40, 16, device="cuda"), torch.ones(16, device="cuda")
+    dy, xs, ws = torch.randn(40, 24, device="cuda").to(BF), x.to(BF), torch.randn(2, 24, 16, device="cuda").to(BF)
+    off = torch.tensor([0, 15, 40], device="cuda")
+    _, _, mean, rstd = rt.layer_norm(x, w)
+    calls = [(lambda out: rt.dropout(x, 0.1, 0, out=out), torch.zeros(40, 16, device="cuda")),
+             (lambda out: rt.layer_norm_backward(x, x, mean, rstd, w, offsets=off, dweight=out), torch.zeros(2, 16, device="cuda")),
+             (lambda out: rt.layer_norm_backward(x, x, mean, rstd, w, offsets=off, dbias=out, accumulate=True), torch.zeros(2, 16, device="cuda")),
+             (lambda out: rt.grouped_matmul(xs, ws, off, out=out), torch.zeros(40, 24, dtype=BF, device="cuda")),
+             (lambda out: rt.grouped_matmul_dw(dy, xs, off, out=out), torch.zeros(2, 24, 16, device="cuda"))]
+    for call, out in calls:
+        before = out._version
+        call(out)
+        assert out._version == before + 1
+        scale = torch.ones_like(out, requires_grad=True)
+        loss = (scale * out).sum()  # saves out for the gradient to scale
+        call(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        leaf = out.clone().requires_grad_()
+        with pytest.raises(ValueError):
+            call(leaf)
+        with torch.no_grad():
+            call(leaf)
+        assert torch.equal(leaf, out) or call is calls[2][0], "accumulates"
+    with torch.inference_mode():
+        rt.dropout(x, 0.1, 0, out=torch.zeros(40, 16, device="cuda"))
+    shared = torch.zeros(2, 32, device="cuda")
+    rt.layer_norm_backward(x, x, mean, rstd, w, offsets=off, dweight=shared[:, :16], dbias=shared[:, 16:])
+    assert shared._version > 0
