@@ -12,6 +12,7 @@
  *     device memory.  A workspace holds nothing between calls; two calls that may run at once need one each.
  *   - Matrices are row-major; a leading dimension counts elements from one row to the next, and a row's elements are
  *     contiguous.  Any alignment that the element type allows is accepted; 16-byte aligned rows are read fastest.
+ *   - Outputs overlap neither inputs nor one another, except where a call says that they may.
  *   - Calls enqueue work on cuda_stream (a cudaStream_t of the current device, NULL = default stream) and return
  *     without synchronising.  Return value: REGTOPK_OK or a negative REGTOPK_ERR_* code of regtopk.h.  Nothing aborts,
  *     throws or traps.

@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -131,6 +132,11 @@ void written(const Tensor& t, const char* name) {
   if (at::GradMode::is_enabled() && t.requires_grad()) value_error(std::string(name) + " requires a gradient, but autograd does not see this call (use torch.no_grad())");
   t.unsafeGetTensorImpl()->bump_version();
 }
+// Refuses an output that shares memory with an input, where torch can tell.  `same`: it may be the very input.
+void apart(const Tensor& out, const Tensor& in, const char* name, bool same = false) {
+  const at::MemOverlapStatus how = at::get_overlap_status(out, in);
+  if (how == at::MemOverlapStatus::Partial || (how == at::MemOverlapStatus::Full && !same)) value_error(std::string("out and ") + name + " overlap");
+}
 const float* vector_of(const Tensor& t, int64_t n, const Tensor& x, const char* name) {
   if (t.device() != x.device() || t.scalar_type() != at::kFloat || t.numel() != n || !t.is_contiguous())
     type_error(std::string(name) + " must be " + std::to_string(n) + " contiguous float32 values on the input's device");
@@ -192,6 +198,7 @@ PyObject* dropout(PyObject* const* a) {  // x, p, seed, subsequence, out
   if (given) same_shape(*given, x, "out");
   const Tensor out = given ? *given : empty(x.sizes(), x.scalar_type(), x);
   const Rows to = given ? rows_of(out, "out") : Rows{in.rows, in.cols, in.cols};
+  if (given) apart(out, x, "x", true);
   if (given) written(out, "out");
   check(regtopk_dropout(x.data_ptr(), in.ld, out.data_ptr(), to.ld, in.rows, in.cols, type, &drop, stream_of(x)), "regtopk_dropout");
   return THPVariable_Wrap(out);
@@ -292,7 +299,11 @@ PyObject* grouped_matmul(PyObject* const* a) {  // x, w, offsets, out
     type_error("out must be [" + std::to_string(in.rows) + ", " + std::to_string(m) + "] of x's dtype on x's device");
   const Tensor y = given ? *given : empty({in.rows, m}, x.scalar_type(), x);
   const int64_t ldy = given ? rows_of(y, "out").ld : m;
-  if (given) written(y, "out");
+  if (given) {
+    apart(y, x, "x");
+    apart(y, w, "w");
+    written(y, "out");
+  }
   const int32_t weights = static_cast<int32_t>(count);
   const int64_t stride = count > 1 ? w.stride(0) : ldw * (transposed ? k : m);
   const size_t bytes = regtopk_grouped_matmul_workspace_bytes(x.data_ptr(), in.ld, w.data_ptr(), ldw, stride, transposed, weights, groups, in.rows, k, m);

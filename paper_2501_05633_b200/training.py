@@ -40,7 +40,8 @@ def dropout(x: torch.Tensor, p: float, seed: int, subsequence: int = 0, out: Opt
     """x with each element kept with probability 1 - t / 65536 and then scaled by its inverse, t = round(65536 p).
 
     The mask is a function of the element's row and column, seed and subsequence alone (regtopk_train.h states it), and
-    is not stored: the same call on the gradient is the backward pass.  Rows are the last dimension.  out may be x."""
+    is not stored: the same call on the gradient is the backward pass.  Rows are the last dimension.  out may be x, but must
+    not overlap it otherwise."""
     return (_native or _load()).dropout(x, p, seed, subsequence, out)
 
 

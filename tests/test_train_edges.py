@@ -252,3 +252,26 @@ def test_autograd_notices_what_is_written():
     shared = torch.zeros(2, 32, device="cuda")
     rt.layer_norm_backward(x, x, mean, rstd, w, offsets=off, dweight=shared[:, :16], dbias=shared[:, 16:])
     assert shared._version > 0
+
+
+@pytest.mark.gpu
+def test_outputs_that_overlap_inputs_are_refused():
+    flat = torch.ones(4096, device="cuda")
+    x = flat[:1024].view(64, 16)
+    for out in (flat[16:1040].view(64, 16), flat[1008:2032].view(64, 16)):
+        with pytest.raises(ValueError):
+            rt.dropout(x, 0.5, 1, out=out)
+    assert (flat == 1).all()
+    assert torch.equal(rt.dropout(x, 0.5, 1, out=flat[1024:2048].view(64, 16)), rt.dropout(x, 0.5, 1))
+    rt.dropout(x, 0.5, 1, out=x)
+    off = torch.tensor([0, 10, 32], device="cuda")
+    short = torch.ones(4096, dtype=BF, device="cuda")
+    a, w = short[:512].view(32, 16), short[1024:1536].view(2, 16, 16)
+    for out in (a, short[256:768].view(32, 16), short[1000:1512].view(32, 16)):
+        with pytest.raises(ValueError):
+            rt.grouped_matmul(a, w, off, out=out)
+    assert (short == 1).all()
+    assert (rt.grouped_matmul(a, w, off, out=short[512:1024].view(32, 16)) == 16).all()
+    # columns of one array beside one another do not overlap
+    both = torch.ones(32, 32, dtype=BF, device="cuda")
+    assert (rt.grouped_matmul(both[:, :16], w, off, out=both[:, 16:]) == 16).all() and (both[:, :16] == 1).all()
