@@ -6,6 +6,8 @@ import torch
 
 import paper_2501_05633_b200 as rt
 from tests import train_reference as ref
+from tests.test_train_norm import TYPES, check_norm, norm_case
+from tests.test_train_norm import made as rows_made
 
 BF, HF, F = torch.bfloat16, torch.float16, torch.float32
 
@@ -275,3 +277,24 @@ def test_outputs_that_overlap_inputs_are_refused():
     # columns of one array beside one another do not overlap
     both = torch.ones(32, 32, dtype=BF, device="cuda")
     assert (rt.grouped_matmul(both[:, :16], w, off, out=both[:, 16:]) == 16).all() and (both[:, :16] == 1).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,stream", TYPES)
+@pytest.mark.parametrize("rows,cols", [(4001, 257), (3001, 1023), (2500, 1024), (1301, 2047), (700, 4096), (400, 8192), (200, 16383)])
+def test_norm_of_many_rows(rows, cols, dtype, stream):
+    """More rows than teams of warps, so that each team takes several, through rings in shared memory: one warp a row and
+    several, one to four units of columns a warp, two and three arrays, aligned rows and others, groups that end anywhere.
+    The forward pass by test_train_norm's tolerance, the backward pass by check_back's."""
+    for p, pad, shift, more in ((0.1, 0, 0, True), (0.0, 5, 1, False), (0.3, 3, 1, True)):
+        x, residual, weight, bias, gen = norm_case(rows, cols, dtype, stream, rows + cols, pad, shift)
+        if not more:
+            residual = None
+        if more or stream == dtype:
+            check_norm(x, residual, weight, bias, p, 99)
+        h = (residual if more else rows_made(rows, cols, stream, gen, pad, shift))
+        dy, dh = rows_made(rows, cols, dtype, gen, pad, shift), rows_made(rows, cols, stream, gen, pad, shift)
+        _, _, mean, rstd = rt.layer_norm(h, weight, bias)
+        cut = sorted(int(i) for i in torch.randint(0, rows + 1, (4,), generator=gen))
+        check_back(dy, h, mean, rstd, weight, dh if more else None, [0, *cut, cut[-1], rows], p)
+    rt.training_status()
