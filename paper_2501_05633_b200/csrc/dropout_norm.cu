@@ -335,7 +335,7 @@ struct NormArgs {
 // Mean and sum of squared deviations come from the registers in two passes within a warp and are then combined over the
 // team by the rule for joining two samples (Chan, Golub, LeVeque 1979): nothing is lost when the mean is large beside the
 // deviation, and one exchange a row is enough.
-// RING false: every team has one row at most and reads it, and the vectors, where they are.
+// RING false: a team has a few rows at most (plan_of says how many) and reads them, and the vectors for each, where they are.
 // 32,768 rows of 1,024 bfloat16 columns with dropout beside a binary32 stream, 403 MB: 70 to 76 us, 5.3 to 5.8 TB/s, with 54 %
 // of the issue slots busy.
 template <typename T, typename S, bool VEC, int U, bool RING>
@@ -688,9 +688,11 @@ __global__ void __launch_bounds__(32 * kRuns) k_norm_sum(const NormSumArgs a) {
 //   teams or more.  Two rows of a team are under way, up to four where an SM has fewer than twelve teams (8 teams, 32,768 rows of
 //   1,024 columns, bfloat16 beside a binary32 stream: 69.5 us against 85 us; with twelve, 6,000 rows of 1,000 bfloat16 columns
 //   only start later: 17.8 us against 15.6 us).
-//   no rings, where a team would have one row at most (or two rows do not fit): as many warps a row as it has units,
-//   because then the time is that of one row (backward pass, 1,000 rows of 1,000 columns: 14.3 us against 20.5 us with four
-//   units a warp).
+//   no rings, where no team of the rings would have a second row (or two rows do not fit): as many warps a row as it has units,
+//   because then the time is nearly that of one row (backward pass, 1,000 rows of 1,000 columns: 14.3 us against 20.5 us with
+//   four units a warp).  There are fewer teams then, so that one takes a few rows in turn: up to three of 1,024 bfloat16 columns, 592
+//   teams where the rings have 1,776.  Rings from the second row on would take 5.9 us in place of 7.0 us for 1,500 such rows, and in the
+//   backward pass 19.3 us in place of 16.6 us for 1,000 and 19.6 us in place of 18.0 us for 1,500.
 struct Plan {
   int units, threads, blocks;
   size_t smem;
@@ -841,13 +843,13 @@ int regtopk_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t
   a.cols = (int)cols; a.eps = eps; a.wide = (uintptr_t)weight % 16 == 0 && (uintptr_t)bias % 16 == 0;
   const bool vec = cols % 8 == 0 && rows_aligned(x, ldx, size, rows) && rows_aligned(y, ldy, size, rows) &&
                    rows_aligned(residual, ld_residual, ssize, rows) && rows_aligned(h, ldh, ssize, rows);
-  // Up to 1,024 columns two units a warp and 24 warps on an SM, sixteen where a binary32 stream comes in beside more than 512; wider,
-  // where the warps of a row wait for one another, four units and sixteen warps.  32,768 rows of 1,024 bfloat16 columns: 61.7 us,
-  // 70.4 us with four units; beside a binary32 stream 69.5 us, 78.0 us with 24 warps; 8,192 rows of 4,096: 55.9 us, 73.7 us with
-  // two units.
-  const bool few = cols > 512 && cols <= 1024 && vec && residual && ssize == 4;
+  // Up to 1,024 columns two units a warp and 24 warps on an SM; wider, where the warps of a row wait for one another, four units and
+  // sixteen warps.  32,768 rows of 1,024 bfloat16 columns: 61.7 us, 70.4 us with four units; 8,192 rows of 4,096: 55.9 us, 73.7 us
+  // with two units.  Beside a binary32 stream too: sixteen warps, which leave room for four rows of a team under way, take 65 to 66 us for
+  // 32,768 rows of 520, 640 and 768 columns against 58 to 59 us, 15.5 us for 4,096 of 1,024 against 14.1 us, and as long for 32,768 of 1,000
+  // and of 1,024 (71 to 78 us against 70 to 75 us, either the shorter from one run to the next).
   const Plan p = plan_of(cols, rows, {size, residual ? ssize : 0, 0}, cols <= 1024 || size + ssize == 8 ? 2 : 4,
-                         cols <= 1024 && !few ? 3 : 2, 2, 0, sms);
+                         cols <= 1024 ? 3 : 2, 2, 0, sms);
   a.ring = p.ring;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
 #define REGTOPK_NORM(T, S, V, U) launch_norm<T, S, V, U>(a, p, dev, sms, s)
