@@ -38,6 +38,7 @@ extern "C" {
 enum { REGTOPK_TYPE_F32 = 0, REGTOPK_TYPE_BF16 = 1, REGTOPK_TYPE_F16 = 2 };
 
 #define REGTOPK_NORM_MAX_COLS 16384   /* widest row of a layer norm */
+#define REGTOPK_NORM_MAX_GROUPS 65535 /* most groups of one layer norm's weight gradients */
 #define REGTOPK_MATMUL_MAX_GROUPS 2048 /* most groups of one grouped product */
 
 /* Dropout with a mask that is never stored.  t = 65536 p rounded to the nearest whole number; the element in column c
@@ -54,7 +55,8 @@ typedef struct {
   uint32_t subsequence;
 } regtopk_dropout_params;
 
-/* y = dropout(x), both [rows][cols] of `type`; y may be x.  rows, cols >= 0.  Errors: INVALID_ARG, NO_DEVICE, CUDA. */
+/* y = dropout(x), both [rows][cols] of `type`; y may be x.  rows, cols >= 0; cols <= 2^34.
+ * Errors: INVALID_ARG, NO_DEVICE, CUDA. */
 int regtopk_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, int32_t type,
                     const regtopk_dropout_params* drop, void* cuda_stream);
 
@@ -76,7 +78,8 @@ int regtopk_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t
  *   dx = dropout(dresidual), the mask of the forward pass
  *   dweight[n] (+)= sum of dy * u,  dbias[n] (+)= sum of dy,  over the rows of group n, each in row n of its array
  * dy, dx of `type`; h, dh, dresidual of `stream_type`; dresidual NULL: not written.  dweight, dbias binary32 with
- * leading dimensions of their own, NULL: not wanted.  offsets NULL: one group of all rows (groups is then 1).
+ * leading dimensions of their own, NULL: not wanted.  offsets NULL: one group of all rows (groups is then 1);
+ * 1 <= groups <= REGTOPK_NORM_MAX_GROUPS.
  * accumulate != 0 adds to what dweight and dbias hold.  Rows of no group get their dx and add to no weight gradient.
  * workspace: 16-byte aligned, at least regtopk_layer_norm_backward_workspace_bytes(rows, cols, groups) bytes; may be NULL
  * if neither dweight nor dbias is wanted.  Errors: as above, and WORKSPACE_TOO_SMALL. */

@@ -874,8 +874,8 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
   const size_t size = type_size(type), ssize = type_size(stream_type);
   const bool sums = dweight || dbias;
   if (!size || !ssize || (stream_type != type && stream_type != REGTOPK_TYPE_F32) || rows < 0 || cols < 1 || groups < 1 ||
-      groups > 65535 || (!offsets && groups != 1) || (uintptr_t)offsets % 8 || !make_drop(drop, &a.drop)) return REGTOPK_ERR_INVALID_ARG;
-  if (cols > REGTOPK_NORM_MAX_COLS) return REGTOPK_ERR_TOO_LARGE;
+      (!offsets && groups != 1) || (uintptr_t)offsets % 8 || !make_drop(drop, &a.drop)) return REGTOPK_ERR_INVALID_ARG;
+  if (cols > REGTOPK_NORM_MAX_COLS || groups > REGTOPK_NORM_MAX_GROUPS) return REGTOPK_ERR_TOO_LARGE;
   if ((dweight && !good_matrix(dweight, ld_dweight, groups, cols, 4)) || (dbias && !good_matrix(dbias, ld_dbias, groups, cols, 4)))
     return REGTOPK_ERR_INVALID_ARG;
   if (rows > 0 && (!good_matrix(dy, ld_dy, rows, cols, size) || !good_matrix(h, ldh, rows, cols, ssize) ||

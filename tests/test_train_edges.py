@@ -97,6 +97,27 @@ def test_c_matrices_that_overlap():
     assert dw(inner_stride=2**62, outer_stride=2**62) == -1
 
 
+def test_c_most_groups():
+    """More groups than a launch has rows of blocks come back as too large, as the products' do."""
+    lib, p = ref.c_library(), 4096
+
+    def back(groups, rows=0):
+        return lib.regtopk_layer_norm_backward(p, 8, p, 8, p, p, p, None, 0, p, 8, None, 0, p, 8, None, 0, p, groups, 0, rows, 8, 0, 0, None, p, 1 << 40, None)
+    assert back(65536) == -7 and back(65536, 4) == -7 and back(0) == -1
+
+
+@pytest.mark.gpu
+def test_most_groups():
+    h = torch.randn(300, 24, generator=torch.Generator().manual_seed(1)).cuda()
+    w = torch.ones(24, device="cuda")
+    _, _, mean, rstd = rt.layer_norm(h, w)
+    at = torch.arange(65536, device="cuda").clamp(max=300)  # a group for each row, and empty ones
+    _, _, dw, db = rt.layer_norm_backward(h, h, mean, rstd, w, offsets=at)
+    assert torch.equal(db[:300], h) and not db[300:].any() and not dw[300:].any()
+    with pytest.raises(rt.RegTopKError):
+        rt.layer_norm_backward(h, h, mean, rstd, w, offsets=torch.arange(65537, device="cuda").clamp(max=300))
+
+
 @pytest.mark.gpu
 def test_matrices_that_overlap_are_refused():
     gen = torch.Generator().manual_seed(3)
