@@ -161,6 +161,21 @@ struct Team {
   }
 };
 
+// Waits for a row that has not come yet.  If it does not, the team's first lane (`drains`) waits once more for all that is under
+// way, because the shared memory is another block's after this one's end.  Stages without a copy come last and cost one more such
+// wait in all.
+__device__ __noinline__ bool ring_wait(u32 bars, u32 stage, u32 phase, int stages, volatile u32* quit, bool drains) {
+  if (bar_wait_long(bars + stage * 8, phase, quit)) return true;
+  for (int i = 0; i < stages && drains; ++i) {
+    bar_wait(bars + stage * 8, phase, quit + 1);
+    if (++stage == (u32)stages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+  return false;
+}
+
 // A team's ring: it holds the rows first, first + step, ... below `end` of the arrays, one after the other.
 // WALKS: where the copies go on from is kept in registers and goes from row to row by additions; otherwise it is worked out
 // from the row.  The forward pass is faster with the former (6,000 rows of 1,000 bfloat16 columns 17.6 us against 19.0 us),
@@ -170,7 +185,7 @@ template <bool WALKS> struct Ring {
   const Source* source;
   char* base;
   u32 bars;
-  volatile u32* quit;
+  volatile u32* quit;  // and in the word behind it: given up a second time
   int64_t step, end;
   u32 stage, phase;      // where the next row to be read lies
   const char* ahead[3];  // WALKS: of each array the row to be requested next,
@@ -204,8 +219,12 @@ template <bool WALKS> struct Ring {
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                      ::"r"(to[i]), "l"(from[i]), "r"(size[i]), "r"(bar) : "memory");
   }
-  // Waits for the next row.  Should it not come, the kernel runs to its end with what there is (see bar_wait).
-  __device__ __forceinline__ void await() const { bar_wait(bars + stage * 8, phase, quit); }
+  // Waits for the next row.  Should it not come (see bar_wait), nothing more is requested, and the kernel runs to its end with what
+  // there is.
+  __device__ __forceinline__ void await(bool leads) {
+    if (!bar_done(bars + stage * 8, phase) && !ring_wait(bars, stage, phase, shape.stages, quit, leads && (WALKS ? left : end) >= 0))
+      (WALKS ? left : end) = -1;
+  }
   // Array number `array` of the next row, which is row `row` of the arrays.
   template <typename T, bool VEC, bool RING> __device__ __forceinline__ const T* row_of(int64_t row, int array) const {
     if (!RING) return reinterpret_cast<const T*>(source[array].p + row * source[array].pitch);
@@ -277,7 +296,7 @@ template <bool VEC> __device__ __forceinline__ void load_vector(Octet& f, const 
 struct Common {
   uint64_t bars[kMostWarps][kMostStages];  // [team][stage]
   float2 exchange[2][kMostWarps];          // two sets used in turn
-  u32 quit;
+  u32 quit[2];
 };
 
 __device__ __forceinline__ int padded(int cols) { return (cols + 255) & ~255; }
@@ -286,7 +305,7 @@ __device__ __forceinline__ int padded(int cols) { return (cols + 255) & ~255; }
 template <bool RING, bool WALKS>
 __device__ __forceinline__ Ring<WALKS> make_ring(Common& common, const RingShape& shape, const Source* source, char* rings, const Team& t,
                                                  int64_t first, int64_t step, int64_t end) {
-  Ring<WALKS> ring{shape, source, rings + t.index * shape.stages * shape.stage_bytes, smem_at(&common.bars[t.index][0]), &common.quit,
+  Ring<WALKS> ring{shape, source, rings + t.index * shape.stages * shape.stage_bytes, smem_at(&common.bars[t.index][0]), common.quit,
                    step, end, 0, 0};
   if (!RING) return ring;
   if (WALKS) {
@@ -298,7 +317,7 @@ __device__ __forceinline__ Ring<WALKS> make_ring(Common& common, const RingShape
       ring.low[i] = (u32)(uintptr_t)ring.ahead[i];
     }
   }
-  if (threadIdx.x == 0) common.quit = 0;
+  if (threadIdx.x == 0) common.quit[0] = common.quit[1] = 0;
   if (t.leads()) {
     for (int i = 0; i < shape.stages; ++i) bar_init(ring.bars + i * 8, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -361,7 +380,7 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ No
   const int64_t y_leap = step * a.ldy, h_leap = step * a.ldh;
   u32 turn = 0;
   for (int64_t row = first; row < a.rows; row += step, turn ^= 1, y += y_leap, sum_out += h_leap) {
-    if (RING) ring.await();
+    if (RING) ring.await(t.leads());
     Octet f[U];
     float2 sum = both(0.0f), square = both(0.0f);
     const T* x = ring.row_of<T, VEC, RING>(row, 0);
@@ -516,7 +535,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_c
         next_mean = a.mean[row + step];
         next_rstd = a.rstd[row + step];
       }
-      if (RING) ring.await();
+      if (RING) ring.await(t.leads());
       const T* dy = ring.row_of<T, VEC, RING>(row, 0);
       const S* h = ring.row_of<S, VEC, RING>(row, 1);
       float2 s1 = both(0.0f), s2 = both(0.0f);
