@@ -3,8 +3,9 @@
 // All of them have memory traffic for their floor: a few operations per element and one read and one write of each array.
 // So each kernel reads every input once, keeps many copies under way, and draws the dropout mask again wherever it is
 // needed instead of storing it (one Philox call for eight columns costs less issue time than a byte of mask costs
-// bandwidth).  Dropout reaches that floor; the norms spend 1.2 to 1.4 instructions of a lane on a value and are bound by
-// their issue.
+// bandwidth).  Dropout reaches that floor.  The norms spend 1.2 to 1.5 instructions of a lane on a value at 16 to 24 warps an SM:
+// little over half of the issue slots and of the memory's bandwidth are in use, and it is the latency between the two, with too few
+// warps to hide it, that binds them.
 
 #include "train_common.cuh"
 
@@ -178,8 +179,10 @@ __device__ __noinline__ bool ring_wait(u32 bars, u32 stage, u32 phase, int stage
 
 // A team's ring: it holds the rows first, first + step, ... below `end` of the arrays, one after the other.
 // WALKS: where the copies go on from is kept in registers and goes from row to row by additions; otherwise it is worked out
-// from the row.  The forward pass is faster with the former (6,000 rows of 1,000 bfloat16 columns 17.6 us against 19.0 us),
-// the backward pass, which has no registers to spare, with the latter (2,048 rows of 8,192: 73 us against 84 us).
+// from the row.  The forward pass is faster with the former for most sizes (16,384 rows of 1,023 bfloat16 columns 48.0 us against
+// 50.5 us, 20,000 of 232 float16 columns beside a binary32 stream 14.8 us against 15.7 us, but 6,000 of 1,000 bfloat16 columns 17.1 us
+// against 15.7 us), the backward pass, which has no registers to spare, with the latter (2,048 rows of 8,192: 78 us against 83 us;
+// 16,384 of 1,023: 70 us against 84 us).
 template <bool WALKS> struct Ring {
   const RingShape& shape;
   const Source* source;
@@ -704,9 +707,9 @@ __global__ void __launch_bounds__(32 * kRuns) k_norm_sum(const NormSumArgs a) {
 // How a row is shared and how the shared memory of an SM is divided.
 //   rings: `blocks` blocks of eight warps on an SM (one of sixteen for the widest rows); a warp takes up to
 //   `most_units` units.  `vectors` float32 vectors of the columns lie beside the rings, `joint` more where a block has two
-//   teams or more.  Two rows of a team are under way, up to four where an SM has fewer than twelve teams (8 teams, 32,768 rows of
-//   1,024 columns, bfloat16 beside a binary32 stream: 69.5 us against 85 us; with twelve, 6,000 rows of 1,000 bfloat16 columns
-//   only start later: 17.8 us against 15.6 us).
+//   teams or more.  Two rows of a team are under way, up to four where an SM has fewer than twelve teams (gradient of 4,096 rows of
+//   4,096 binary32 columns, two teams to an SM: 76 us against 101 us; wide 16-bit rows lose 3 %, 2,000 of 8,192 take 42.5 us
+//   against 41.2 us; with twelve teams, 6,000 rows of 1,000 bfloat16 columns only start later: 18.1 us against 17.1 us).
 //   no rings, where no team of the rings would have a second row (or two rows do not fit): as many warps a row as it has units,
 //   because then the time is nearly that of one row (backward pass, 1,000 rows of 1,000 columns: 14.3 us against 20.5 us with
 //   four units a warp).  There are fewer teams then, so that one takes a few rows in turn: up to three of 1,024 bfloat16 columns, 592
@@ -865,8 +868,8 @@ int regtopk_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t
   // Up to 1,024 columns two units a warp and 24 warps on an SM; wider, where the warps of a row wait for one another, four units and
   // sixteen warps.  32,768 rows of 1,024 bfloat16 columns: 61.7 us, 70.4 us with four units; 8,192 rows of 4,096: 55.9 us, 73.7 us
   // with two units.  Beside a binary32 stream too: sixteen warps, which leave room for four rows of a team under way, take 65 to 66 us for
-  // 32,768 rows of 520, 640 and 768 columns against 58 to 59 us, 15.5 us for 4,096 of 1,024 against 14.1 us, and as long for 32,768 of 1,000
-  // and of 1,024 (71 to 78 us against 70 to 75 us, either the shorter from one run to the next).
+  // 32,768 rows of 520, 640 and 768 columns against 58 to 59 us, 15.5 us for 4,096 of 1,024 against 14.1 us, and for 32,768 of 1,000 and
+  // of 1,024, the only sizes where they are faster, 70 to 78 us from run to run against 70 to 77 us, 3 % less on average.
   const Plan p = plan_of(cols, rows, {size, residual ? ssize : 0, 0}, cols <= 1024 || size + ssize == 8 ? 2 : 4,
                          cols <= 1024 ? 3 : 2, 2, 0, sms);
   a.ring = p.ring;
