@@ -3,7 +3,7 @@
 // All of them have memory traffic for their floor: a few operations per element and one read and one write of each array.
 // So each kernel reads every input once, keeps many copies under way, and draws the dropout mask again wherever it is
 // needed instead of storing it (one Philox call for eight columns costs less issue time than a byte of mask costs
-// bandwidth).  Dropout reaches that floor.  The norms spend 1.2 to 1.5 instructions of a lane on a value at 16 to 24 warps an SM:
+// bandwidth).  Dropout reaches that floor.  The norms spend 40 to 46 instructions of a lane on a value at 16 to 24 warps an SM:
 // little over half of the issue slots and of the memory's bandwidth are in use, and it is the latency between the two, with too few
 // warps to hide it, that binds them.
 
@@ -358,7 +358,7 @@ struct NormArgs {
 // team by the rule for joining two samples (Chan, Golub, LeVeque 1979): nothing is lost when the mean is large beside the
 // deviation, and one exchange a row is enough.
 // RING false: a team has a few rows at most (plan_of says how many) and reads them, and the vectors for each, where they are.
-// 32,768 rows of 1,024 bfloat16 columns with dropout beside a binary32 stream, 403 MB: 70 to 76 us, 5.3 to 5.8 TB/s, with 54 %
+// 32,768 rows of 1,024 bfloat16 columns with dropout beside a binary32 stream, 403 MB: 70 to 77 us, 5.2 to 5.8 TB/s, with 60 %
 // of the issue slots busy.
 template <typename T, typename S, bool VEC, int U, bool RING>
 __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_norm(const __grid_constant__ NormArgs a) {
@@ -486,7 +486,7 @@ __device__ __forceinline__ int group_of(const int64_t* offsets, int groups, int6
 // gradients in registers; where the range meets the end of a group the sums so far go to the slot (block + group) of
 // the partial sums.  With ascending groups no two blocks share a slot: a later block's groups are not lower, so
 // block + group only grows.
-// 32,768 rows of 1,024 bfloat16 columns with dropout, 336 MB: 83 us with the sum after it, 4.0 TB/s.  58 % of the issue slots
+// 32,768 rows of 1,024 bfloat16 columns with dropout, 336 MB: 83 to 85 us with the sum after it, 4.0 TB/s.  58 % of the issue slots
 // are busy with eight warps a block, whose 128 registers a thread leave no room for more of them.
 template <typename T, typename S, bool VEC, int U, bool RING>
 __global__ void __launch_bounds__(32 * kMostWarps, 1) k_norm_back(const __grid_constant__ NormBackArgs a) {

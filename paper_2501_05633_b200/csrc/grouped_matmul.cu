@@ -16,9 +16,10 @@
 // both operands, and the products of the first block read both halves.  Tiles lie in shared memory in the 128-byte
 // swizzle, copied in boxes that are 64 elements (128 bytes) wide.
 //
-// What bounds them (B200, 1.3-1.9 GHz under its power limit): 32,768 tokens in 64 groups, 2,048 -> 2,304, 246 us or
-// 1,260 TFLOP/s (282 us where the power limit has set in; the tensor core is active for 77 % of the cycles), where the same loops without any copies take 219 us and a library's product of one dense group of the same
-// sizes 209 us: groups that are no multiple of 256 tokens cost 5 %, tiles of 207 tokens on average the rest.
+// What bounds them (B200, 1.3-1.9 GHz under its power limit): 32,768 tokens in 64 groups, 2,048 -> 2,304, 240 us or 1,290 TFLOP/s, 288 us
+// or 1,070 where the power limit has set in; the tensor core is active for 77 % of the cycles.  The same loops without any copies take
+// 219 us and a library's product of one dense group of the same sizes 209 us: groups that are no multiple of 256 tokens cost 5 %,
+// tiles of 207 tokens on average the rest.
 
 #include <cuda.h>
 #include <string.h>
@@ -617,7 +618,7 @@ struct WeightWalk {
   }
 };
 
-// 32,768 tokens in 32 groups, 1,024 x 2,304, into rows of eight workers: 167 to 195 us, 792 to 925 TFLOP/s.  The products wait for
+// 32,768 tokens in 32 groups, 1,024 x 2,304, into rows of eight workers: 193 to 199 us, 780 to 800 TFLOP/s; added to what the rows hold, 227 to 232 us.  The products wait for
 // accumulators on their way through registers and for the gradient's 302 MB (tensor core active for 46 % of the cycles).
 template <typename T, int kCtas>
 __global__ void __launch_bounds__(kWeightThreads, 1) k_weights(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap dy_map, const WeightsArgs a) {
