@@ -285,7 +285,7 @@ constexpr int kTableGroups = REGTOPK_MATMUL_MAX_GROUPS;
 // How a group's rows are cut: as many tiles as the widest allows, all of one size but the last.
 __device__ __forceinline__ int tile_rows(int count, int most) {
   const int tiles = (count + most - 1) / most;
-  return tiles ? ((count + tiles - 1) / tiles + 15) & ~15 : 16;
+  return tiles ? (int)(((u32)count + (u32)tiles - 1) / (u32)tiles + 15) & ~15 : 16;  // count + tiles may pass 2^31
 }
 
 // The tiles of a pair (or a block), every `pairs`-th of all: for each tile of tokens those of the features one after the other.

@@ -319,3 +319,26 @@ def test_norm_of_many_rows(rows, cols, dtype, stream):
         cut = sorted(int(i) for i in torch.randint(0, rows + 1, (4,), generator=gen))
         check_back(dy, h, mean, rstd, weight, dh if more else None, [0, *cut, cut[-1], rows], p)
     rt.training_status()
+
+
+MOST = 2**31 - 2**20  # rows, k and m of a product
+
+
+@pytest.mark.gpu
+def test_largest_sizes():
+    """The most rows and the longest sum, of values whose sums are exact however they are grouped."""
+    x = torch.ones(MOST, 8, dtype=BF, device="cuda")
+    off = torch.tensor([0, MOST], device="cuda")
+    dw = rt.grouped_matmul_dw(x, x, off)
+    assert (dw == float(MOST)).all()
+    dw = rt.grouped_matmul_dw(x, x, torch.tensor([0, MOST - 1024, MOST - 1], device="cuda"))
+    assert (dw[0] == float(MOST - 1024)).all() and (dw[1] == 1023).all()
+    w = torch.eye(8, dtype=BF, device="cuda")[None]
+    w[:, 7, 7] = 2.0
+    y = rt.grouped_matmul(x, w, off)
+    top = torch.tensor([1.0] * 7 + [2.0], device="cuda")
+    assert torch.equal(y.amin(0).float(), top) and torch.equal(y.amax(0).float(), top)
+    del x, y
+    x, w = (torch.full((1, MOST), v, dtype=HF, device="cuda") for v in (2.0**-10, 2.0**-21))
+    assert rt.grouped_matmul(x, w[None], torch.tensor([0, 1], device="cuda")).item() == 1 - 2.0**-11
+    rt.training_status()
