@@ -40,6 +40,7 @@ enum { REGTOPK_TYPE_F32 = 0, REGTOPK_TYPE_BF16 = 1, REGTOPK_TYPE_F16 = 2 };
 #define REGTOPK_NORM_MAX_COLS 16384   /* widest row of a layer norm */
 #define REGTOPK_NORM_MAX_GROUPS 65535 /* most groups of one layer norm's weight gradients */
 #define REGTOPK_MATMUL_MAX_GROUPS 2048 /* most groups of one grouped product */
+#define REGTOPK_MATMUL_MAX_SIZE 0x7FF00000 /* its largest rows, k and m, 2^31 - 2^20 */
 
 /* Dropout with a mask that is never stored.  t = 65536 p rounded to the nearest whole number; the element in column c
  * of row r is kept if its 16-bit number n(r, c) is at least t, and is then multiplied by 65536 / (65536 - t); it is +0
@@ -100,7 +101,7 @@ int regtopk_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, in
  * tokens.  groups is a multiple of weights: groups sorted by (worker, expert) share the experts' matrices.
  * Products are exact and sums binary32 on the tensor cores, which cut the running sum off where an addition would round: sums of up to
  * 4,096 terms are some 3e-5 of the sum of magnitudes too small at most, and longer ones are joined from such by rounded additions.  y is
- * rounded once.  rows < 2^31; k, m < 2^31; k == 0 gives zeros.
+ * rounded once.  rows, k, m <= REGTOPK_MATMUL_MAX_SIZE; k == 0 gives zeros.
  * workspace: 16-byte aligned, at least regtopk_grouped_matmul_workspace_bytes(...) bytes, which hold a copy of
  * x or w where it has no 16-byte aligned rows (base and leading dimension; for w the stride between matrices too), and partial
  * sums where k is long and there are few rows; often 0.  Errors: INVALID_ARG, TOO_LARGE (groups), WORKSPACE_TOO_SMALL, NO_DEVICE, CUDA. */

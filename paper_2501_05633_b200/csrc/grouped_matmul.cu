@@ -983,7 +983,10 @@ int parts_of(int64_t tiles, int64_t places, int64_t summed) {
 }
 constexpr int kPlaces = 148;
 
-constexpr int64_t kMostRows = 0x7FFFFF00;  // coordinates of a copy are 32-bit, and a tile may reach past the end
+// Coordinates of a copy are 32-bit, and what is worked out from them may pass the end: a tile by 256, an accumulator's terms by kRowsChain,
+// a divided dimension by kDepth for each of kPlaces parts.
+constexpr int64_t kMostRows = REGTOPK_MATMUL_MAX_SIZE;
+static_assert(kMostRows + kRowsChain + kWeightsChain + (int64_t)kPlaces * kDepth < ((int64_t)1 << 31) - 1, "32-bit arithmetic");
 
 struct RowPlan {
   int most, parts, part_k;  // tokens of a tile; parts of the summed dimension and their length

@@ -324,6 +324,15 @@ def test_norm_of_many_rows(rows, cols, dtype, stream):
 MOST = 2**31 - 2**20  # rows, k and m of a product
 
 
+def test_c_largest_sizes():
+    """What is worked out in 32 bits from rows, k and m stays below 2^31; larger ones are refused before anything is launched."""
+    lib, p = ref.c_library(), 4096
+    for rows, k, m in ((MOST + 1, 8, 8), (8, MOST + 1, 8), (8, 8, MOST + 1), (2**31 - 256, 8, 8)):
+        assert lib.regtopk_grouped_matmul(p, k, p, k, 0, 0, 1, p, m, p, 1, rows, k, m, 1, None, 0, None) == -1
+        assert lib.regtopk_grouped_matmul_dw(p, m, p, k, p, k, 0, 0, 1, 0, p, 1, rows, k, m, 1, None, 0, None) == -1
+        assert lib.regtopk_grouped_matmul_workspace_bytes(p, k + 1, p, k, 0, 0, 1, 1, rows, k, m) == 0
+
+
 @pytest.mark.gpu
 def test_largest_sizes():
     """The most rows and the longest sum, of values whose sums are exact however they are grouped."""
