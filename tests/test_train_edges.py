@@ -351,3 +351,43 @@ def test_largest_sizes():
     x, w = (torch.full((1, MOST), v, dtype=HF, device="cuda") for v in (2.0**-10, 2.0**-21))
     assert rt.grouped_matmul(x, w[None], torch.tensor([0, 1], device="cuda")).item() == 1 - 2.0**-11
     rt.training_status()
+
+
+@pytest.mark.gpu
+def test_captured_graph():
+    """A whole step recorded as a CUDA graph and replayed on other inputs gives the bits of the calls themselves: every launch may
+    start while the one before it ends, and unaligned operands, divided sums and joins are among them."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    rows, cols, m = 900, 257, 90
+    w, b = torch.randn(cols, generator=gen, device="cuda"), torch.randn(cols, generator=gen, device="cuda")
+    experts = (torch.randn(2, m, cols, generator=gen, device="cuda") / 16).to(BF)
+    off, one = torch.tensor([0, 100, 500, 620, rows], device="cuda"), torch.tensor([0, rows], device="cuda")
+    x, residual = torch.zeros(rows, cols, dtype=BF, device="cuda"), torch.zeros(rows, cols, device="cuda")
+    rows_out = torch.zeros(2, 2 * m * cols + 3, device="cuda")
+
+    def step():
+        y, h, mean, rstd = rt.layer_norm(rt.dropout(x, 0.1, 3), w, b, residual=residual, p=0.2, seed=5, subsequence=1)
+        o = rt.grouped_matmul(y, experts, off)
+        dy = rt.grouped_matmul(o, experts.transpose(1, 2), off)
+        rt.grouped_matmul_dw(o, y, off, out=rows_out[:, 3:].view(2, 2, m, cols), accumulate=True)
+        whole = rt.grouped_matmul_dw(o, y, one)
+        return [y, h, mean, rstd, o, dy, whole, *rt.layer_norm_backward(dy, h, mean, rstd, w, dh=h, p=0.2, seed=5, subsequence=1, offsets=off)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for _ in range(3):
+        x.copy_(torch.randn(rows, cols, generator=gen, device="cuda"))
+        residual.copy_(torch.randn(rows, cols, generator=gen, device="cuda"))
+        rows_out.zero_()
+        graph.replay()
+        got = [t.clone() for t in kept] + [rows_out.clone()]
+        rows_out.zero_()
+        want = step() + [rows_out]
+        assert all(torch.equal(a, c) for a, c in zip(got, want))
+    rt.training_status()
