@@ -21,10 +21,13 @@ _ROOT = os.path.dirname(_PKG)
 _SRC = os.path.join(_PKG, "csrc", "regtopk.cu")
 _INC = os.path.join(_ROOT, "include")
 _LIB = os.path.join(_PKG, "libregtopk.so")
-_TRAIN_SRC = [os.path.join(_PKG, "csrc", name) for name in ("dropout_norm.cu", "grouped_matmul.cu")]
-_TRAIN_DEPS = [os.path.join(_PKG, "csrc", "train_common.cuh"), os.path.join(_INC, "regtopk_train.h"), os.path.join(_INC, "regtopk.h")]
+_TRAIN_SRC = [os.path.join(_PKG, "csrc", name) for name in
+              ("dropout_norm.cu", "grouped_matmul.cu", "route.cu", "move_tokens.cu", "activation.cu", "rms_norm.cu")]
+_TRAIN_HEADERS = [os.path.join(_INC, name) for name in ("regtopk_experts.h", "regtopk_train.h", "regtopk.h")]
+_TRAIN_DEPS = [os.path.join(_PKG, "csrc", name) for name in ("train_common.cuh", "norm_rows.cuh", "rows8.cuh")] + _TRAIN_HEADERS
 _TRAIN_LIB = os.path.join(_PKG, "libregtopk_train.so")
-_TRAIN_BINDING = os.path.join(_PKG, "csrc", "training_binding.cpp")
+_TRAIN_BINDING = [os.path.join(_PKG, "csrc", name) for name in ("training_binding.cpp", "experts_binding.cpp")]
+_TRAIN_BINDING_DEPS = [os.path.join(_PKG, "csrc", "binding_common.h")] + _TRAIN_HEADERS
 _TRAIN_MODULE = os.path.join(_PKG, "_training.so")
 
 OK = 0
@@ -97,18 +100,20 @@ def build_training(force: bool = False, verbose: bool = False) -> str:
             made = os.path.join(tmp, os.path.basename(_TRAIN_LIB))
             subprocess.run(["nvcc", *flags, "--shared", "-o", made, *objects], check=True)
             shutil.move(made, _TRAIN_LIB)
-        if force or _stale(_TRAIN_MODULE, [_TRAIN_BINDING, *_TRAIN_DEPS[1:]]):
+        if force or _stale(_TRAIN_MODULE, _TRAIN_BINDING + _TRAIN_BINDING_DEPS):
             missing = _missing_for_module()
             if missing:
                 raise RuntimeError(f"the Python module of the training operators cannot be built without {missing}")
             root = os.path.dirname(torch.__file__)
             cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc"))))
             made = os.path.join(tmp, os.path.basename(_TRAIN_MODULE))
-            subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                            "-I", _INC, "-I", os.path.join(root, "include"), "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-                            "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-o", made, _TRAIN_BINDING,
-                            "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
-                            "-L", _PKG, "-lregtopk_train", "-Wl,-rpath,$ORIGIN"], check=True)
+            flags = ["-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                     "-I", _INC, "-I", os.path.join(root, "include"), "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                     "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include")]
+            objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in _TRAIN_BINDING]
+            _wait([subprocess.Popen(["g++", *flags, "-c", "-o", o, f]) for f, o in zip(_TRAIN_BINDING, objects)])
+            subprocess.run(["g++", "-shared", "-o", made, *objects, "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                            "-ltorch_cuda", "-ltorch_python", "-L", _PKG, "-lregtopk_train", "-Wl,-rpath,$ORIGIN"], check=True)
             shutil.move(made, _TRAIN_MODULE)
     return _TRAIN_LIB
 

@@ -1180,6 +1180,7 @@ int regtopk_train_status(void* cuda_stream) {
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   int rc = gave_up(s);
   if (rc == 0) rc = regtopk_norm_gave_up(s);
+  if (rc == 0) rc = regtopk_rms_gave_up(s);
   return rc > 0 ? REGTOPK_ERR_INTERNAL : rc;
 }
 

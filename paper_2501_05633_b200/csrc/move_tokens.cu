@@ -1,0 +1,307 @@
+// The tokens' way into the order of their (worker, expert) groups and back, with its gradient (include/regtopk_experts.h).
+//
+// Memory traffic is the floor.  Tokens are the ones that a thread goes by, and not the sorted rows: then a token's row, its place
+// numbers and weights are read once, and the rows of its experts, which lie anywhere, are whole rows that are written, or read, once.
+
+#include "rows8.cuh"
+
+namespace {
+
+constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32;
+
+struct MoveArgs {
+  const void* in;            // spread: the tokens, or values of their 8-bit rows; join: the sorted rows; backward: dout
+  const uint8_t* in_scales;
+  const void* other;         // join: residual, or NULL; backward: the sorted rows
+  const int32_t* place;
+  const float* weights;
+  const int64_t* filled;     // NULL: no row is cleared
+  void* out;
+  float* dweights;
+  int64_t ld_in, ld_scales, ld_other, ld_out, tokens, rows, cols;
+  Divisor pieces;            // of a row: threads (VEC) or warps
+  u32 total;                 // of this launch
+  int k, team;               // team: warps of a token (backward)
+  bool clears;               // this launch clears the rows behind the last
+};
+
+__device__ __forceinline__ bool in_rows(int32_t p, int64_t rows) { return p >= 0 && p < rows; }
+
+// Zeros to the rows from *filled on, by all threads of the grid.
+template <typename T, bool VEC> __device__ __forceinline__ void clear_tail(const MoveArgs& a) {
+  if (!a.filled || !a.clears) return;
+  int64_t first = *a.filled;
+  first = first < 0 ? 0 : first > a.rows ? a.rows : first;
+  const int64_t threads = (int64_t)gridDim.x * kMoveThreads, own = (int64_t)blockIdx.x * kMoveThreads + threadIdx.x;
+  const int64_t pieces = VEC ? a.cols / 8 : a.cols;
+  for (int64_t i = own; i < (a.rows - first) * pieces; i += threads) {
+    const int64_t r = i / pieces, c = i - r * pieces;
+    T* to = static_cast<T*>(a.out) + (first + r) * a.ld_out;
+    if (VEC) {
+      Eight<T> v;
+      v.clear();
+      v.store(to + c * 8);
+    } else {
+      to[c] = from_float<T>(0.0f);
+    }
+  }
+}
+
+// Which token and which of its columns: VEC: a thread has eight neighbours; otherwise a warp has 256 columns.
+template <bool VEC> struct Piece {
+  int64_t token, c0;
+  int lane;
+  bool there;
+  __device__ __forceinline__ Piece(const MoveArgs& a) {
+    const u32 at = blockIdx.x * (VEC ? kMoveThreads : kMoveWarps) + (VEC ? threadIdx.x : threadIdx.x >> 5);
+    const u32 r = a.pieces.quotient_of(at);
+    there = at < a.total;
+    token = r;
+    c0 = (int64_t)(at - r * a.pieces.d) * (VEC ? 8 : 256);
+    lane = VEC ? 0 : threadIdx.x & 31;
+  }
+};
+
+template <typename T, bool PACKED, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_spread(const __grid_constant__ MoveArgs a) {
+  begin_after_predecessor();
+  const Piece<VEC> at(a);
+  if (at.there) {
+    Octet f;
+    Eight<T> v;
+    if (PACKED) read_rows8<VEC>(f, static_cast<const uint8_t*>(a.in) + at.token * a.ld_in, a.in_scales + at.token * a.ld_scales, at.c0, at.lane, a.cols);
+    else if (VEC) v.fetch(static_cast<const T*>(a.in) + at.token * a.ld_in + at.c0);
+    else read_eight<T, VEC, false>(f, static_cast<const T*>(a.in) + at.token * a.ld_in, at.c0, at.lane, a.cols);
+    if (PACKED && VEC) v.put(f);
+    const int32_t* place = a.place + at.token * a.k;
+    for (int j = 0; j < a.k; ++j) {
+      const int32_t p = place[j];
+      if (!in_rows(p, a.rows)) continue;
+      T* to = static_cast<T*>(a.out) + (int64_t)p * a.ld_out;
+      if (VEC) v.store(to + at.c0);
+      else store_eight<T, VEC>(f, to, at.c0, at.lane, a.cols);
+    }
+  }
+  clear_tail<T, VEC>(a);
+}
+
+constexpr int kJoinStep = 4;  // rows under way
+
+template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_join(const __grid_constant__ MoveArgs a) {
+  begin_after_predecessor();
+  const Piece<VEC> at(a);
+  if (!at.there) return;
+  const int32_t* place = a.place + at.token * a.k;
+  const float* weights = a.weights + at.token * a.k;
+  Octet sum;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = both(0.0f);
+  for (int j0 = 0; j0 < a.k; j0 += kJoinStep) {
+    int32_t p[kJoinStep];
+    float w[kJoinStep];
+#pragma unroll
+    for (int j = 0; j < kJoinStep; ++j) {
+      p[j] = j0 + j < a.k ? place[j0 + j] : -1;
+      w[j] = !a.weights ? 1.0f : j0 + j < a.k ? weights[j0 + j] : 0.0f;
+    }
+    Octet f[kJoinStep];
+#pragma unroll
+    for (int j = 0; j < kJoinStep; ++j) {
+      const bool there = in_rows(p[j], a.rows);
+      read_eight<T, VEC, false>(f[j], static_cast<const T*>(a.in) + (there ? (int64_t)p[j] * a.ld_in : 0), at.c0, at.lane, there ? a.cols : 0);
+      if (!there) w[j] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kJoinStep; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = fma2(f[j][i], both(w[j]), sum[i]);
+  }
+  if (a.other) {
+    Octet r;
+    read_eight<O, VEC, false>(r, static_cast<const O*>(a.other) + at.token * a.ld_other, at.c0, at.lane, a.cols);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = add2(sum[i], r[i]);
+  }
+  store_eight<O, VEC>(sum, static_cast<O*>(a.out) + at.token * a.ld_out, at.c0, at.lane, a.cols);
+}
+
+// A team of warps a token: its warps share the row's units of 256 columns, and each keeps the products of eight of the token's rows
+// with dout under way.
+constexpr int kBackStep = 8;
+template <typename T, typename D, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_join_back(const __grid_constant__ MoveArgs a) {
+  __shared__ float part[kMoveWarps][kBackStep];
+  begin_after_predecessor();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, member = warp % a.team, teams = kMoveWarps / a.team;
+  const int64_t t = (int64_t)blockIdx.x * teams + warp / a.team;
+  const bool there = t < a.tokens;
+  for (int j0 = 0; j0 < a.k; j0 += kBackStep) {
+    int32_t p[kBackStep];
+    float w[kBackStep], dot[kBackStep];
+#pragma unroll
+    for (int j = 0; j < kBackStep; ++j) {
+      p[j] = there && j0 + j < a.k ? a.place[t * a.k + j0 + j] : -1;
+      w[j] = there && j0 + j < a.k ? a.weights[t * a.k + j0 + j] : 0.0f;
+      dot[j] = 0.0f;
+    }
+    if (there) {
+      for (int64_t c0 = member * 256; c0 < a.cols; c0 += a.team * 256) {
+        Octet d;
+        read_eight<D, VEC, false>(d, static_cast<const D*>(a.in) + t * a.ld_in, c0, lane, a.cols);
+#pragma unroll
+        for (int j = 0; j < kBackStep; ++j) {
+          if (!in_rows(p[j], a.rows)) continue;
+          Octet f;
+          read_eight<T, VEC, false>(f, static_cast<const T*>(a.other) + (int64_t)p[j] * a.ld_other, c0, lane, a.cols);
+          float2 s = both(0.0f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s = fma2(f[i], d[i], s);
+            f[i] = mul2(d[i], both(w[j]));
+          }
+          dot[j] += s.x + s.y;
+          store_eight<T, VEC>(f, static_cast<T*>(a.out) + (int64_t)p[j] * a.ld_out, c0, lane, a.cols);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kBackStep; ++j) {
+      if (j0 + j >= a.k) break;
+      const float s = warp_sum(dot[j]);
+      if (lane == 0) part[warp][j] = s;
+    }
+    __syncthreads();
+    if (member == 0 && lane < kBackStep && there && j0 + lane < a.k) {
+      float s = 0.0f;
+      for (int i = 0; i < a.team; ++i) s += part[warp + i][lane];
+      a.dweights[t * a.k + j0 + lane] = s;
+    }
+    __syncthreads();
+  }
+  clear_tail<T, VEC>(a);
+}
+
+// ---- launches --------------------------------------------------------------------------------------------------------
+constexpr int64_t kMostCols = (int64_t)1 << 30, kMostPieces = ((int64_t)1 << 31) - kMoveThreads;
+
+// launch(args, grid) for as many tokens at a time as have fewer than 2^31 pieces.
+template <typename Launch> int in_parts(MoveArgs a, bool vec, size_t in_size, size_t other_size, size_t out_size, const Launch& launch) {
+  const int64_t pieces = vec ? a.cols / 8 : (a.cols + 255) / 256, tokens = a.tokens, most = kMostPieces / pieces;
+  const u32 per = vec ? kMoveThreads : kMoveWarps;
+  a.pieces = divisor(pieces);
+  int64_t done = 0;
+  do {
+    a.tokens = tokens - done < most ? tokens - done : most;
+    a.total = (u32)(a.tokens * pieces);
+    a.clears = done == 0;
+    const unsigned blocks = (a.total + per - 1) / per;
+    const int rc = launch(a, blocks ? blocks : 1u);
+    if (rc != REGTOPK_OK) return rc;
+    done += a.tokens;
+    a.in = static_cast<const char*>(a.in) + a.tokens * a.ld_in * (int64_t)in_size;
+    if (a.in_scales) a.in_scales += a.tokens * a.ld_scales;
+    if (a.other) a.other = static_cast<const char*>(a.other) + a.tokens * a.ld_other * (int64_t)other_size;
+    a.place += a.tokens * a.k;
+    if (a.weights) a.weights += a.tokens * a.k;
+    a.out = static_cast<char*>(a.out) + a.tokens * a.ld_out * (int64_t)out_size;
+  } while (done < tokens);
+  return REGTOPK_OK;
+}
+
+inline bool bad_shape(int64_t tokens, int32_t k, int64_t rows, int64_t cols) {
+  return tokens < 0 || k < 1 || rows < 0 || cols < 0 || cols > kMostCols || tokens > INT64_MAX / 64;
+}
+
+}  // namespace
+
+#define REGTOPK_BY_TYPE(call) \
+  (type == REGTOPK_TYPE_F32 ? call(float) : type == REGTOPK_TYPE_BF16 ? call(__nv_bfloat16) : call(__half))
+#define REGTOPK_BY_TYPES(call, second)                                                                            \
+  (type == REGTOPK_TYPE_F32    ? call(float, float)                                                               \
+   : type == REGTOPK_TYPE_BF16 ? (second == type ? call(__nv_bfloat16, __nv_bfloat16) : call(__nv_bfloat16, float)) \
+   : second == type            ? call(__half, __half)                                                             \
+                               : call(__half, float))
+
+extern "C" {
+
+int regtopk_spread_tokens(const void* x, int64_t ldx, const uint8_t* scales, int64_t ld_scales, const int32_t* place,
+                          const int64_t* filled, void* out, int64_t ld_out, int64_t tokens, int32_t k, int64_t rows, int64_t cols,
+                          int32_t type, void* cuda_stream) {
+  const size_t size = type_size(type);
+  if (!size || bad_shape(tokens, k, rows, cols) || (uintptr_t)filled % 8) return REGTOPK_ERR_INVALID_ARG;
+  if (k > REGTOPK_ROUTE_MAX_CHOICES) return REGTOPK_ERR_TOO_LARGE;
+  if (rows == 0 || cols == 0) return REGTOPK_OK;
+  if (!good_matrix(out, ld_out, rows, cols, size)) return REGTOPK_ERR_INVALID_ARG;
+  if (tokens > 0 && (!good_matrix(place, k, 1, k, 4) || (scales ? !good_rows8(static_cast<const uint8_t*>(x), ldx, scales, ld_scales, tokens, cols, 1)
+                                                                : !good_matrix(x, ldx, tokens, cols, size)))) return REGTOPK_ERR_INVALID_ARG;
+  int dev, sms;
+  if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
+  MoveArgs a = {};
+  a.in = x; a.ld_in = ldx; a.in_scales = scales; a.ld_scales = ld_scales; a.place = place; a.filled = filled; a.out = out; a.ld_out = ld_out;
+  a.tokens = tokens; a.rows = rows; a.cols = cols; a.k = k;
+  const bool vec = cols % 8 == 0 && rows_aligned(out, ld_out, size, rows) &&
+                   (scales ? rows8_aligned(static_cast<const uint8_t*>(x), ldx, tokens) : rows_aligned(x, ldx, size, tokens));
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return in_parts(a, vec, scales ? 1 : size, 0, 0, [&](const MoveArgs& part, unsigned grid) {
+#define REGTOPK_SPREAD(T)                                                                                         \
+  (scales ? (vec ? start(k_spread<T, true, true>, grid, kMoveThreads, 0, s, part) : start(k_spread<T, true, false>, grid, kMoveThreads, 0, s, part)) \
+          : (vec ? start(k_spread<T, false, true>, grid, kMoveThreads, 0, s, part) : start(k_spread<T, false, false>, grid, kMoveThreads, 0, s, part)))
+    return REGTOPK_BY_TYPE(REGTOPK_SPREAD);
+#undef REGTOPK_SPREAD
+  });
+}
+
+int regtopk_join_tokens(const void* from, int64_t ld_from, const int32_t* place, const float* weights, const void* residual,
+                        int64_t ld_residual, void* out, int64_t ld_out, int64_t tokens, int32_t k, int64_t rows, int64_t cols,
+                        int32_t type, int32_t out_type, void* cuda_stream) {
+  const size_t size = type_size(type), osize = type_size(out_type);
+  if (!size || !osize || (out_type != type && out_type != REGTOPK_TYPE_F32) || bad_shape(tokens, k, rows, cols) || (uintptr_t)weights % 4)
+    return REGTOPK_ERR_INVALID_ARG;
+  if (k > REGTOPK_ROUTE_MAX_CHOICES) return REGTOPK_ERR_TOO_LARGE;
+  if (tokens == 0 || cols == 0) return REGTOPK_OK;
+  if (!good_matrix(out, ld_out, tokens, cols, osize) || !good_matrix(place, k, 1, k, 4) || (rows > 0 && !good_matrix(from, ld_from, rows, cols, size)) ||
+      (residual && !good_matrix(residual, ld_residual, tokens, cols, osize))) return REGTOPK_ERR_INVALID_ARG;
+  int dev, sms;
+  if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
+  MoveArgs a = {};
+  a.in = from; a.ld_in = ld_from; a.other = residual; a.ld_other = ld_residual; a.place = place; a.weights = weights; a.out = out; a.ld_out = ld_out;
+  a.tokens = tokens; a.rows = rows; a.cols = cols; a.k = k;
+  const bool vec = cols % 8 == 0 && rows_aligned(from, ld_from, size, rows) && rows_aligned(out, ld_out, osize, tokens) &&
+                   rows_aligned(residual, ld_residual, osize, tokens);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return in_parts(a, vec, 0, osize, osize, [&](const MoveArgs& part, unsigned grid) {
+#define REGTOPK_JOIN(T, O) (vec ? start(k_join<T, O, true>, grid, kMoveThreads, 0, s, part) : start(k_join<T, O, false>, grid, kMoveThreads, 0, s, part))
+    return REGTOPK_BY_TYPES(REGTOPK_JOIN, out_type);
+#undef REGTOPK_JOIN
+  });
+}
+
+int regtopk_join_tokens_backward(const void* dout, int64_t ld_dout, const void* from, int64_t ld_from, const int32_t* place,
+                                 const float* weights, const int64_t* filled, void* dfrom, int64_t ld_dfrom, float* dweights,
+                                 int64_t tokens, int32_t k, int64_t rows, int64_t cols, int32_t type, int32_t dout_type,
+                                 void* cuda_stream) {
+  const size_t size = type_size(type), dsize = type_size(dout_type);
+  if (!size || !dsize || (dout_type != type && dout_type != REGTOPK_TYPE_F32) || bad_shape(tokens, k, rows, cols) || (uintptr_t)filled % 8)
+    return REGTOPK_ERR_INVALID_ARG;
+  if (k > REGTOPK_ROUTE_MAX_CHOICES || tokens > INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
+  if (rows > 0 && cols > 0 && (!good_matrix(from, ld_from, rows, cols, size) || !good_matrix(dfrom, ld_dfrom, rows, cols, size))) return REGTOPK_ERR_INVALID_ARG;
+  if (tokens > 0 && (!good_matrix(place, k, 1, k, 4) || !good_matrix(weights, k, 1, k, 4) || !good_matrix(dweights, k, 1, k, 4) ||
+                     (cols > 0 && !good_matrix(dout, ld_dout, tokens, cols, dsize)))) return REGTOPK_ERR_INVALID_ARG;
+  if (tokens == 0 && (rows == 0 || cols == 0)) return REGTOPK_OK;
+  int dev, sms;
+  if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
+  MoveArgs a = {};
+  a.in = dout; a.ld_in = ld_dout; a.other = from; a.ld_other = ld_from; a.place = place; a.weights = weights; a.filled = filled;
+  a.out = dfrom; a.ld_out = ld_dfrom; a.dweights = dweights; a.tokens = tokens; a.rows = cols ? rows : 0; a.cols = cols; a.k = k; a.clears = true;
+  const bool vec = cols % 8 == 0 && rows_aligned(dout, ld_dout, dsize, tokens) && rows_aligned(from, ld_from, size, rows) && rows_aligned(dfrom, ld_dfrom, size, rows);
+  // As many warps a token as it has units, while that leaves fewer than 16 warps for an SM.
+  const int64_t units = (cols + 255) / 256;
+  a.team = 1;
+  while (a.team < kMoveWarps && a.team < units && tokens * a.team < (int64_t)sms * 16) a.team *= 2;
+  const int64_t teams = kMoveWarps / a.team, blocks = tokens ? (tokens + teams - 1) / teams : 1;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+#define REGTOPK_JOIN_BACK(T, D) \
+  (vec ? start(k_join_back<T, D, true>, (unsigned)blocks, kMoveThreads, 0, s, a) : start(k_join_back<T, D, false>, (unsigned)blocks, kMoveThreads, 0, s, a))
+  return REGTOPK_BY_TYPES(REGTOPK_JOIN_BACK, dout_type);
+#undef REGTOPK_JOIN_BACK
+}
+
+}  // extern "C"

@@ -305,4 +305,5 @@ inline int gave_up(cudaStream_t s) {
 }  // namespace
 
 int regtopk_norm_gave_up(cudaStream_t s);  // dropout_norm.cu's
+int regtopk_rms_gave_up(cudaStream_t s);   // rms_norm.cu's
 #endif
