@@ -11,15 +11,13 @@ namespace {
 constexpr int kActThreads = 256;
 
 // ---- f(x) = x p(x) and its slope ---------------------------------------------------------------------------------
-// exp and 1 / (1 + t), t in [0, 1].  FAST, for 16-bit types: the hardware's approximations, off by 2^-20 where they matter.
-template <bool FAST> __device__ __forceinline__ float exp_of(float x) { return FAST ? __expf(x) : expf(x); }
-template <bool FAST> __device__ __forceinline__ float over(float t) { return FAST ? __fdividef(1.0f, t) : 1.0f / t; }
+// FAST, for 16-bit types: exponentials and reciprocals are the hardware's approximations, which are off by 2^-20 where that matters.
 
-// p = 1 / (1 + exp(-x)) and q = 1 - p, both from exp(-|x|), so that neither overflows nor cancels.
+// p = 1 / (1 + exp(-x)) and q = 1 - p, without cancellation; an infinite exponential gives 0 and 1.
 template <bool FAST> __device__ __forceinline__ void logistic(float x, float& p, float& q) {
-  const float t = exp_of<FAST>(-fabsf(x)), r = over<FAST>(1.0f + t), s = t * r;
-  p = x >= 0.0f ? r : s;
-  q = x >= 0.0f ? s : r;
+  const float e = FAST ? exp2_fast(-kLog2E * x) : expf(-x);
+  p = FAST ? reciprocal_fast(1.0f + e) : 1.0f / (1.0f + e);
+  q = FAST || x < 0.0f ? 1.0f - p : e * p;  // what 1 - p loses for large x is 2^-23 x, x at most 17, where p is not 1
 }
 
 // f(x) = x p; slope: f'(x) too.
@@ -34,16 +32,16 @@ template <int KIND, bool FAST> __device__ __forceinline__ float activate(float x
     logistic<FAST>(c * fmaf(0.044715f * w2, w, w), p, q);
     if (slope) *slope = fmaf(x * (p * q), c * fmaf(0.134145f, w2, 1.0f), p);
   } else {
-    const float e = exp_of<FAST>(-0.5f * x * x);
+    const float e = FAST ? exp2_fast(-0.5f * kLog2E * x * x) : expf(-0.5f * x * x);
     if (FAST) {
       // Phi(-|x|) by approximation 7.1.26 of Abramowitz and Stegun (Hastings), off by 7.5e-8: six terms and one exponential that
       // the slope needs anyway.
-      const float t = over<true>(fmaf(0.23164189f, fabsf(x), 1.0f));
-      float h = fmaf(1.061405429f, t, -1.453152027f);
-      h = fmaf(h, t, 1.421413741f);
-      h = fmaf(h, t, -0.284496736f);
-      h = fmaf(h, t, 0.254829592f);
-      h = 0.5f * h * t * e;
+      const float t = reciprocal_fast(fmaf(0.23164189f, fabsf(x), 1.0f));
+      float h = fmaf(0.5f * 1.061405429f, t, -0.5f * 1.453152027f);
+      h = fmaf(h, t, 0.5f * 1.421413741f);
+      h = fmaf(h, t, -0.5f * 0.284496736f);
+      h = fmaf(h, t, 0.5f * 0.254829592f);
+      h = h * t * e;
       p = x >= 0.0f ? 1.0f - h : h;
     } else {
       // erfc(z + r), r what z = -x / sqrt(2) has lost by rounding: without it p is off by z^2 units of 2^-22
@@ -55,27 +53,32 @@ template <int KIND, bool FAST> __device__ __forceinline__ float activate(float x
   return x * p;
 }
 
-// ---- where a thread's eight columns lie ----------------------------------------------------------------------------
-// VEC: rows are aligned and have a multiple of eight columns; a thread has eight neighbours, four threads a block of 32, and
-// the threads go through all rows' blocks one after the other.  Otherwise a warp has 256 columns of a row, and each lane every 32nd.
+// ---- where a thread's columns lie ------------------------------------------------------------------------------------
+// VEC: rows are aligned and have a multiple of eight columns; a thread has kActStep times eight neighbours, four threads share a block
+// of 32, and the threads go through all rows' blocks one after the other.  Otherwise a warp has 256 columns of a row, every 32nd a
+// lane's.
 struct Layout {
   int64_t cols, row0;  // row0: where this launch begins
-  Divisor pieces;      // of a row: threads (VEC) or warps
+  Divisor pieces;      // of a row: groups of eight columns (VEC), or of 256
   u32 total;           // of this launch, fewer than 2^31
 };
+constexpr int kActStep = 2;
+
 template <bool VEC> struct Spot {
-  int64_t row, c0;
-  int lane;
+  int64_t row;
+  int c0;
   bool there;
-  __device__ __forceinline__ Spot(const Layout& l) {
-    const u32 at = blockIdx.x * (VEC ? kActThreads : kActThreads / 32) + (VEC ? threadIdx.x : threadIdx.x >> 5);
+  __device__ __forceinline__ Spot(const Layout& l, u32 at) {
     const u32 r = l.pieces.quotient_of(at);
-    there = at < l.total;
-    row = l.row0 + (there ? r : 0);
-    c0 = (int64_t)(at - r * l.pieces.d) * (VEC ? 8 : 256);
-    lane = VEC ? 0 : threadIdx.x & 31;
+    c0 = (int)(at - r * l.pieces.d) * (VEC ? 8 : 256);
+    there = at < l.total && c0 < (int)l.cols;
+    row = l.row0 + (at < l.total ? r : 0);
   }
 };
+template <bool VEC> __device__ __forceinline__ u32 first_piece() {
+  return VEC ? blockIdx.x * (kActThreads * kActStep) + threadIdx.x : blockIdx.x * (kActThreads / 32) + (threadIdx.x >> 5);
+}
+
 // ---- kernels -------------------------------------------------------------------------------------------------------
 struct ActArgs {
   Layout at;
@@ -86,86 +89,210 @@ struct ActArgs {
   int64_t lda, ldy, ld_dy, ld_da, ld_in_scales, ld_values, ld_scales, half_blocks;
 };
 
-template <typename T, int KIND, bool GATED, bool VEC>
-__global__ void __launch_bounds__(kActThreads) k_activation(const __grid_constant__ ActArgs a) {
-  begin_after_predecessor();
-  const Spot<VEC> at(a.at);
-  const int64_t cols = at.there ? a.at.cols : 0;
-  const T* row = static_cast<const T*>(a.a) + at.row * a.lda;
-  Octet x, u;
-  read_eight<T, VEC, false>(x, row, at.c0, at.lane, cols);
-  if (GATED) read_eight<T, VEC, false>(u, row + a.at.cols, at.c0, at.lane, cols);
-  if (a.values) {
-    uint8_t *values = a.values + at.row * a.ld_values, *scales = a.scales + at.row * a.ld_scales;
-    store_rows8<VEC>(x, values, scales, at.c0, at.lane, cols);
-    if (GATED) store_rows8<VEC>(u, values + a.at.cols, scales + a.half_blocks, at.c0, at.lane, cols);
-  }
+template <typename T, int KIND, bool GATED> __device__ __forceinline__ void forward_of(Octet& x, const Octet& u) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[i] = make_float2(activate<KIND, sizeof(T) == 2>(x[i].x, nullptr), activate<KIND, sizeof(T) == 2>(x[i].y, nullptr));
     if (GATED) x[i] = mul2(x[i], u[i]);
   }
-  store_eight<T, VEC>(x, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, at.lane, cols);
+}
+
+template <typename T, int KIND, bool GATED, bool VEC>
+__global__ void __launch_bounds__(kActThreads) k_activation(const __grid_constant__ ActArgs a) {
+  begin_after_predecessor();
+  const int cols = (int)a.at.cols;
+  if constexpr (VEC) {
+    Eight<T> x[kActStep], u[kActStep];
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      const T* from = static_cast<const T*>(a.a) + at.row * a.lda + at.c0;
+      x[n].clear();
+      u[n].clear();
+      if (at.there) x[n].fetch(from);
+      if (GATED && at.there) u[n].fetch(from + cols);
+    }
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      Octet f, g;
+      x[n].get(f);
+      u[n].get(g);
+      if (a.values) {
+        uint8_t *values = a.values + at.row * a.ld_values + at.c0, *scales = a.scales + at.row * a.ld_scales + (at.c0 >> 5);
+        store_rows8(f, values, scales, at.there);
+        if (GATED) store_rows8(g, values + cols, scales + a.half_blocks, at.there);
+      }
+      forward_of<T, KIND, GATED>(f, g);
+      x[n].put(f);
+      if (at.there) x[n].store(static_cast<T*>(a.y) + at.row * a.ldy + at.c0);
+    }
+  } else {
+    const Spot<false> at(a.at, first_piece<false>());
+    const int lane = threadIdx.x & 31;
+    if (!at.there) return;
+    const T* row = static_cast<const T*>(a.a) + at.row * a.lda;
+    Octet x, u;
+    read_eight<T, false, false>(x, row, at.c0, lane, cols);
+    if (GATED) read_eight<T, false, false>(u, row + cols, at.c0, lane, cols);
+    if (a.values) {
+      uint8_t *values = a.values + at.row * a.ld_values, *scales = a.scales + at.row * a.ld_scales;
+      store_rows8_apart(x, values, scales, at.c0, lane, cols);
+      if (GATED) store_rows8_apart(u, values + cols, scales + a.half_blocks, at.c0, lane, cols);
+    }
+    forward_of<T, KIND, GATED>(x, u);
+    store_eight<T, false>(x, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, lane, cols);
+  }
+}
+
+// x and u become the gradients to the halves, d the output.
+template <typename T, int KIND, bool GATED> __device__ __forceinline__ void backward_of(Octet& x, Octet& u, Octet& d) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2 slope, f = make_float2(activate<KIND, sizeof(T) == 2>(x[i].x, &slope.x), activate<KIND, sizeof(T) == 2>(x[i].y, &slope.y));
+    x[i] = mul2(slope, d[i]);
+    if (GATED) {
+      const float2 up = u[i];
+      x[i] = mul2(x[i], up);
+      u[i] = mul2(d[i], f);
+      d[i] = mul2(up, f);
+    } else {
+      d[i] = f;
+    }
+  }
 }
 
 template <typename T, int KIND, bool GATED, bool KEPT8, bool VEC>
 __global__ void __launch_bounds__(kActThreads) k_activation_back(const __grid_constant__ ActArgs a) {
   begin_after_predecessor();
-  const Spot<VEC> at(a.at);
-  const int64_t cols = at.there ? a.at.cols : 0;
+  const int cols = (int)a.at.cols;
   Octet d, x, u;
-  if (KEPT8) {
-    const uint8_t *row = static_cast<const uint8_t*>(a.a) + at.row * a.lda, *scales = a.in_scales + at.row * a.ld_in_scales;
-    read_rows8<VEC>(x, row, scales, at.c0, at.lane, cols);
-    if (GATED) read_rows8<VEC>(u, row + a.at.cols, scales + a.half_blocks, at.c0, at.lane, cols);
-  } else {
-    const T* row = static_cast<const T*>(a.a) + at.row * a.lda;
-    read_eight<T, VEC, false>(x, row, at.c0, at.lane, cols);
-    if (GATED) read_eight<T, VEC, false>(u, row + a.at.cols, at.c0, at.lane, cols);
-  }
-  read_eight<T, VEC, false>(d, static_cast<const T*>(a.dy) + at.row * a.ld_dy, at.c0, at.lane, cols);
-  Octet slope;
+  if constexpr (VEC) {
+    Eight<T> in[kActStep], wide_x[KEPT8 ? 1 : kActStep], wide_u[KEPT8 ? 1 : kActStep];
+    Packed8 packed_x[KEPT8 ? kActStep : 1], packed_u[KEPT8 ? kActStep : 1];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    x[i] = make_float2(activate<KIND, sizeof(T) == 2>(x[i].x, &slope[i].x), activate<KIND, sizeof(T) == 2>(x[i].y, &slope[i].y));
-  T* da = static_cast<T*>(a.da) + at.row * a.ld_da;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    slope[i] = mul2(slope[i], d[i]);
-    if (GATED) {
-      slope[i] = mul2(slope[i], u[i]);
-      u[i] = mul2(u[i], x[i]);  // the output
-      d[i] = mul2(d[i], x[i]);  // the gradient to the second half
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      if (KEPT8) {
+        const uint8_t *from = static_cast<const uint8_t*>(a.a) + at.row * a.lda + at.c0, *scales = a.in_scales + at.row * a.ld_in_scales + (at.c0 >> 5);
+        packed_x[n].clear();
+        packed_u[n].clear();
+        if (at.there) packed_x[n].fetch(from, scales);
+        if (GATED && at.there) packed_u[n].fetch(from + cols, scales + a.half_blocks);
+      } else {
+        const T* from = static_cast<const T*>(a.a) + at.row * a.lda + at.c0;
+        wide_x[n].clear();
+        wide_u[n].clear();
+        if (at.there) wide_x[n].fetch(from);
+        if (GATED && at.there) wide_u[n].fetch(from + cols);
+      }
+      in[n].clear();
+      if (at.there) in[n].fetch(static_cast<const T*>(a.dy) + at.row * a.ld_dy + at.c0);
     }
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      in[n].get(d);
+      if (KEPT8) {
+        packed_x[n].get(x);
+        if (GATED) packed_u[n].get(u);
+      } else {
+        wide_x[n].get(x);
+        if (GATED) wide_u[n].get(u);
+      }
+      backward_of<T, KIND, GATED>(x, u, d);
+      if (!at.there) continue;
+      T* da = static_cast<T*>(a.da) + at.row * a.ld_da + at.c0;
+      in[n].put(x);
+      in[n].store(da);
+      if (GATED) {
+        in[n].put(u);
+        in[n].store(da + cols);
+      }
+      if (a.y) {
+        in[n].put(d);
+        in[n].store(static_cast<T*>(a.y) + at.row * a.ldy + at.c0);
+      }
+    }
+  } else {
+    const Spot<false> at(a.at, first_piece<false>());
+    const int lane = threadIdx.x & 31;
+    if (!at.there) return;
+    if (KEPT8) {
+      const uint8_t *row = static_cast<const uint8_t*>(a.a) + at.row * a.lda, *scales = a.in_scales + at.row * a.ld_in_scales;
+      read_rows8_apart(x, row, scales, at.c0, lane, cols);
+      if (GATED) read_rows8_apart(u, row + cols, scales + a.half_blocks, at.c0, lane, cols);
+    } else {
+      const T* row = static_cast<const T*>(a.a) + at.row * a.lda;
+      read_eight<T, false, false>(x, row, at.c0, lane, cols);
+      if (GATED) read_eight<T, false, false>(u, row + cols, at.c0, lane, cols);
+    }
+    read_eight<T, false, false>(d, static_cast<const T*>(a.dy) + at.row * a.ld_dy, at.c0, lane, cols);
+    backward_of<T, KIND, GATED>(x, u, d);
+    T* da = static_cast<T*>(a.da) + at.row * a.ld_da;
+    store_eight<T, false>(x, da, at.c0, lane, cols);
+    if (GATED) store_eight<T, false>(u, da + cols, at.c0, lane, cols);
+    if (a.y) store_eight<T, false>(d, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, lane, cols);
   }
-  store_eight<T, VEC>(slope, da, at.c0, at.lane, cols);
-  if (GATED) store_eight<T, VEC>(d, da + a.at.cols, at.c0, at.lane, cols);
-  if (a.y) store_eight<T, VEC>(GATED ? u : x, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, at.lane, cols);
 }
 
 template <typename T, bool VEC> __global__ void __launch_bounds__(kActThreads) k_pack8(const __grid_constant__ ActArgs a) {
   begin_after_predecessor();
-  const Spot<VEC> at(a.at);
-  const int64_t cols = at.there ? a.at.cols : 0;
-  Octet x;
-  read_eight<T, VEC, false>(x, static_cast<const T*>(a.a) + at.row * a.lda, at.c0, at.lane, cols);
-  store_rows8<VEC>(x, a.values + at.row * a.ld_values, a.scales + at.row * a.ld_scales, at.c0, at.lane, cols);
+  Octet f;
+  if constexpr (VEC) {
+    Eight<T> x[kActStep];
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      x[n].clear();
+      if (at.there) x[n].fetch(static_cast<const T*>(a.a) + at.row * a.lda + at.c0);
+    }
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      x[n].get(f);
+      store_rows8(f, a.values + at.row * a.ld_values + at.c0, a.scales + at.row * a.ld_scales + (at.c0 >> 5), at.there);
+    }
+  } else {
+    const Spot<false> at(a.at, first_piece<false>());
+    if (!at.there) return;
+    read_eight<T, false, false>(f, static_cast<const T*>(a.a) + at.row * a.lda, at.c0, threadIdx.x & 31, (int)a.at.cols);
+    store_rows8_apart(f, a.values + at.row * a.ld_values, a.scales + at.row * a.ld_scales, at.c0, threadIdx.x & 31, (int)a.at.cols);
+  }
 }
 
 template <typename T, bool VEC> __global__ void __launch_bounds__(kActThreads) k_unpack8(const __grid_constant__ ActArgs a) {
   begin_after_predecessor();
-  const Spot<VEC> at(a.at);
-  const int64_t cols = at.there ? a.at.cols : 0;
-  Octet x;
-  read_rows8<VEC>(x, static_cast<const uint8_t*>(a.a) + at.row * a.lda, a.in_scales + at.row * a.ld_in_scales, at.c0, at.lane, cols);
-  store_eight<T, VEC>(x, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, at.lane, cols);
+  Octet f;
+  if constexpr (VEC) {
+    Packed8 v[kActStep];
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      v[n].clear();
+      if (at.there) v[n].fetch(static_cast<const uint8_t*>(a.a) + at.row * a.lda + at.c0, a.in_scales + at.row * a.ld_in_scales + (at.c0 >> 5));
+    }
+#pragma unroll
+    for (int n = 0; n < kActStep; ++n) {
+      const Spot<true> at(a.at, first_piece<true>() + n * kActThreads);
+      v[n].get(f);
+      Eight<T> x;
+      x.put(f);
+      if (at.there) x.store(static_cast<T*>(a.y) + at.row * a.ldy + at.c0);
+    }
+  } else {
+    const Spot<false> at(a.at, first_piece<false>());
+    if (!at.there) return;
+    read_rows8_apart(f, static_cast<const uint8_t*>(a.a) + at.row * a.lda, a.in_scales + at.row * a.ld_in_scales, at.c0, threadIdx.x & 31, (int)a.at.cols);
+    store_eight<T, false>(f, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, threadIdx.x & 31, (int)a.at.cols);
+  }
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
 // `launch` for as many rows at a time as have fewer than 2^31 pieces.
 template <typename Launch> int in_parts(ActArgs a, bool vec, int64_t rows, int64_t cols, const Launch& launch) {
-  const int64_t pieces = vec ? 4 * blocks_of(cols) : (cols + 255) / 256, most = (((int64_t)1 << 31) - kActThreads) / pieces;
-  const u32 per = vec ? kActThreads : kActThreads / 32;
+  const int64_t pieces = vec ? 4 * blocks_of(cols) : (cols + 255) / 256, most = (((int64_t)1 << 31) - kActThreads * kActStep) / pieces;
+  const u32 per = vec ? kActThreads * kActStep : kActThreads / 32;
   a.at.cols = cols;
   a.at.pieces = divisor(pieces);
   for (a.at.row0 = 0; a.at.row0 < rows; a.at.row0 += most) {

@@ -184,6 +184,23 @@ std::pair<Tensor, Tensor> two_of(at::IntArrayRef size, const Tensor& like) {
   };
   return {part(0), part(n)};
 }
+// The same for two tensors of any sizes and types; the second begins at a multiple of 16 bytes.
+std::pair<Tensor, Tensor> two_of(at::IntArrayRef size, at::ScalarType type, at::IntArrayRef other_size, at::ScalarType other_type, const Tensor& like) {
+  const auto bytes_of = [](at::IntArrayRef s, at::ScalarType t) {
+    int64_t n = static_cast<int64_t>(c10::elementSize(t));
+    for (const int64_t i : s) n *= i;
+    return n;
+  };
+  const int64_t second = (bytes_of(size, type) + 15) & ~int64_t(15);
+  const Tensor whole = empty({second + bytes_of(other_size, other_type)}, at::kByte, like);
+  const auto part = [&](at::IntArrayRef s, at::ScalarType t, int64_t at) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), c10::scalarTypeToTypeMeta(t));
+    impl->set_storage_offset(at / static_cast<int64_t>(c10::elementSize(t)));
+    impl->set_sizes_contiguous(s);
+    return Tensor(std::move(impl));
+  };
+  return {part(size, type, 0), part(other_size, other_type, second)};
+}
 void* stream_of(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.device().index()).stream(); }
 void* data(const Tensor* t) { return t ? t->data_ptr() : nullptr; }
 

@@ -55,7 +55,8 @@ NewPacked new_packed(at::IntArrayRef sizes, const Tensor& like, int halves) {
   std::vector<int64_t> s(sizes.begin(), sizes.end());
   const int64_t cols = s.back(), blocks = halves * blocks_of(cols / halves);
   s.back() = blocks;
-  return {empty(sizes, at::kFloat8_e4m3fn, like), empty(s, at::kFloat8_e8m0fnu, like), cols, blocks};
+  auto [v, e] = two_of(sizes, at::kFloat8_e4m3fn, s, at::kFloat8_e8m0fnu, like);
+  return {std::move(v), std::move(e), cols, blocks};
 }
 
 // [..., k] values of one 32-bit type, contiguous, on x's device.
@@ -133,7 +134,7 @@ PyObject* route(PyObject* const* a) {  // logits, k, scores, bias, groups, group
   if (!(p.scale - p.scale == 0.0f)) value_error("scale is a finite float32 number");
   const c10::cuda::CUDAGuard guard(logits.device());
   const std::vector<int64_t> size = with_cols(logits.sizes(), k);
-  const Tensor experts = empty(size, at::kInt, logits), weights = empty(size, at::kFloat, logits);
+  const auto [experts, weights] = two_of(size, at::kInt, size, at::kFloat, logits);
   check(regtopk_route(logits.data_ptr(), in.ld, static_cast<const float*>(data(bias)), static_cast<int32_t*>(experts.data_ptr()),
                       static_cast<float*>(weights.data_ptr()), in.rows, most, k, type, &p, stream_of(logits)), "regtopk_route");
   return Py_BuildValue("NN", THPVariable_Wrap(experts), THPVariable_Wrap(weights));
@@ -169,7 +170,7 @@ PyObject* sort_tokens(PyObject* const* a) {  // experts, n_experts, workers
   const int64_t tokens = tokens_of(experts);
   if (static_cast<int64_t>(n) * workers > REGTOPK_MATMUL_MAX_GROUPS) check(REGTOPK_ERR_TOO_LARGE, "regtopk_sort_tokens");
   const c10::cuda::CUDAGuard guard(experts.device());
-  const Tensor offsets = empty({static_cast<int64_t>(n) * workers + 1}, at::kLong, experts), place = empty(experts.sizes(), at::kInt, experts);
+  const auto [offsets, place] = two_of({static_cast<int64_t>(n) * workers + 1}, at::kLong, experts.sizes(), at::kInt, experts);
   const size_t bytes = regtopk_sort_tokens_workspace_bytes(tokens, k, n, workers);
   Tensor ws;
   if (bytes) ws = empty({static_cast<int64_t>(bytes)}, at::kByte, experts);

@@ -49,15 +49,15 @@ template <typename T, bool VEC> __device__ __forceinline__ void clear_tail(const
 
 // Which token and which of its columns: VEC: a thread has eight neighbours; otherwise a warp has 256 columns.
 template <bool VEC> struct Piece {
-  int64_t token, c0;
-  int lane;
+  int64_t token;
+  int c0, lane;
   bool there;
   __device__ __forceinline__ Piece(const MoveArgs& a) {
     const u32 at = blockIdx.x * (VEC ? kMoveThreads : kMoveWarps) + (VEC ? threadIdx.x : threadIdx.x >> 5);
     const u32 r = a.pieces.quotient_of(at);
     there = at < a.total;
     token = r;
-    c0 = (int64_t)(at - r * a.pieces.d) * (VEC ? 8 : 256);
+    c0 = (int)(at - r * a.pieces.d) * (VEC ? 8 : 256);
     lane = VEC ? 0 : threadIdx.x & 31;
   }
 };
@@ -66,19 +66,25 @@ template <typename T, bool PACKED, bool VEC> __global__ void __launch_bounds__(k
   begin_after_predecessor();
   const Piece<VEC> at(a);
   if (at.there) {
+    const int cols = (int)a.cols;
     Octet f;
     Eight<T> v;
-    if (PACKED) read_rows8<VEC>(f, static_cast<const uint8_t*>(a.in) + at.token * a.ld_in, a.in_scales + at.token * a.ld_scales, at.c0, at.lane, a.cols);
-    else if (VEC) v.fetch(static_cast<const T*>(a.in) + at.token * a.ld_in + at.c0);
-    else read_eight<T, VEC, false>(f, static_cast<const T*>(a.in) + at.token * a.ld_in, at.c0, at.lane, a.cols);
-    if (PACKED && VEC) v.put(f);
+    if (PACKED && VEC) {
+      Packed8 p;
+      p.fetch(static_cast<const uint8_t*>(a.in) + at.token * a.ld_in + at.c0, a.in_scales + at.token * a.ld_scales + (at.c0 >> 5));
+      p.get(f);
+      v.put(f);
+    } else if (PACKED) {
+      read_rows8_apart(f, static_cast<const uint8_t*>(a.in) + at.token * a.ld_in, a.in_scales + at.token * a.ld_scales, at.c0, at.lane, cols);
+    } else if (VEC) v.fetch(static_cast<const T*>(a.in) + at.token * a.ld_in + at.c0);
+    else read_eight<T, VEC, false>(f, static_cast<const T*>(a.in) + at.token * a.ld_in, at.c0, at.lane, cols);
     const int32_t* place = a.place + at.token * a.k;
     for (int j = 0; j < a.k; ++j) {
       const int32_t p = place[j];
       if (!in_rows(p, a.rows)) continue;
       T* to = static_cast<T*>(a.out) + (int64_t)p * a.ld_out;
       if (VEC) v.store(to + at.c0);
-      else store_eight<T, VEC>(f, to, at.c0, at.lane, a.cols);
+      else store_eight<T, VEC>(f, to, at.c0, at.lane, cols);
     }
   }
   clear_tail<T, VEC>(a);
@@ -90,6 +96,7 @@ template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kM
   begin_after_predecessor();
   const Piece<VEC> at(a);
   if (!at.there) return;
+  const int cols = (int)a.cols;
   const int32_t* place = a.place + at.token * a.k;
   const float* weights = a.weights + at.token * a.k;
   Octet sum;
@@ -107,7 +114,7 @@ template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kM
 #pragma unroll
     for (int j = 0; j < kJoinStep; ++j) {
       const bool there = in_rows(p[j], a.rows);
-      read_eight<T, VEC, false>(f[j], static_cast<const T*>(a.in) + (there ? (int64_t)p[j] * a.ld_in : 0), at.c0, at.lane, there ? a.cols : 0);
+      read_eight<T, VEC, false>(f[j], static_cast<const T*>(a.in) + (there ? (int64_t)p[j] * a.ld_in : 0), at.c0, at.lane, there ? cols : 0);
       if (!there) w[j] = 0.0f;
     }
 #pragma unroll
@@ -117,64 +124,67 @@ template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kM
   }
   if (a.other) {
     Octet r;
-    read_eight<O, VEC, false>(r, static_cast<const O*>(a.other) + at.token * a.ld_other, at.c0, at.lane, a.cols);
+    read_eight<O, VEC, false>(r, static_cast<const O*>(a.other) + at.token * a.ld_other, at.c0, at.lane, cols);
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = add2(sum[i], r[i]);
   }
-  store_eight<O, VEC>(sum, static_cast<O*>(a.out) + at.token * a.ld_out, at.c0, at.lane, a.cols);
+  store_eight<O, VEC>(sum, static_cast<O*>(a.out) + at.token * a.ld_out, at.c0, at.lane, cols);
 }
 
-// A team of warps a token: its warps share the row's units of 256 columns, and each keeps the products of eight of the token's rows
-// with dout under way.
-constexpr int kBackStep = 8;
-template <typename T, typename D, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_join_back(const __grid_constant__ MoveArgs a) {
-  __shared__ float part[kMoveWarps][kBackStep];
+// A team of warps a token: its warps share the row's units of 256 columns, and each has STEP of the token's rows under way beside
+// dout.
+template <typename T, typename D, bool VEC, int STEP> __global__ void __launch_bounds__(kMoveThreads) k_join_back(const __grid_constant__ MoveArgs a) {
+  __shared__ float part[kMoveWarps][STEP];
   begin_after_predecessor();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, member = warp % a.team, teams = kMoveWarps / a.team;
   const int64_t t = (int64_t)blockIdx.x * teams + warp / a.team;
   const bool there = t < a.tokens;
-  for (int j0 = 0; j0 < a.k; j0 += kBackStep) {
-    int32_t p[kBackStep];
-    float w[kBackStep], dot[kBackStep];
+  for (int j0 = 0; j0 < a.k; j0 += STEP) {
+    int64_t to[STEP];  // where each row is, -1: nowhere
+    float w[STEP], dot[STEP];
 #pragma unroll
-    for (int j = 0; j < kBackStep; ++j) {
-      p[j] = there && j0 + j < a.k ? a.place[t * a.k + j0 + j] : -1;
-      w[j] = there && j0 + j < a.k ? a.weights[t * a.k + j0 + j] : 0.0f;
+    for (int j = 0; j < STEP; ++j) {
+      const bool used = there && j0 + j < a.k;
+      const int32_t p = used ? a.place[t * a.k + j0 + j] : -1;
+      to[j] = in_rows(p, a.rows) ? p : -1;
+      w[j] = used ? a.weights[t * a.k + j0 + j] : 0.0f;
       dot[j] = 0.0f;
     }
     if (there) {
-      for (int64_t c0 = member * 256; c0 < a.cols; c0 += a.team * 256) {
-        Octet d;
-        read_eight<D, VEC, false>(d, static_cast<const D*>(a.in) + t * a.ld_in, c0, lane, a.cols);
+      for (int c0 = member * 256; c0 < a.cols; c0 += a.team * 256) {
+        const int cols = (int)a.cols;
+        Octet d, f[STEP];
+        read_eight<D, VEC, false>(d, static_cast<const D*>(a.in) + t * a.ld_in, c0, lane, cols);
 #pragma unroll
-        for (int j = 0; j < kBackStep; ++j) {
-          if (!in_rows(p[j], a.rows)) continue;
-          Octet f;
-          read_eight<T, VEC, false>(f, static_cast<const T*>(a.other) + (int64_t)p[j] * a.ld_other, c0, lane, a.cols);
+        for (int j = 0; j < STEP; ++j) read_eight<T, VEC, false>(f[j], static_cast<const T*>(a.other) + (to[j] < 0 ? 0 : to[j]) * a.ld_other, c0, lane, to[j] < 0 ? 0 : cols);
+#pragma unroll
+        for (int j = 0; j < STEP; ++j) {
           float2 s = both(0.0f);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            s = fma2(f[i], d[i], s);
-            f[i] = mul2(d[i], both(w[j]));
+            s = fma2(f[j][i], d[i], s);
+            f[j][i] = mul2(d[i], both(w[j]));
           }
+          if (to[j] < 0) continue;
           dot[j] += s.x + s.y;
-          store_eight<T, VEC>(f, static_cast<T*>(a.out) + (int64_t)p[j] * a.ld_out, c0, lane, a.cols);
+          store_eight<T, VEC>(f[j], static_cast<T*>(a.out) + to[j] * a.ld_out, c0, lane, cols);
         }
       }
     }
 #pragma unroll
-    for (int j = 0; j < kBackStep; ++j) {
-      if (j0 + j >= a.k) break;
+    for (int j = 0; j < STEP; ++j) {
       const float s = warp_sum(dot[j]);
       if (lane == 0) part[warp][j] = s;
     }
-    __syncthreads();
-    if (member == 0 && lane < kBackStep && there && j0 + lane < a.k) {
+    if (a.team > 1) __syncthreads();
+    else __syncwarp();
+    if (member == 0 && lane < STEP && there && j0 + lane < a.k) {
       float s = 0.0f;
       for (int i = 0; i < a.team; ++i) s += part[warp + i][lane];
       a.dweights[t * a.k + j0 + lane] = s;
     }
-    __syncthreads();
+    if (a.team > 1) __syncthreads();
+    else __syncwarp();
   }
   clear_tail<T, VEC>(a);
 }
@@ -204,6 +214,14 @@ template <typename Launch> int in_parts(MoveArgs a, bool vec, size_t in_size, si
     a.out = static_cast<char*>(a.out) + a.tokens * a.ld_out * (int64_t)out_size;
   } while (done < tokens);
   return REGTOPK_OK;
+}
+
+template <typename T, typename D, int STEP> int launch_join_back_step(const MoveArgs& a, bool vec, unsigned grid, cudaStream_t s) {
+  return vec ? start(k_join_back<T, D, true, STEP>, grid, kMoveThreads, 0, s, a) : start(k_join_back<T, D, false, STEP>, grid, kMoveThreads, 0, s, a);
+}
+template <typename T, typename D> int launch_join_back(const MoveArgs& a, bool vec, unsigned grid, cudaStream_t s) {
+  return a.k == 1 ? launch_join_back_step<T, D, 1>(a, vec, grid, s) : a.k == 2 ? launch_join_back_step<T, D, 2>(a, vec, grid, s)
+                                                                               : launch_join_back_step<T, D, 4>(a, vec, grid, s);
 }
 
 inline bool bad_shape(int64_t tokens, int32_t k, int64_t rows, int64_t cols) {
@@ -292,14 +310,13 @@ int regtopk_join_tokens_backward(const void* dout, int64_t ld_dout, const void* 
   a.in = dout; a.ld_in = ld_dout; a.other = from; a.ld_other = ld_from; a.place = place; a.weights = weights; a.filled = filled;
   a.out = dfrom; a.ld_out = ld_dfrom; a.dweights = dweights; a.tokens = tokens; a.rows = cols ? rows : 0; a.cols = cols; a.k = k; a.clears = true;
   const bool vec = cols % 8 == 0 && rows_aligned(dout, ld_dout, dsize, tokens) && rows_aligned(from, ld_from, size, rows) && rows_aligned(dfrom, ld_dfrom, size, rows);
-  // As many warps a token as it has units, while that leaves fewer than 16 warps for an SM.
+  // As many warps a token as it has units, while that makes no more than four times the warps that the device holds at once.
   const int64_t units = (cols + 255) / 256;
   a.team = 1;
-  while (a.team < kMoveWarps && a.team < units && tokens * a.team < (int64_t)sms * 16) a.team *= 2;
+  while (a.team < kMoveWarps && a.team < units && tokens * a.team * 2 <= (int64_t)sms * 32 * 4) a.team *= 2;
   const int64_t teams = kMoveWarps / a.team, blocks = tokens ? (tokens + teams - 1) / teams : 1;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-#define REGTOPK_JOIN_BACK(T, D) \
-  (vec ? start(k_join_back<T, D, true>, (unsigned)blocks, kMoveThreads, 0, s, a) : start(k_join_back<T, D, false>, (unsigned)blocks, kMoveThreads, 0, s, a))
+#define REGTOPK_JOIN_BACK(T, D) launch_join_back<T, D>(a, vec, (unsigned)blocks, s)
   return REGTOPK_BY_TYPES(REGTOPK_JOIN_BACK, dout_type);
 #undef REGTOPK_JOIN_BACK
 }

@@ -77,7 +77,11 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_rms(const __grid_constant__ Rms
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[u][i] = mul2(mul2(f[u][i], both(rstd)), w[i]);
       if (a.y) store_eight<T, VEC>(f[u], static_cast<T*>(a.y) + row * a.ldy, c0, t.lane, a.cols);
-      if (a.values) store_rows8<VEC>(f[u], a.values + row * a.ld_values, a.scales + row * a.ld_scales, c0, t.lane, a.cols);
+      if (a.values) {
+        uint8_t *values = a.values + row * a.ld_values, *scales = a.scales + row * a.ld_scales;
+        if (VEC) store_rows8(f[u], values + c0 + t.lane * 8, scales + ((c0 + t.lane * 8) >> 5), c0 + t.lane * 8 < a.cols);
+        else store_rows8_apart(f[u], values, scales, c0, t.lane, a.cols);
+      }
     }
   }
 }
@@ -384,7 +388,7 @@ int regtopk_rms_norm_backward(const void* dy, int64_t ld_dy, const void* h, int6
     a.rstd = rstd; a.weight = weight; a.dx = dx; a.dres = dresidual; a.ld_dx = ld_dx; a.ld_dres = ld_dresidual;
     a.rows = rows; a.cols = (int)cols; a.wide = (uintptr_t)weight % 16 == 0; a.groups = groups; a.offsets = offsets;
     a.partial = dweight ? static_cast<float*>(workspace) : nullptr;
-    const Plan p = plan_of(cols, rows, {size, ssize, dh ? ssize : 0}, size + ssize == 4 ? 4 : 2, 2, 1, 1, sms);
+    const Plan p = plan_of(cols, rows, {size, ssize, dh ? ssize : 0}, 2, 2, 1, 1, sms);
     a.ring = p.ring;
     const int64_t blocks = (int64_t)sms * (p.blocks < 4 ? p.blocks : 4), turns = (rows + blocks * p.ring.teams - 1) / (blocks * p.ring.teams);
     a.block_rows = turns * p.ring.teams;

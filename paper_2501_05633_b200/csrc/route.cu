@@ -23,15 +23,18 @@ struct RouteArgs {
   int lanes_log2, lanes, each;    // lanes of a group, experts of a lane (at most the template's N)
   int wide;                       // every lane has N neighbours, aligned, or none
   int sigmoid, renormalise;
+  int places_log2, batch, share;  // places for a token's experts in a warp's lanes, at least k; tokens that a warp finishes together, and in all
   float scale;
 };
 
-// Binary32 numbers as whole numbers of the same order (-0 as +0).  0 is left for what cannot be chosen, and NaN is below all numbers.
+// Binary32 numbers as whole numbers of the same order.  The number is canonical: no -0, and a NaN positive, as after an addition.
 __device__ __forceinline__ u32 ordered(float v) {
-  const u32 b = __float_as_uint(v + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const u32 b = __float_as_uint(v);
+  return b ^ ((u32)((int)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float unordered(u32 o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ float unordered(u32 o) { return __uint_as_float(o ^ ((u32)((int)~o >> 31) | 0x80000000u)); }
+constexpr u32 kNone = 0x007FFFFFu;      // -infinity, with all low bits set: this and what is below is no expert
+constexpr u32 kInfinite = 0xFF800000u;  // +infinity; NaN is above
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -76,17 +79,43 @@ template <typename T, int N> __device__ __forceinline__ void read_logits(float (
   }
 }
 
-// The choice in binary64, for the few tokens whose numbers lie too close for binary32: into slots[0 .. k), as many as it returns.
-// `by_logit`: the experts are compared by their logits, which are exact.
+// The weights of the experts chosen, one a lane and `places` lanes a token, as shares: exp(l) (softmax) or 1 / (1 + exp(-l)) over their
+// sum.  Everything is taken relative to the largest, so that no sum is 0 whatever the logits.
+__device__ __forceinline__ float share_of(float l, bool there, bool sigmoid, int places) {
+  float most = there ? l : -INFINITY, v;
+  for (int o = 1; o < places; o <<= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
+  if (sigmoid) {
+    most = fminf(most, 0.0f);
+    v = l < 0.0f ? expf(l - most) / (1.0f + expf(l)) : 1.0f / (1.0f + expf(-l));
+  } else {
+    v = expf(l - most);
+  }
+  if (!there) v = 0.0f;
+  float total = v;
+  for (int o = 1; o < places; o <<= 1) total += __shfl_xor_sync(kAll, total, o);
+  return v / total;
+}
+
+// A token's weight of an expert with this logit; most, total: of all the token's logits, if not renormalised.
+__device__ __forceinline__ float weight_of(const RouteArgs& a, float logit, bool there, int places, float most, float total) {
+  if (a.renormalise) return share_of(logit, there, a.sigmoid, places);
+  return a.sigmoid ? 1.0f / (1.0f + expf(-logit)) : expf(logit - most) / total;
+}
+
+// A whole token in binary64, for the few whose numbers lie too close for binary32.  slots: room for k numbers.
 template <typename T, int N>
-__device__ __noinline__ int choose_in_64_bits(const RouteArgs& a, const T* row, int* slots, int lane) {
+__device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int* slots, int lane) {
+  const T* row = static_cast<const T*>(a.logits) + t * a.ld;
   const Share own(a, lane);
   double c[N], most = -INFINITY;
+  bool bad = false;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     c[i] = i < own.count ? (double)to_float(row[own.first + i]) : -INFINITY;
     if (c[i] > most) most = c[i];
+    bad |= !(c[i] < INFINITY);
   }
+  bad = __any_sync(kAll, bad);
 #pragma unroll
   for (int o = 16; o; o >>= 1) most = fmax(most, __shfl_xor_sync(kAll, most, o));
   double total = 0.0;
@@ -132,205 +161,274 @@ __device__ __noinline__ int choose_in_64_bits(const RouteArgs& a, const T* row, 
       for (int i = 0; i < N; ++i) c[i] = -INFINITY;
     }
   }
-  for (int j = 0; j < a.k; ++j) {
-    double best = -INFINITY;
-    int e = INT32_MAX;
+  // the numbers in the order of whole numbers, as in k_route; 0: none
+  uint64_t key[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (c[i] > best) {
-        best = c[i];
-        e = own.first + i;
-      }
+  for (int i = 0; i < N; ++i) {
+    const int64_t b = __double_as_longlong(c[i] + 0.0);
+    key[i] = c[i] == -INFINITY ? 0ull : (uint64_t)(b ^ (b >> 63 | INT64_MIN));
+  }
+  int found = 0;
+  for (; found < a.k; ++found) {
+    uint64_t best = key[0];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const double b = __shfl_xor_sync(kAll, best, o);
-      const int f = __shfl_xor_sync(kAll, e, o);
-      if (b > best || (b == best && f < e)) {
-        best = b;
-        e = f;
-      }
+    for (int i = 1; i < N; ++i) best = best > key[i] ? best : key[i];
+    const u32 high = __reduce_max_sync(kAll, (u32)(best >> 32));
+    const u32 low = __reduce_max_sync(kAll, (u32)(best >> 32) == high ? (u32)best : 0u);
+    const uint64_t m = (uint64_t)high << 32 | low;
+    if (m == 0) break;
+    if (lane == __ffs(__ballot_sync(kAll, best == m)) - 1) {  // the lowest lane, and its lowest
+      bool open = true;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (open && key[i] == m) {
+          key[i] = 0;
+          slots[found] = own.first + i;
+          open = false;
+        }
     }
-    if (best == -INFINITY) return j;
-    if (lane == 0) slots[j] = e;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (own.first + i == e && i < own.count) c[i] = -INFINITY;
   }
-  return a.k;
+  __syncwarp();
+  const bool there = lane < found;
+  const int e = there ? slots[lane] : -1;
+  __syncwarp();
+  const float logit = there ? to_float(row[e]) : 0.0f;
+  float w = weight_of(a, logit, there, 32, (float)most, (float)total);
+  if (bad && !a.sigmoid) w = __uint_as_float(0x7FC00000u);
+  if (lane < a.k) {
+    a.experts[t * a.k + lane] = e;
+    a.weights[t * a.k + lane] = there ? w * a.scale : 0.0f;
+  }
 }
 
-// Descending order within a lane (Batcher's odd-even merge sort).
+// Descending order within a lane, by the shortest networks for two, four and eight (Knuth, volume 3, 5.3.4).
+__device__ __forceinline__ void exchange(u32& a, u32& b) {
+  const u32 x = a;
+  a = max(x, b);
+  b = min(x, b);
+}
 template <int N> __device__ __forceinline__ void sort_descending(u32 (&v)[N]) {
-#pragma unroll
-  for (int p = 1; p < N; p *= 2)
-#pragma unroll
-    for (int q = p; q >= 1; q /= 2)
-#pragma unroll
-      for (int j = q % p; j + q < N; j += 2 * q)
-#pragma unroll
-        for (int i = 0; i < q; ++i)
-          if (i + j + q < N && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
-            const u32 x = v[i + j], y = v[i + j + q];
-            v[i + j] = max(x, y);
-            v[i + j + q] = min(x, y);
-          }
-}
-
-// The weights of the experts chosen, one a lane, as shares: exp(l) (softmax) or 1 / (1 + exp(-l)) over their sum.  Everything is
-// taken relative to the largest, so that no sum is 0 whatever the logits.
-__device__ __forceinline__ float share_of(float l, bool there, bool sigmoid) {
-  float most = warp_max(there ? l : -INFINITY), v;
-  if (sigmoid) {
-    most = fminf(most, 0.0f);
-    v = l < 0.0f ? expf(l - most) / (1.0f + expf(l)) : 1.0f / (1.0f + expf(-l));
-  } else {
-    v = expf(l - most);
+  if constexpr (N == 2) {
+    exchange(v[0], v[1]);
+  } else if constexpr (N == 4) {
+    exchange(v[0], v[2]); exchange(v[1], v[3]);
+    exchange(v[0], v[1]); exchange(v[2], v[3]);
+    exchange(v[1], v[2]);
+  } else if constexpr (N == 8) {
+    exchange(v[0], v[2]); exchange(v[1], v[3]); exchange(v[4], v[6]); exchange(v[5], v[7]);
+    exchange(v[0], v[4]); exchange(v[1], v[5]); exchange(v[2], v[6]); exchange(v[3], v[7]);
+    exchange(v[0], v[1]); exchange(v[2], v[3]); exchange(v[4], v[5]); exchange(v[6], v[7]);
+    exchange(v[2], v[4]); exchange(v[3], v[5]);
+    exchange(v[1], v[4]); exchange(v[3], v[6]);
+    exchange(v[1], v[2]); exchange(v[3], v[4]); exchange(v[5], v[6]);
   }
-  if (!there) v = 0.0f;
-  return v / warp_sum(v);
 }
 
-// A token's experts are found by k times taking the largest key of the warp.  A key is a number in the order of c (of the logits
-// themselves without bias: the order is the same) whose low bits say which of the lane's experts it belongs to, so that one
-// reduction finds number and place.
-//   16-bit logits, no bias: the low bits of the numbers are 0, the expert's own number fits there, and the keys are in the exact
+__device__ __forceinline__ void write_if(bool really, int2* to, int x, u32 y) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %0, 0;\n@p st.shared.v2.b32 [%1], {%2, %3};\n}"
+               ::"r"((u32)really), "r"(smem_at(to)), "r"(x), "r"(y) : "memory");
+}
+
+// How experts are compared: by their logits (without bias: the order is the same), or by c.  With groups that are judged by two of their
+// scores these are needed all the same, and then c stands in for the logits' order: see `by_logit` in k_route.
+constexpr int kMostShare = 4096;  // tokens of a warp
+
+enum How { kByLogit, kBySoftmax, kBySigmoid };
+
+// A token's experts are found by k times taking the largest key of the warp.  A key is a number in the order of c whose low bits say
+// which of the lane's experts it belongs to, so that one reduction finds number and place; a lane keeps its keys sorted.
+//   16-bit logits that are compared themselves: the low bits of the numbers are 0, the expert's own number fits there, and the keys are in the exact
 //   order, ties included.
-//   Otherwise log2(N) bits are cut off and the scores themselves are rounded: tokens among whose first k + 1 numbers, or
-//   groups, two are closer than both errors together go to choose_in_64_bits.
-// Errors: an expf within 2 units of its last place and the rounding of its argument x, which changes x exp(-x) by 0.37 units of
-// 2^-24 at most; a sum of up to 512 of them as a tree of at most 21 additions; a division: 2^-19 of the largest score covers them.
-template <typename T, int N>
-__global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__ RouteArgs a) {
-  __shared__ int all_slots[kRouteWarps][REGTOPK_ROUTE_MAX_CHOICES];
+//   Otherwise log2(N) bits are cut off and scores are rounded: tokens among whose first k + 1 numbers, or at the border of whose
+//   groups, two are closer than both errors together are done again by route_in_64_bits, as are those with NaN.
+// Errors: an exponential within 2 units of its last place and its rounded argument x, which changes x exp(-x) by 0.37 * 1.5 units of
+// 2^-24 at most; a sum of up to 512 of them as a tree of at most 21 additions; a reciprocal and two products: 2^-19 of the largest score
+// covers them.
+// The weights of a warp's `batch` tokens are worked out together, in lanes that would be idle with one token's.
+template <typename T, int N, int HOW>
+__global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const __grid_constant__ RouteArgs a) {
+  __shared__ int all_slots[kRouteWarps][32];
+  __shared__ u32 all_unsure[kRouteWarps][kMostShare / 32];  // a bit for each of the warp's tokens
+  __shared__ int2 all_found[kRouteWarps][64];  // of a token's keys: the holder's first expert, the key; and the key after the last
   begin_after_predecessor();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr bool kSorted = N <= 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, places = 1 << a.places_log2;
   int* slots = all_slots[warp];
+  int2* all = all_found[warp];
+  u32* unsure = all_unsure[warp];
   const Share own(a, lane);
-  float bias[N];
+  const bool by_logit = HOW == kByLogit || !a.bias, exact = sizeof(T) == 2 && by_logit;
+  const u32 low_bits = exact ? 511u : (u32)(N - 1), pair_bits = HOW == kByLogit ? low_bits : (u32)(N - 1);
+  float bias[HOW == kByLogit ? 1 : N];
+  if (HOW != kByLogit) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) bias[i] = a.bias && i < own.count ? a.bias[own.first + i] : 0.0f;
-  const bool scored = a.bias || (a.groups > 1 && a.top == 2), exact_keys = sizeof(T) == 2 && !a.bias;
-  const int64_t step = (int64_t)gridDim.x * kRouteWarps;
-  for (int64_t t = (int64_t)blockIdx.x * kRouteWarps + warp; t < a.tokens; t += step) {
-    const T* row = static_cast<const T*>(a.logits) + t * a.ld;
-    float l[N];
-    read_logits<T, N>(l, row, own, a.wide);
-    // softmax: the largest logit, the sum of all exponentials beside it
-    bool bad = false;
-    float most = -INFINITY, total = 1.0f, per_total = 1.0f;
-    if (!a.sigmoid) {
+    for (int i = 0; i < N; ++i) bias[i] = a.bias && i < own.count ? a.bias[own.first + i] : 0.0f;
+  }
+  int64_t t0 = ((int64_t)blockIdx.x * kRouteWarps + warp) * a.share;
+  const int64_t end = min(t0 + a.share, a.tokens);
+  const T* logits = static_cast<const T*>(a.logits);
+  float ahead[N];
+  if (t0 < end) read_logits<T, N>(ahead, logits + t0 * a.ld, own, a.wide);
+  const int64_t begin = t0;
+  for (int i = lane; i < (a.share + 31) >> 5; i += 32) unsure[i] = 0;
+  bool any = false;
+  __syncwarp();
+  for (; t0 < end; t0 += a.batch) {
+    int count = 0;           // this lane's token's: experts found,
+    float most = 0.0f, total = 1.0f, margin = 0.0f;  // largest logit, sum of the exponentials, error of a difference of scores
+    u32 close = 0;           // a bit a token
+    for (int r = 0; r < a.batch; ++r) {
+      const int64_t t = t0 + r;
+      if (t >= end) break;
+      float l[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) l[i] = ahead[i];
+      if (t + 1 < end) read_logits<T, N>(ahead, logits + (t + 1) * a.ld, own, a.wide);
+      const bool mine = lane >> a.places_log2 == r;
+      float top = 0.0f, sum = 1.0f, per_sum = 1.0f;
+      if (HOW == kBySoftmax || (HOW == kByLogit && !a.sigmoid && !a.renormalise)) {
+        top = l[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) top = fmaxf(top, l[i]);
+        top = warp_max(top);
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += exp2_fast((l[i] == -INFINITY ? -INFINITY : l[i] - top) * kLog2E);
+        sum = warp_sum(sum);
+        per_sum = 1.0f / sum;
+        if (mine) most = top, total = sum;
+      }
+      const float apart = HOW == kByLogit ? 0.0f : 0x1p-18f * per_sum;
+      if (mine) margin = apart;
+      u32 key[N], pair1 = 0, pair2 = 0;  // pair: the keys of this lane's two largest scores, where experts are compared by other numbers
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        most = fmaxf(most, l[i]);
-        bad |= !(l[i] <= FLT_MAX);
-      }
-      bad = __any_sync(kAll, bad);
-      if (scored || !a.renormalise) {
-        most = warp_max(most);
-        total = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) total += l[i] == -INFINITY ? 0.0f : expf(l[i] - most);
-        total = warp_sum(total);
-        per_total = 1.0f / total;
-      }
-    }
-    const float margin = scored ? 0x1p-18f * per_total : 0.0f;  // of the difference of two scores
-    bool near = false;
-    u32 key[N];
-    float t1 = -INFINITY, t2 = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float c = l[i], s = l[i];
-      if (scored) {
-        s = a.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-c)) : expf(c - most) * per_total;
-        if (a.bias) c = s = s + bias[i];
-        if (l[i] == -INFINITY) c = s = -INFINITY;
-      }
-      if (s != s) s = -FLT_MAX;
-      t2 = fmaxf(t2, fminf(t1, s));
-      t1 = fmaxf(t1, s);
-      const u32 low = exact_keys ? 511u - (u32)(own.first + i) : (u32)(N - 1 - i), mask = exact_keys ? 511u : (u32)(N - 1);
-      key[i] = c == -INFINITY ? 0u : c != c ? 0x400u | low : (ordered(c) & ~mask) | low;
-    }
-    if (a.groups > 1) {
-      for (int o = 1; o < a.lanes; o <<= 1) {
-        const float o1 = __shfl_xor_sync(kAll, t1, o), o2 = __shfl_xor_sync(kAll, t2, o);
-        t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
-        t1 = fmaxf(t1, o1);
-      }
-      const float strength = a.top == 2 && t2 != -INFINITY ? t1 + t2 : t1;
-      int rank = 0;
-      for (int g = 0; g < a.groups; ++g) {
-        const float s = __shfl_sync(kAll, strength, g << a.lanes_log2);
-        rank += s > strength || (s == strength && g < own.group);
-        near |= scored && g != own.group && own.group < a.groups && fabsf(s - strength) <= fmaf(0x1p-21f, fabsf(s) + fabsf(strength), 2.0f * margin);
-      }
-      if (rank >= a.kept) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) key[i] = 0;
-      }
-    }
-    // the k largest keys
-    constexpr bool kSorted = N <= 8;
-    if (kSorted) sort_descending<N>(key);
-    u32 mine = 0, beyond = 0;  // lane j: the j-th largest; beyond: the one after the last
-    int picked = 0;
-    for (int j = 0;; ++j) {
-      u32 top = key[0];
-      if (!kSorted) {
-#pragma unroll
-        for (int i = 1; i < N; ++i) top = max(top, key[i]);
-      }
-      const u32 m = __reduce_max_sync(kAll, top);
-      if (j == a.k) {
-        beyond = m;
-        break;
-      }
-      if (m == 0) break;
-      ++picked;
-      if (lane == j) mine = m;
-      const u32 holders = __ballot_sync(kAll, top == m);
-      near |= (holders & (holders - 1)) != 0;  // never among exact keys
-      if (top == m) {
-        slots[j] = exact_keys ? (int)(511u - (m & 511u)) : own.first + N - 1 - (int)(m & (N - 1));
-        if (kSorted) {
-#pragma unroll
-          for (int i = 0; i + 1 < N; ++i) key[i] = key[i + 1];
-          key[N - 1] = 0;
+        float c = l[i];
+        const u32 low = exact ? 511u - (u32)(own.first + i) & 511u : (u32)(N - 1 - i);  // behind the last expert it may wrap
+        if (HOW != kByLogit) {
+          const float s = HOW == kBySigmoid ? reciprocal_fast(1.0f + exp2_fast(c * -kLog2E)) : exp2_fast((c - top) * kLog2E) * per_sum;
+          const float biased = c == -INFINITY ? -INFINITY : s + bias[i];
+          if (by_logit) {
+            const u32 k = ordered(biased) & ~pair_bits;
+            pair2 = max(pair2, min(pair1, k));
+            pair1 = max(pair1, k);
+            c += 0.0f;
+          } else {
+            c = biased;
+          }
         } else {
+          c += 0.0f;
+        }
+        key[i] = (ordered(c) & ~low_bits) | low;
+      }
+      if (kSorted) sort_descending<N>(key);
+      bool near = false;
+      if (a.groups > 1) {
+        if (HOW == kByLogit || !by_logit) {
+          if (kSorted) {
+            pair1 = key[0];
+            pair2 = N > 1 ? key[N > 1 ? 1 : 0] : 0;
+          } else {
 #pragma unroll
-          for (int i = 0; i < N; ++i) key[i] = key[i] == m ? 0u : key[i];
+            for (int i = 0; i < N; ++i) {
+              pair2 = max(pair2, min(pair1, key[i]));
+              pair1 = max(pair1, key[i]);
+            }
+          }
+        }
+        for (int o = 1; o < a.lanes; o <<= 1) {
+          const u32 o1 = __shfl_xor_sync(kAll, pair1, o), o2 = __shfl_xor_sync(kAll, pair2, o);
+          pair2 = max(min(pair1, o1), max(pair2, o2));
+          pair1 = max(pair1, o1);
+        }
+        const float t1 = unordered(pair1 & ~pair_bits), t2 = unordered(pair2 & ~pair_bits);
+        const float strength = pair1 <= kNone ? -INFINITY : (HOW != kByLogit && a.top == 2 && pair2 > kNone ? t1 + t2 : t1) + 0.0f;
+        u32 group = own.group < a.groups ? (ordered(strength) & ~31u) | (31u - own.group) : 0u, last = 0;
+        bool kept = false;
+        for (int g = 0; g < a.kept; ++g) {
+          last = __reduce_max_sync(kAll, group);
+          kept |= group == last;
+          group = group == last ? 0u : group;
+        }
+        if (!(exact && HOW == kByLogit) && a.kept < a.groups) {
+          const float v = unordered(last & ~31u), w = unordered(__reduce_max_sync(kAll, group) & ~31u);
+          near = w > -INFINITY && !(v - w > fmaf(0x1p-23f * (32 + 2 * N), fabsf(v) + fabsf(w), 2.0f * apart));
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) key[i] = kept ? key[i] : 0u;
+      }
+      // the k largest keys and the one after them, four at a time
+      int found = 0, taken = 0;
+      int2* slot = all + r * (places + 1);
+      for (int j0 = 0; j0 <= a.k; j0 += 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          u32 best = key[0];
+          if (!kSorted) {
+#pragma unroll
+            for (int i = 1; i < N; ++i) best = max(best, key[i]);
+          }
+          const u32 m = __reduce_max_sync(kAll, best);
+          if (j0 + j >= a.k) {
+            if (lane == 0) slot[a.k].y = (int)m;
+            break;
+          }
+          // the lane that holds it writes it down and goes on to its next; without branches, which would take longer than all this
+          const bool holds = best == m && m > kNone;
+          found += m > kNone;
+          taken += holds;
+          write_if(holds, slot + j0 + j, own.first, m);
+          if (kSorted) {
+#pragma unroll
+            for (int i = 0; i + 1 < N; ++i) key[i] = holds ? key[i + 1] : key[i];
+            key[N - 1] = holds ? 0u : key[N - 1];
+          } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) key[i] = key[i] == m ? 0u : key[i];
+          }
         }
       }
+      if (found < a.k && lane == 0) slot[found].y = 0;
+      if (!exact) near |= __reduce_add_sync(kAll, taken) != found;  // the same key twice
+      if (near) close |= 1u << r;
+      if (mine) count = found;
     }
-    if (!exact_keys) {
-      constexpr u32 kMask = N - 1;
-      u32 next = __shfl_down_sync(kAll, mine, 1);
-      if (lane == picked - 1) next = beyond;
-      if (lane < picked && next) {
-        const float v = unordered(mine & ~kMask), w = unordered(next & ~kMask);
-        near |= !(v - w > fmaf(N * 0x1p-22f, fabsf(v) + fabsf(w), margin)) && v < INFINITY && next > 0x7FFu;
-        near |= v == INFINITY && w == INFINITY;
-        near |= mine < 0x800u;  // NaN: their order in a lane and over lanes
+    __syncwarp();
+    // from here on a lane has one place of one token
+    const int r = lane >> a.places_log2, j = lane & (places - 1);
+    const int64_t t = t0 + r;
+    u32 first = 0;
+    bool near = false;
+    int e = -1;
+    if (count > 0) {
+      const int2* slot = all + r * (places + 1);
+      first = (u32)slot[0].y;
+      if (j < count) {
+        const u32 k = (u32)slot[j].y, next = (u32)slot[j + 1].y;
+        const float v = unordered(k & ~low_bits), w = unordered(next & ~low_bits);
+        near = k > (kInfinite | low_bits) || (!exact && next > kNone && !(v - w > fmaf(N * 0x1p-22f, fabsf(v) + fabsf(w), by_logit ? 0.0f : margin)));
+        e = exact ? (int)(511u - (k & 511u)) : slot[j].x + N - 1 - (int)(k & (N - 1));
       }
     }
-    __syncwarp();
-    if (__any_sync(kAll, near)) picked = choose_in_64_bits<T, N>(a, row, slots, lane);
-    __syncwarp();
-    const bool there = lane < picked;
-    const int e = there ? slots[lane] : -1;
-    __syncwarp();
-    const float logit = there ? to_float(row[e]) : 0.0f;
-    float w;
-    if (a.renormalise) w = share_of(logit, there, a.sigmoid);
-    else if (a.sigmoid) w = 1.0f / (1.0f + expf(-logit));
-    else w = expf(logit - most) / total;
-    w = bad ? __uint_as_float(0x7FC00000u) : w * a.scale;
-    if (lane < a.k) {
-      a.experts[t * a.k + lane] = e;
-      a.weights[t * a.k + lane] = there ? w : 0.0f;
+    near |= (close >> r & 1u) != 0;
+    if (__any_sync(kAll, near)) {
+      any = true;
+      if (near && t < end) atomicOr(&unsure[(t - begin) >> 5], 1u << ((t - begin) & 31));
     }
+    const bool there = j < count;
+    const float logit = there ? to_float(logits[t * a.ld + e]) : 0.0f;
+    float w = weight_of(a, logit, there, places, most, total);
+    // a NaN or an infinity anywhere makes the scores of a softmax NaN
+    if (!a.sigmoid && (HOW == kBySoftmax ? total != total : first >= kInfinite)) w = __uint_as_float(0x7FC00000u);
+    if (j < a.k && r < a.batch && t < end) {
+      a.experts[t * a.k + j] = e;
+      a.weights[t * a.k + j] = there ? w * a.scale : 0.0f;
+    }
+    __syncwarp();
   }
+  if (!any) return;
+  for (int64_t t = begin; t < end; ++t)
+    if (unsure[(t - begin) >> 5] >> ((t - begin) & 31) & 1u) route_in_64_bits<T, N>(a, t, slots, lane);
 }
 
 // ---- the gradient to the logits ------------------------------------------------------------------------------------
@@ -373,7 +471,7 @@ template <typename T> __global__ void __launch_bounds__(kRouteThreads) k_route_b
       g = a.scale * dw;
       mean = warp_sum(there && l != -INFINITY ? g * expf(l - most) * per_total : 0.0f);
     } else if (a.renormalise) {
-      const float p = share_of(l, there, a.sigmoid);
+      const float p = share_of(l, there, a.sigmoid, 32);
       g = a.scale * p * (dw - warp_sum(there ? dw * p : 0.0f));
       if (a.sigmoid) g /= 1.0f + expf(l);
     } else {
@@ -443,80 +541,106 @@ struct SortArgs {
 };
 
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+constexpr int kSortKept = 8;  // steps of a run whose groups stay in registers between the two times that they are needed
 
-// The group of a pair, or -1.
-__device__ __forceinline__ int group_of_pair(const SortArgs& a, u32 pair) {
+// The group of a pair, or -1; `at` is a copy of workers_at in shared memory.
+__device__ __forceinline__ int group_of_pair(const SortArgs& a, const int64_t* at, u32 pair) {
   const int e = a.experts[pair];
   if (e < 0 || e >= a.n_experts) return -1;
   if (!a.workers_at) return e;
   const int64_t t = a.k.quotient_of(pair);
-  if (t < a.workers_at[0] || t >= a.workers_at[a.workers]) return -1;
+  if (t < at[0] || t >= at[a.workers]) return -1;
   int lo = 0, hi = a.workers;  // the last worker that begins at t or before
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (a.workers_at[mid] <= t) lo = mid;
+    if (at[mid] <= t) lo = mid;
     else hi = mid;
   }
   return lo * a.n_experts + e;
 }
+__device__ __forceinline__ void copy_workers(const SortArgs& a, int64_t* at) {
+  if (a.workers_at)
+    for (int i = threadIdx.x; i <= a.workers; i += kSortThreads) at[i] = a.workers_at[i];
+}
 
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(const __grid_constant__ SortArgs a) {
   __shared__ u32 count[REGTOPK_MATMUL_MAX_GROUPS];
+  __shared__ int64_t workers_at[REGTOPK_MATMUL_MAX_GROUPS + 1];
   begin_after_predecessor();
+  copy_workers(a, workers_at);
   for (int g = threadIdx.x; g < a.groups; g += kSortThreads) count[g] = 0;
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * a.chunk, end = min(first + a.chunk, a.pairs);
   for (int64_t p = first + threadIdx.x; p < end; p += kSortThreads) {
-    const int g = group_of_pair(a, (u32)p);
+    const int g = group_of_pair(a, workers_at, (u32)p);
     if (g >= 0) atomicAdd(&count[g], 1u);
   }
   __syncthreads();
   for (int g = threadIdx.x; g < a.groups; g += kSortThreads) a.counts[(int64_t)blockIdx.x * a.groups + g] = count[g];
 }
 
-// dynamic shared memory: base [groups], then runs [warps][groups]
-__global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a) {
+// dynamic shared memory: workers_at; of each group its size and what lies before it [2][groups], then runs [warps][groups]
+// KEPT: a run has kSortKept steps at most.
+template <bool KEPT> __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ u32 sums[kSortWarps];
   begin_after_predecessor();
-  u32* base = reinterpret_cast<u32*>(smem);
-  u32* runs = base + a.groups;
+  int64_t* workers_at = reinterpret_cast<int64_t*>(smem);
+  u32 *base = reinterpret_cast<u32*>(workers_at + a.workers + 1), *sizes = base + a.groups, *runs = sizes + a.groups;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < kSortWarps * a.groups; i += kSortThreads) runs[i] = 0;
-  __syncthreads();
+  copy_workers(a, workers_at);
+  for (int i = threadIdx.x; i < (2 + kSortWarps) * a.groups; i += kSortThreads) base[i] = 0;
   // this warp's run
   const int64_t first = (int64_t)blockIdx.x * a.chunk, end = min(first + a.chunk, a.pairs);
   const int64_t length = ((end - first + kSortWarps - 1) / kSortWarps + 31) & ~31ll, from = first + warp * length, to = min(from + length, end);
   u32* own = runs + warp * a.groups;
-  for (int64_t p = from + lane; p - lane < to; p += 32) {
-    const int g = p < to ? group_of_pair(a, (u32)p) : -1;
+  int kept[KEPT ? kSortKept : 1];
+  __syncthreads();
+  if (KEPT) {
+#pragma unroll
+    for (int i = 0; i < kSortKept; ++i) kept[i] = from + i * 32 + lane < to ? group_of_pair(a, workers_at, (u32)(from + i * 32 + lane)) : -1;
+  }
+#pragma unroll KEPT ? kSortKept : 1
+  for (int i = 0; KEPT ? i < kSortKept : from + i * 32 < to; ++i) {
+    if (KEPT && from + i * 32 >= to) break;
+    const int64_t p = from + i * 32 + lane;
+    const int g = KEPT ? kept[KEPT ? i : 0] : p < to ? group_of_pair(a, workers_at, (u32)p) : -1;
     const u32 same = __match_any_sync(kAll, g);
     if (g >= 0 && lane == __ffs(same) - 1) own[g] += __popc(same);
     __syncwarp();
+  }
+  // the sums over chunks, by as many threads a group as there are
+  if (a.chunks > 1) {
+    const int parts = a.groups >= kSortThreads ? 1 : kSortThreads / a.groups;
+    for (int i = threadIdx.x; i < parts * a.groups; i += kSortThreads) {
+      const int part = i / a.groups, g = i - part * a.groups;
+      u32 total = 0, before = 0;
+#pragma unroll 8
+      for (int c = part; c < a.chunks; c += parts) {
+        const u32 n = a.counts[(int64_t)c * a.groups + g];
+        total += n;
+        before += c < (int)blockIdx.x ? n : 0;
+      }
+      atomicAdd(&sizes[g], total);
+      atomicAdd(&base[g], before);
+    }
   }
   __syncthreads();
   // of every group: its size, what lies in the chunks before, and within this one in the runs before
   u32 at = 0;  // start of the groups that this round of threads looks at
   for (int g0 = 0; g0 < a.groups; g0 += kSortThreads) {
     const int g = g0 + threadIdx.x;
-    u32 total = 0, before = 0;
+    u32 total = 0;
     if (g < a.groups) {
-      u32 here = 0;
+      u32 n[kSortWarps], here = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) n[w] = runs[w * a.groups + g];
+#pragma unroll
       for (int w = 0; w < kSortWarps; ++w) {
-        const u32 n = runs[w * a.groups + g];
         runs[w * a.groups + g] = here;
-        here += n;
+        here += n[w];
       }
-      if (a.chunks == 1) {
-        total = here;
-      } else {
-#pragma unroll 8
-        for (int c = 0; c < a.chunks; ++c) {
-          const u32 n = a.counts[(int64_t)c * a.groups + g];
-          total += n;
-          before += c < (int)blockIdx.x ? n : 0;
-        }
-      }
+      total = a.chunks == 1 ? here : sizes[g];
     }
     u32 scan = total;
 #pragma unroll
@@ -527,12 +651,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_consta
     if (lane == 31) sums[warp] = scan;
     __syncthreads();
     u32 lower = at, all = at;
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
       if (w < warp) lower += sums[w];
       all += sums[w];
     }
     if (g < a.groups) {
-      base[g] = lower + scan - total + before;
+      base[g] += lower + scan - total;
       if (blockIdx.x == 0) {
         a.offsets[g] = lower + scan - total;
         if (g == a.groups - 1) a.offsets[a.groups] = lower + scan;
@@ -541,8 +666,11 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_consta
     at = all;
     __syncthreads();
   }
-  for (int64_t p = from + lane; p - lane < to; p += 32) {
-    const int g = p < to ? group_of_pair(a, (u32)p) : -1;
+#pragma unroll KEPT ? kSortKept : 1
+  for (int i = 0; KEPT ? i < kSortKept : from + i * 32 < to; ++i) {
+    if (KEPT && from + i * 32 >= to) break;
+    const int64_t p = from + i * 32 + lane;
+    const int g = KEPT ? kept[KEPT ? i : 0] : p < to ? group_of_pair(a, workers_at, (u32)p) : -1;
     const u32 same = __match_any_sync(kAll, g);
     const u32 rank = __popc(same & ((1u << lane) - 1));
     u32 where = 0;
@@ -556,7 +684,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_consta
 
 // Pairs of a chunk: see regtopk_sort_tokens.
 inline int chunk_of(int64_t pairs) {
-  int64_t chunk = pairs <= 4096 ? 4096 : 1024;
+  int64_t chunk = pairs <= kSortThreads * kSortKept ? kSortThreads * kSortKept : 1024;
   while (chunk * 128 < pairs) chunk *= 2;
   return (int)chunk;
 }
@@ -569,9 +697,21 @@ template <auto kKernel> bool allow_smem_of(int dev, int bytes) {
   return true;
 }
 
-template <typename T, int N> int launch_route(const RouteArgs& a, int sms, cudaStream_t s) {
-  const int64_t blocks = (a.tokens + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sms * 8;
-  return start(k_route<T, N>, (unsigned)(blocks < most ? blocks : most), kRouteThreads, 0, s, a);
+template <typename T, int N> int launch_route(RouteArgs& a, int sms, cudaStream_t s) {
+  // Every warp takes the same number of tokens, neighbours.  Finished together are as many as have places in a warp.
+  a.places_log2 = 0;
+  while (1 << a.places_log2 < a.k) ++a.places_log2;
+  const int64_t warps = (int64_t)sms * (N <= 8 ? 4 : 2) * kRouteWarps;
+  int64_t each = (a.tokens + warps - 1) / warps;
+  if (each > kMostShare) each = kMostShare;
+  if (a.tokens / each / kRouteWarps >= INT32_MAX) return REGTOPK_ERR_TOO_LARGE;
+  a.share = (int)each;
+  a.batch = 1;
+  while (a.batch << a.places_log2 < 32 && a.batch < 8 && a.batch < each) a.batch *= 2;
+  const unsigned grid = (unsigned)((a.tokens + each * kRouteWarps - 1) / (each * kRouteWarps));
+  if (a.bias || (a.groups > 1 && a.top == 2))
+    return a.sigmoid ? start(k_route<T, N, kBySigmoid>, grid, kRouteThreads, 0, s, a) : start(k_route<T, N, kBySoftmax>, grid, kRouteThreads, 0, s, a);
+  return start(k_route<T, N, kByLogit>, grid, kRouteThreads, 0, s, a);
 }
 template <typename T> int launch_route_of(RouteArgs& a, int sms, cudaStream_t s) {
   int n = 1;
@@ -680,9 +820,14 @@ int regtopk_sort_tokens(const int32_t* experts, const int64_t* workers_at, int32
     const int rc = start(k_sort_count, a.chunks, kSortThreads, 0, s, a);
     if (rc != REGTOPK_OK) return rc;
   }
-  constexpr int kMostSmem = REGTOPK_MATMUL_MAX_GROUPS * 4 * (1 + kSortWarps);
-  if (!allow_smem_of<k_sort_place>(dev, kMostSmem)) return train_rc(cudaGetLastError());
-  return start(k_sort_place, a.chunks, kSortThreads, (size_t)a.groups * 4 * (1 + kSortWarps), s, a);
+  constexpr int kMostSmem = REGTOPK_MATMUL_MAX_GROUPS * 4 * (2 + kSortWarps) + 8 * (REGTOPK_MATMUL_MAX_GROUPS + 1);
+  const size_t bytes = (size_t)a.groups * 4 * (2 + kSortWarps) + 8 * ((size_t)a.workers + 1);
+  if (a.chunk <= kSortThreads * kSortKept) {
+    if (!allow_smem_of<k_sort_place<true>>(dev, kMostSmem)) return train_rc(cudaGetLastError());
+    return start(k_sort_place<true>, a.chunks, kSortThreads, bytes, s, a);
+  }
+  if (!allow_smem_of<k_sort_place<false>>(dev, kMostSmem)) return train_rc(cudaGetLastError());
+  return start(k_sort_place<false>, a.chunks, kSortThreads, bytes, s, a);
 }
 
 }  // extern "C"

@@ -32,82 +32,97 @@ __device__ __forceinline__ float2 pair_value(u32 pair) {
   return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
 }
 
-// Eight of a lane's values, laid out as read_eight does, to their place in the 8-bit row; columns from `cols` on are zeros in f and
-// not written.  The whole warp takes part; VEC: four lanes in a row, whose first one's column is a multiple of 32, share a block.
-template <bool VEC> __device__ __forceinline__ void store_rows8(const Octet& given, uint8_t* values, uint8_t* scales, int64_t c0, int lane, int64_t cols) {
+// Eight neighbours, a thread's, to their place in an 8-bit row (at values, with their block's scale at *scale).  Four threads in a row share
+// a block and the whole warp takes part; `there`: the columns exist, otherwise f holds zeros.
+__device__ __forceinline__ void store_rows8(const Octet& given, uint8_t* values, uint8_t* scale, bool there) {
   Octet f;
+  float top = 0.0f;  // NaN are passed over
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = given[i];
-  if (VEC) {
-    u32 most = 0;
+  for (int i = 0; i < 4; ++i) {
+    f[i] = given[i];
+    top = fmaxf(top, fmaxf(fabsf(f[i].x), fabsf(f[i].y)));
+  }
+  u32 most = __float_as_uint(top);
+  most = max(most, __shfl_xor_sync(kAll, most, 1));
+  most = max(most, __shfl_xor_sync(kAll, most, 2));
+  if (__any_sync(kAll, most >= kInfinity)) {
+    most = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) most = max(most, max(magnitude(f[i].x), magnitude(f[i].y)));
+    for (int i = 0; i < 4; ++i) {
+      most = max(most, max(finite_magnitude(f[i].x), finite_magnitude(f[i].y)));
+      f[i] = make_float2(without_infinity(f[i].x), without_infinity(f[i].y));
+    }
     most = max(most, __shfl_xor_sync(kAll, most, 1));
     most = max(most, __shfl_xor_sync(kAll, most, 2));
-    if (__any_sync(kAll, most >= kInfinity)) {
-      most = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        most = max(most, max(finite_magnitude(f[i].x), finite_magnitude(f[i].y)));
-        f[i] = make_float2(without_infinity(f[i].x), without_infinity(f[i].y));
-      }
-      most = max(most, __shfl_xor_sync(kAll, most, 1));
-      most = max(most, __shfl_xor_sync(kAll, most, 2));
-    }
-    const u32 byte = scale_byte(most);
-    const float2 inverse = both(inverse_scale(byte));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = mul2(f[i], inverse);
-    const int64_t c = c0 + lane * 8;
-    if (c < cols) {
-      uint2 v;
-      v.x = e4m3_pair(f[0].x, f[0].y) | e4m3_pair(f[1].x, f[1].y) << 16;
-      v.y = e4m3_pair(f[2].x, f[2].y) | e4m3_pair(f[3].x, f[3].y) << 16;
-      *reinterpret_cast<uint2*>(values + c) = v;
-      if (!(c & 31)) scales[c >> 5] = (uint8_t)byte;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float v = (j & 1) ? f[j >> 1].y : f[j >> 1].x;
-      u32 most = __reduce_max_sync(kAll, magnitude(v));
-      if (most >= kInfinity) {
-        most = __reduce_max_sync(kAll, finite_magnitude(v));
-        v = without_infinity(v);
-      }
-      const u32 byte = scale_byte(most);
-      const int64_t c = c0 + j * 32 + lane;
-      if (c < cols) {
-        values[c] = (uint8_t)e4m3_pair(v * inverse_scale(byte), 0.0f);
-        if (lane == 0) scales[c >> 5] = (uint8_t)byte;
-      }
-    }
   }
+  const u32 byte = scale_byte(most);
+  const float2 inverse = both(inverse_scale(byte));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = mul2(f[i], inverse);
+  if (!there) return;
+  uint2 v;
+  v.x = e4m3_pair(f[0].x, f[0].y) | e4m3_pair(f[1].x, f[1].y) << 16;
+  v.y = e4m3_pair(f[2].x, f[2].y) | e4m3_pair(f[3].x, f[3].y) << 16;
+  *reinterpret_cast<uint2*>(values) = v;
+  if (!(threadIdx.x & 3)) *scale = (uint8_t)byte;
 }
 
-// The same eight columns of an 8-bit row; zeros from `cols` on.
-template <bool VEC> __device__ __forceinline__ void read_rows8(Octet& f, const uint8_t* values, const uint8_t* scales, int64_t c0, int lane, int64_t cols) {
+// A warp's 256 columns from c0 on, a multiple of 256, of an 8-bit row, every 32nd a lane's (element j is column j * 32 + lane);
+// zeros in f from `cols` on.
+__device__ __forceinline__ void store_rows8_apart(const Octet& f, uint8_t* values, uint8_t* scales, int c0, int lane, int cols) {
+  const int left = cols - c0 - lane;
+  uint8_t* to = values + c0 + lane;
+  u32 own = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = both(0.0f);
-  if (VEC) {
-    const int64_t c = c0 + lane * 8;
-    if (c >= cols) return;
-    const uint2 v = *reinterpret_cast<const uint2*>(values + c);
-    const float2 scale = both(scale_value(scales[c >> 5]));
+  for (int i = 0; i < 4; ++i) {
+    float e[2] = {f[i].x, f[i].y};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      u32 most = __reduce_max_sync(kAll, magnitude(e[j]));
+      if (most >= kInfinity) {
+        most = __reduce_max_sync(kAll, finite_magnitude(e[j]));
+        e[j] = without_infinity(e[j]);
+      }
+      const u32 byte = scale_byte(most);
+      e[j] *= inverse_scale(byte);
+      own = lane == 2 * i + j ? byte : own;
+    }
+    const u32 pair = e4m3_pair(e[0], e[1]);
+    if (i * 64 < left) to[i * 64] = (uint8_t)pair;
+    if (i * 64 + 32 < left) to[i * 64 + 32] = (uint8_t)(pair >> 8);
+  }
+  if (lane < 8 && c0 + lane * 32 < cols) scales[(c0 >> 5) + lane] = (uint8_t)own;
+}
+
+// Eight neighbours of an 8-bit row, as they lie in memory.
+struct Packed8 {
+  uint2 v;
+  u32 byte;
+  __device__ __forceinline__ void fetch(const uint8_t* values, const uint8_t* scale) {
+    v = *reinterpret_cast<const uint2*>(values);
+    byte = *scale;
+  }
+  __device__ __forceinline__ void clear() { v = make_uint2(0, 0), byte = 0; }
+  __device__ __forceinline__ void get(Octet& f) const {
+    const float2 scale = both(scale_value(byte));
     f[0] = mul2(pair_value(v.x & 0xFFFFu), scale);
     f[1] = mul2(pair_value(v.x >> 16), scale);
     f[2] = mul2(pair_value(v.y & 0xFFFFu), scale);
     f[3] = mul2(pair_value(v.y >> 16), scale);
-  } else {
-    float e[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t c = c0 + j * 32 + lane;
-      e[j] = c < cols ? pair_value(values[c]).x * scale_value(scales[c >> 5]) : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = make_float2(e[2 * i], e[2 * i + 1]);
   }
+};
+
+// A warp's 256 columns, as store_rows8_apart lays them out; zeros from `cols` on.
+__device__ __forceinline__ void read_rows8_apart(Octet& f, const uint8_t* values, const uint8_t* scales, int c0, int lane, int cols) {
+  const int left = cols - c0 - lane;
+  const uint8_t* from = values + c0 + lane;
+  const float own = scale_value(lane < 8 && c0 + lane * 32 < cols ? scales[(c0 >> 5) + lane] : 0u);
+  u32 v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j * 32 < left ? from[j * 32] : 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    f[i] = mul2(pair_value(v[2 * i] | v[2 * i + 1] << 8), make_float2(__shfl_sync(kAll, own, 2 * i), __shfl_sync(kAll, own, 2 * i + 1)));
 }
 
 inline int64_t blocks_of(int64_t cols) { return (cols + 31) / 32; }
