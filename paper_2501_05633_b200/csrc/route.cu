@@ -102,47 +102,86 @@ __device__ __forceinline__ float weight_of(const RouteArgs& a, float logit, bool
   return a.sigmoid ? 1.0f / (1.0f + expf(-logit)) : expf(logit - most) / total;
 }
 
-// A whole token in binary64, for the few whose numbers lie too close for binary32.  slots: room for k numbers.
+// exp(x) for x <= 0 in binary64: x = n ln 2 + r (Cody and Waite, 1980), the exponential's series for |r| <= ln 2 / 2 to the thirteenth
+// power, 2^-57 of it, and 2^n.  Without branches, so that those of a lane's experts overlap; below exp(-708) 0.
+__device__ __forceinline__ double exp_64(double x) {
+  const double n = rint(x * 1.4426950408889634), r = fma(n, -2.3190468138462996e-17, fma(n, -0.6931471805599453, x));
+  double y = 1.0 / 6227020800.0;
+  y = fma(y, r, 1.0 / 479001600.0);
+  y = fma(y, r, 1.0 / 39916800.0);
+  y = fma(y, r, 1.0 / 3628800.0);
+  y = fma(y, r, 1.0 / 362880.0);
+  y = fma(y, r, 1.0 / 40320.0);
+  y = fma(y, r, 1.0 / 5040.0);
+  y = fma(y, r, 1.0 / 720.0);
+  y = fma(y, r, 1.0 / 120.0);
+  y = fma(y, r, 1.0 / 24.0);
+  y = fma(y, r, 1.0 / 6.0);
+  y = fma(y, r, 0.5);
+  y = fma(y, r, 1.0);
+  y = fma(y, r, 1.0);
+  y = y * __longlong_as_double((int64_t)(fmax(n, -1022.0) + 1023.0) << 52);
+  return x < -708.0 ? 0.0 : y;  // a NaN stays one: r is
+}
+// 1 / x for 1 <= x <= 512 in binary64: binary32's, and Newton's method twice.
+__device__ __forceinline__ double reciprocal_64(double x) {
+  double y = reciprocal_fast((float)x);
+  y = fma(y, fma(-x, y, 1.0), y);
+  return fma(y, fma(-x, y, 1.0), y);
+}
+
+constexpr int kMostShare = 4096;  // tokens of a warp
+
+// A whole token in binary64, for the few whose numbers lie too close for binary32.  slots and numbers: room for k and n_experts.  Short
+// loops: what such a token costs is the time that a warp alone takes, of which the fetching of instructions is a good part.
+// The largest are looked for among the numbers rounded to binary32, which keeps their order; where several round to the same, the numbers
+// themselves decide.
 template <typename T, int N>
-__device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int* slots, int lane) {
+__device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int* slots, double* numbers, int lane) {
   const T* row = static_cast<const T*>(a.logits) + t * a.ld;
   const Share own(a, lane);
-  double c[N], most = -INFINITY;
+  float l[N], most = -INFINITY;
+  read_logits<T, N>(l, row, own, a.wide);
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    c[i] = i < own.count ? (double)to_float(row[own.first + i]) : -INFINITY;
-    if (c[i] > most) most = c[i];
-    bad |= !(c[i] < INFINITY);
+    most = fmaxf(most, l[i]);
+    bad |= !(l[i] <= FLT_MAX);
   }
   bad = __any_sync(kAll, bad);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) most = fmax(most, __shfl_xor_sync(kAll, most, o));
-  double total = 0.0;
-  if (!a.sigmoid) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (c[i] != -INFINITY) total += exp(c[i] - most);
+  const bool scored = a.bias || (a.groups > 1 && a.top == 2);
+  double total = 1.0, per_total = 1.0;
+  if (!a.sigmoid && (scored || !a.renormalise)) {
+    most = warp_max(most);
+    total = 0.0;
+#pragma unroll 2
+    for (int i = 0; i < own.count; ++i) total += exp_64((double)to_float(row[own.first + i]) - (double)most);
     total = warp_sum(total);
+    per_total = reciprocal_64(total);
   }
-  const bool scores = a.bias || a.top == 2;
   double t1 = -INFINITY, t2 = -INFINITY;  // of this lane, then of its group
+#pragma unroll 2
+  for (int i = 0; i < own.count; ++i) {
+    const float logit = to_float(row[own.first + i]);
+    double s = logit, c = logit;
+    if (scored) {
+      const double e = exp_64(a.sigmoid ? -fabs(s) : s - (double)most), r = a.sigmoid ? reciprocal_64(1.0 + e) : per_total;
+      s = a.sigmoid && logit >= 0.0f ? r : e * r;
+      if (a.bias) c = s = s + (double)a.bias[own.first + i];
+    }
+    if (logit == -INFINITY) c = -INFINITY;
+    if (c == -INFINITY) s = -INFINITY;
+    else if (s != s) s = -DBL_MAX;
+    numbers[own.first + i] = c;
+    t2 = fmax(t2, fmin(t1, s));
+    t1 = fmax(t1, s);
+  }
+  const double* c = numbers + own.first;
+  u32 key[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    if (c[i] == -INFINITY) continue;
-    double s = c[i];
-    if (scores) {
-      s = a.sigmoid ? 1.0 / (1.0 + exp(-s)) : exp(s - most) / total;
-      if (a.bias) s += (double)a.bias[own.first + i];
-    }
-    if (s != s) s = -DBL_MAX;
-    if (a.bias || c[i] != c[i]) c[i] = s != -INFINITY ? (c[i] != c[i] ? -DBL_MAX : s) : -INFINITY;
-    if (s > t1) {
-      t2 = t1;
-      t1 = s;
-    } else if (s > t2) {
-      t2 = s;
-    }
+    const double v = i < own.count ? c[i] : -INFINITY;
+    key[i] = v == -INFINITY ? 0u : v != v ? 1u : ordered((float)v + 0.0f);
   }
   if (a.groups > 1) {
     for (int o = 1; o < a.lanes; o <<= 1) {
@@ -156,36 +195,44 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
       const double s = __shfl_sync(kAll, strength, g << a.lanes_log2);
       rank += s > strength || (s == strength && g < own.group);
     }
-    if (rank >= a.kept) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) c[i] = -INFINITY;
-    }
-  }
-  // the numbers in the order of whole numbers, as in k_route; 0: none
-  uint64_t key[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int64_t b = __double_as_longlong(c[i] + 0.0);
-    key[i] = c[i] == -INFINITY ? 0ull : (uint64_t)(b ^ (b >> 63 | INT64_MIN));
+    for (int i = 0; i < N; ++i) key[i] = rank < a.kept ? key[i] : 0u;
   }
   int found = 0;
+#pragma unroll 1
   for (; found < a.k; ++found) {
-    uint64_t best = key[0];
+    u32 best = key[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) best = best > key[i] ? best : key[i];
-    const u32 high = __reduce_max_sync(kAll, (u32)(best >> 32));
-    const u32 low = __reduce_max_sync(kAll, (u32)(best >> 32) == high ? (u32)best : 0u);
-    const uint64_t m = (uint64_t)high << 32 | low;
+    for (int i = 1; i < N; ++i) best = max(best, key[i]);
+    const u32 m = __reduce_max_sync(kAll, best);
     if (m == 0) break;
-    if (lane == __ffs(__ballot_sync(kAll, best == m)) - 1) {  // the lowest lane, and its lowest
-      bool open = true;
+    int at = -1, same = 0;  // this lane's first with that key, and how many it has
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (open && key[i] == m) {
-          key[i] = 0;
-          slots[found] = own.first + i;
-          open = false;
-        }
+    for (int i = N - 1; i >= 0; --i) {
+      same += key[i] == m;
+      at = key[i] == m ? i : at;
+    }
+    u32 holders = __ballot_sync(kAll, at >= 0);
+    if (m != 1u && __any_sync(kAll, same > 1 || (holders & (holders - 1)))) {
+      double largest = -INFINITY;
+      if (at >= 0) {
+#pragma unroll 1
+        for (int i = 0; i < own.count; ++i)
+          if (c[i] > largest && ordered((float)c[i] + 0.0f) == m) {
+            largest = c[i];
+            at = i;
+          }
+      }
+      double top = largest;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmax(top, __shfl_xor_sync(kAll, top, o));
+      holders = __ballot_sync(kAll, at >= 0 && largest == top);
+    }
+    if (lane == __ffs(holders) - 1) {
+      slots[found] = own.first + at;
+      numbers[own.first + at] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < N; ++i) key[i] = i == at ? 0u : key[i];
     }
   }
   __syncwarp();
@@ -193,7 +240,7 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
   const int e = there ? slots[lane] : -1;
   __syncwarp();
   const float logit = there ? to_float(row[e]) : 0.0f;
-  float w = weight_of(a, logit, there, 32, (float)most, (float)total);
+  float w = weight_of(a, logit, there, 32, most, (float)total);
   if (bad && !a.sigmoid) w = __uint_as_float(0x7FC00000u);
   if (lane < a.k) {
     a.experts[t * a.k + lane] = e;
@@ -224,15 +271,13 @@ template <int N> __device__ __forceinline__ void sort_descending(u32 (&v)[N]) {
   }
 }
 
-__device__ __forceinline__ void write_if(bool really, int2* to, int x, u32 y) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %0, 0;\n@p st.shared.v2.b32 [%1], {%2, %3};\n}"
-               ::"r"((u32)really), "r"(smem_at(to)), "r"(x), "r"(y) : "memory");
+// The pair (x, y) to shared memory at `to` + `offset`, if a == y.
+__device__ __forceinline__ void write_if(u32 a, u32 y, u32 to, int offset, int x) {
+  asm volatile("{\n.reg .pred p;\nsetp.eq.u32 p, %0, %1;\n@p st.shared.v2.b32 [%2], {%3, %1};\n}" ::"r"(a), "r"(y), "r"(to + offset), "r"(x) : "memory");
 }
 
 // How experts are compared: by their logits (without bias: the order is the same), or by c.  With groups that are judged by two of their
 // scores these are needed all the same, and then c stands in for the logits' order: see `by_logit` in k_route.
-constexpr int kMostShare = 4096;  // tokens of a warp
-
 enum How { kByLogit, kBySoftmax, kBySigmoid };
 
 // A token's experts are found by k times taking the largest key of the warp.  A key is a number in the order of c whose low bits say
@@ -241,19 +286,20 @@ enum How { kByLogit, kBySoftmax, kBySigmoid };
 //   order, ties included.
 //   Otherwise log2(N) bits are cut off and scores are rounded: tokens among whose first k + 1 numbers, or at the border of whose
 //   groups, two are closer than both errors together are done again by route_in_64_bits, as are those with NaN.
-// Errors: an exponential within 2 units of its last place and its rounded argument x, which changes x exp(-x) by 0.37 * 1.5 units of
-// 2^-24 at most; a sum of up to 512 of them as a tree of at most 21 additions; a reciprocal and two products: 2^-19 of the largest score
-// covers them.
+// Errors, in units of 2^-24.  Sigmoid s: its argument x is rounded, which changes s by 0.224 * 1.25, the exponential is 2 units of its last
+// place off, which changes s by 1, the sum is rounded, 1, and the reciprocal, 2: less than 8 for each, 2^-20 for a difference of two.
+// Softmax: the exponential likewise (x exp(-x) is 0.37 at most), the sum of up to 512 of them, a tree of at most 21 additions, a reciprocal
+// and a product: less than 2^-19 of the largest score, 2^-18 for a difference.
 // The weights of a warp's `batch` tokens are worked out together, in lanes that would be idle with one token's.
 template <typename T, int N, int HOW>
 __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const __grid_constant__ RouteArgs a) {
   __shared__ int all_slots[kRouteWarps][32];
   __shared__ u32 all_unsure[kRouteWarps][kMostShare / 32];  // a bit for each of the warp's tokens
+  __shared__ double all_numbers[kRouteWarps][REGTOPK_ROUTE_MAX_EXPERTS];
   __shared__ int2 all_found[kRouteWarps][64];  // of a token's keys: the holder's first expert, the key; and the key after the last
   begin_after_predecessor();
   constexpr bool kSorted = N <= 8;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, places = 1 << a.places_log2;
-  int* slots = all_slots[warp];
   int2* all = all_found[warp];
   u32* unsure = all_unsure[warp];
   const Share own(a, lane);
@@ -298,7 +344,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
         per_sum = 1.0f / sum;
         if (mine) most = top, total = sum;
       }
-      const float apart = HOW == kByLogit ? 0.0f : 0x1p-18f * per_sum;
+      const float apart = HOW == kByLogit ? 0.0f : HOW == kBySigmoid ? 0x1p-20f : 0x1p-18f * per_sum;
       if (mine) margin = apart;
       u32 key[N], pair1 = 0, pair2 = 0;  // pair: the keys of this lane's two largest scores, where experts are compared by other numbers
 #pragma unroll
@@ -357,27 +403,24 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
 #pragma unroll
         for (int i = 0; i < N; ++i) key[i] = kept ? key[i] : 0u;
       }
-      // the k largest keys and the one after them, four at a time
+      // the k largest keys and the one after them, four at a time.  The lane that holds one writes it down and goes on to its next; without
+      // branches, which would take longer than all this.  What is no expert is written down too.
       int found = 0, taken = 0;
-      int2* slot = all + r * (places + 1);
+      const u32 slot = smem_at(all) + r * (places + 1) * 8;
       for (int j0 = 0; j0 <= a.k; j0 += 4) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+          if (j > 0 && j0 + j > a.k) break;
           u32 best = key[0];
           if (!kSorted) {
 #pragma unroll
             for (int i = 1; i < N; ++i) best = max(best, key[i]);
           }
           const u32 m = __reduce_max_sync(kAll, best);
-          if (j0 + j >= a.k) {
-            if (lane == 0) slot[a.k].y = (int)m;
-            break;
-          }
-          // the lane that holds it writes it down and goes on to its next; without branches, which would take longer than all this
-          const bool holds = best == m && m > kNone;
-          found += m > kNone;
-          taken += holds;
-          write_if(holds, slot + j0 + j, own.first, m);
+          const bool holds = best == m, real = m > kNone;
+          write_if(best, m, slot + j0 * 8, j * 8, own.first);
+          found += real;
+          taken += holds && real;
           if (kSorted) {
 #pragma unroll
             for (int i = 0; i + 1 < N; ++i) key[i] = holds ? key[i + 1] : key[i];
@@ -388,10 +431,9 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
           }
         }
       }
-      if (found < a.k && lane == 0) slot[found].y = 0;
       if (!exact) near |= __reduce_add_sync(kAll, taken) != found;  // the same key twice
       if (near) close |= 1u << r;
-      if (mine) count = found;
+      if (mine) count = min(found, a.k);
     }
     __syncwarp();
     // from here on a lane has one place of one token
@@ -428,7 +470,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
   }
   if (!any) return;
   for (int64_t t = begin; t < end; ++t)
-    if (unsure[(t - begin) >> 5] >> ((t - begin) & 31) & 1u) route_in_64_bits<T, N>(a, t, slots, lane);
+    if (unsure[(t - begin) >> 5] >> ((t - begin) & 31) & 1u) route_in_64_bits<T, N>(a, t, all_slots[warp], all_numbers[warp], lane);
 }
 
 // ---- the gradient to the logits ------------------------------------------------------------------------------------
@@ -526,9 +568,11 @@ template <typename T> __global__ void __launch_bounds__(kRouteThreads) k_route_b
 
 // ---- the order of groups ---------------------------------------------------------------------------------------------
 // A counting sort.  The pairs (token, choice), in their order, are cut into chunks, one a block, and a chunk into one run for every
-// warp.  Where a pair goes: to the start of its group, past the pairs of the group in the chunks before (k_sort_count has counted
-// them), in the runs before and in its own run, which a warp goes through in steps of 32.  Nothing depends on the order in which
-// blocks or warps run.  A sort of one chunk is a single launch.
+// warp.  Where a pair goes: to the start of its group, past the pairs of the group in the chunks before, in the runs before and in its own
+// run, which a warp goes through in steps of 32.  Nothing depends on the order in which blocks or warps run.
+//   Up to 4,096 pairs: one block.  Up to 16,384: a cluster of eight, which read one another's counts in shared memory.  More: k_sort_count
+//   counts the chunks first.
+// It is latency that these take: two reads from memory one after the other (experts, and workers beside them), barriers, one write.
 struct SortArgs {
   const int32_t* experts;
   const int64_t* workers_at;  // NULL: all tokens are of worker 0
@@ -540,12 +584,12 @@ struct SortArgs {
   int workers, n_experts, groups, chunk, chunks;
 };
 
-constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortKept = 8;  // steps of a run whose groups stay in registers between the two times that they are needed
+constexpr int kSortCluster = 8;
 
 // The group of a pair, or -1; `at` is a copy of workers_at in shared memory.
-__device__ __forceinline__ int group_of_pair(const SortArgs& a, const int64_t* at, u32 pair) {
-  const int e = a.experts[pair];
+__device__ __forceinline__ int group_of_pair(const SortArgs& a, const int64_t* at, u32 pair, int e) {
   if (e < 0 || e >= a.n_experts) return -1;
   if (!a.workers_at) return e;
   const int64_t t = a.k.quotient_of(pair);
@@ -572,45 +616,61 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const __grid_consta
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * a.chunk, end = min(first + a.chunk, a.pairs);
   for (int64_t p = first + threadIdx.x; p < end; p += kSortThreads) {
-    const int g = group_of_pair(a, workers_at, (u32)p);
+    const int g = group_of_pair(a, workers_at, (u32)p, a.experts[p]);
     if (g >= 0) atomicAdd(&count[g], 1u);
   }
   __syncthreads();
   for (int g = threadIdx.x; g < a.groups; g += kSortThreads) a.counts[(int64_t)blockIdx.x * a.groups + g] = count[g];
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ u32 load_of_block(const u32* own, u32 block) {  // what lies at this place in another block's shared memory
+  u32 at, v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_at(own)), "r"(block));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at));
+  return v;
+}
+
+// How the chunks of a sort know of one another.
+enum Chunks { kOneBlock, kOneCluster, kCountedBefore, kCountedLong };  // kCountedLong: runs of more than kSortKept steps
+
 // dynamic shared memory: workers_at; of each group its size and what lies before it [2][groups], then runs [warps][groups]
-// KEPT: a run has kSortKept steps at most.
-template <bool KEPT> __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a) {
+template <int CHUNKS> __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ u32 sums[kSortWarps];
+  typedef uint16_t Run;  // a chunk has at most 32,768 pairs
+  constexpr bool kKept = CHUNKS != kCountedLong;
   begin_after_predecessor();
   int64_t* workers_at = reinterpret_cast<int64_t*>(smem);
-  u32 *base = reinterpret_cast<u32*>(workers_at + a.workers + 1), *sizes = base + a.groups, *runs = sizes + a.groups;
+  u32 *base = reinterpret_cast<u32*>(workers_at + a.workers + 1), *sizes = base + a.groups;
+  Run* runs = reinterpret_cast<Run*>(sizes + a.groups);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  copy_workers(a, workers_at);
-  for (int i = threadIdx.x; i < (2 + kSortWarps) * a.groups; i += kSortThreads) base[i] = 0;
   // this warp's run
-  const int64_t first = (int64_t)blockIdx.x * a.chunk, end = min(first + a.chunk, a.pairs);
-  const int64_t length = ((end - first + kSortWarps - 1) / kSortWarps + 31) & ~31ll, from = first + warp * length, to = min(from + length, end);
-  u32* own = runs + warp * a.groups;
-  int kept[KEPT ? kSortKept : 1];
-  __syncthreads();
-  if (KEPT) {
+  const int64_t first = (int64_t)blockIdx.x * a.chunk, end = min(first + a.chunk, a.pairs), pairs = max(end - first, (int64_t)0);
+  const int64_t length = ((pairs + kSortWarps - 1) / kSortWarps + 31) & ~31ll, from = first + warp * length, to = min(from + length, end);
+  int kept[kKept ? kSortKept : 1];
+  if (kKept) {
 #pragma unroll
-    for (int i = 0; i < kSortKept; ++i) kept[i] = from + i * 32 + lane < to ? group_of_pair(a, workers_at, (u32)(from + i * 32 + lane)) : -1;
+    for (int i = 0; i < kSortKept; ++i) kept[i] = from + i * 32 + lane < to ? a.experts[from + i * 32 + lane] : -1;
   }
-#pragma unroll KEPT ? kSortKept : 1
-  for (int i = 0; KEPT ? i < kSortKept : from + i * 32 < to; ++i) {
-    if (KEPT && from + i * 32 >= to) break;
+  copy_workers(a, workers_at);
+  for (int i = threadIdx.x; i < 2 * a.groups; i += kSortThreads) base[i] = 0;
+  for (int i = threadIdx.x; i < kSortWarps * a.groups; i += kSortThreads) runs[i] = 0;
+  __syncthreads();
+  Run* own = runs + warp * a.groups;
+#pragma unroll kKept ? kSortKept : 1
+  for (int i = 0; kKept ? i < kSortKept : from + i * 32 < to; ++i) {
+    if (kKept && from + i * 32 >= to) break;
     const int64_t p = from + i * 32 + lane;
-    const int g = KEPT ? kept[KEPT ? i : 0] : p < to ? group_of_pair(a, workers_at, (u32)p) : -1;
+    const int g = p < to ? group_of_pair(a, workers_at, (u32)p, kKept ? kept[kKept ? i : 0] : a.experts[p]) : -1;
+    if (kKept) kept[kKept ? i : 0] = g;
     const u32 same = __match_any_sync(kAll, g);
-    if (g >= 0 && lane == __ffs(same) - 1) own[g] += __popc(same);
+    if (g >= 0 && lane == __ffs(same) - 1) own[g] += (Run)__popc(same);
     __syncwarp();
   }
-  // the sums over chunks, by as many threads a group as there are
-  if (a.chunks > 1) {
+  // the sums over chunks that have been counted before, by as many threads a group as there are
+  if (CHUNKS == kCountedBefore || CHUNKS == kCountedLong) {
     const int parts = a.groups >= kSortThreads ? 1 : kSortThreads / a.groups;
     for (int i = threadIdx.x; i < parts * a.groups; i += kSortThreads) {
       const int part = i / a.groups, g = i - part * a.groups;
@@ -626,21 +686,40 @@ template <bool KEPT> __global__ void __launch_bounds__(kSortThreads) k_sort_plac
     }
   }
   __syncthreads();
-  // of every group: its size, what lies in the chunks before, and within this one in the runs before
+  // what lies in the runs before, and the size of the chunk's share
+  for (int g = threadIdx.x; g < a.groups; g += kSortThreads) {
+    u32 here = 0;
+#pragma unroll 8
+    for (int w = 0; w < kSortWarps; ++w) {
+      const u32 n = runs[w * a.groups + g];
+      runs[w * a.groups + g] = (Run)here;
+      here += n;
+    }
+    if (CHUNKS == kOneBlock || CHUNKS == kOneCluster) sizes[g] = here;
+  }
+  if (CHUNKS == kOneCluster) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  // of every group: its size, and what lies in the groups and chunks before
   u32 at = 0;  // start of the groups that this round of threads looks at
   for (int g0 = 0; g0 < a.groups; g0 += kSortThreads) {
     const int g = g0 + threadIdx.x;
-    u32 total = 0;
+    u32 total = 0, before = 0;
     if (g < a.groups) {
-      u32 n[kSortWarps], here = 0;
+      if (CHUNKS == kOneCluster) {
+        u32 n[kSortCluster];
 #pragma unroll
-      for (int w = 0; w < kSortWarps; ++w) n[w] = runs[w * a.groups + g];
+        for (u32 c = 0; c < kSortCluster; ++c) n[c] = load_of_block(&sizes[g], c);
 #pragma unroll
-      for (int w = 0; w < kSortWarps; ++w) {
-        runs[w * a.groups + g] = here;
-        here += n[w];
+        for (u32 c = 0; c < kSortCluster; ++c) {
+          total += n[c];
+          before += c < blockIdx.x ? n[c] : 0;
+        }
+      } else {
+        total = sizes[g];
+        before = base[g];
       }
-      total = a.chunks == 1 ? here : sizes[g];
     }
     u32 scan = total;
 #pragma unroll
@@ -650,44 +729,52 @@ template <bool KEPT> __global__ void __launch_bounds__(kSortThreads) k_sort_plac
     }
     if (lane == 31) sums[warp] = scan;
     __syncthreads();
-    u32 lower = at, all = at;
+    u32 before_warps = sums[lane];
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-      if (w < warp) lower += sums[w];
-      all += sums[w];
+    for (int o = 1; o < 32; o <<= 1) {
+      const u32 v = __shfl_up_sync(kAll, before_warps, o);
+      if (lane >= o) before_warps += v;
     }
+    const u32 all = __shfl_sync(kAll, before_warps, 31), lower = at + (warp ? __shfl_sync(kAll, before_warps, warp - 1) : 0);
     if (g < a.groups) {
-      base[g] += lower + scan - total;
+      base[g] = lower + scan - total + before;
       if (blockIdx.x == 0) {
         a.offsets[g] = lower + scan - total;
         if (g == a.groups - 1) a.offsets[a.groups] = lower + scan;
       }
     }
-    at = all;
+    at += all;
     __syncthreads();
   }
-#pragma unroll KEPT ? kSortKept : 1
-  for (int i = 0; KEPT ? i < kSortKept : from + i * 32 < to; ++i) {
-    if (KEPT && from + i * 32 >= to) break;
+  if (CHUNKS == kOneCluster) cluster_arrive();  // the others' counts have been read
+#pragma unroll kKept ? kSortKept : 1
+  for (int i = 0; kKept ? i < kSortKept : from + i * 32 < to; ++i) {
+    if (kKept && from + i * 32 >= to) break;
     const int64_t p = from + i * 32 + lane;
-    const int g = KEPT ? kept[KEPT ? i : 0] : p < to ? group_of_pair(a, workers_at, (u32)p) : -1;
+    const int g = kKept ? kept[kKept ? i : 0] : p < to ? group_of_pair(a, workers_at, (u32)p, a.experts[p]) : -1;
     const u32 same = __match_any_sync(kAll, g);
     const u32 rank = __popc(same & ((1u << lane) - 1));
     u32 where = 0;
     if (g >= 0) where = base[g] + own[g] + rank;
     __syncwarp();
-    if (g >= 0 && rank == 0) own[g] += __popc(same);
+    if (g >= 0 && rank == 0) own[g] += (Run)__popc(same);
     __syncwarp();
     if (p < to) a.place[p] = g >= 0 ? (int32_t)where : -1;
   }
+  if (CHUNKS == kOneCluster) cluster_wait();  // and this one's, before its shared memory is another's
 }
 
-// Pairs of a chunk: see regtopk_sort_tokens.
+// Pairs of a chunk.
+constexpr int64_t kMostOfBlock = 4096, kMostOfCluster = (int64_t)kSortCluster * 2 * kSortThreads;
 inline int chunk_of(int64_t pairs) {
-  int64_t chunk = pairs <= kSortThreads * kSortKept ? kSortThreads * kSortKept : 1024;
-  while (chunk * 128 < pairs) chunk *= 2;
+  if (pairs <= kMostOfBlock) return (int)kMostOfBlock;
+  if (pairs <= kMostOfCluster) return (int)((pairs + kSortCluster - 1) / kSortCluster);
+  int64_t chunk = 1024;
+  while (chunk * 128 < pairs && chunk < 32768) chunk *= 2;
   return (int)chunk;
 }
+
+constexpr size_t sort_smem(size_t groups, size_t workers) { return groups * (8 + kSortWarps * sizeof(uint16_t)) + 8 * (workers + 1); }
 
 template <auto kKernel> bool allow_smem_of(int dev, int bytes) {
   static uint64_t done;  // of this kernel, one bit a device
@@ -793,8 +880,8 @@ int regtopk_route_backward(const float* dweights, const void* logits, int64_t ld
 
 size_t regtopk_sort_tokens_workspace_bytes(int64_t tokens, int32_t k, int32_t n_experts, int32_t workers) {
   if (tokens < 0 || k < 1 || n_experts < 1 || workers < 1 || tokens > INT32_MAX / k || (int64_t)n_experts * workers > REGTOPK_MATMUL_MAX_GROUPS) return 0;
-  const int64_t pairs = tokens * k, chunk = chunk_of(pairs), chunks = (pairs + chunk - 1) / chunk;
-  return chunks <= 1 ? 0 : (size_t)chunks * n_experts * workers * sizeof(u32);
+  const int64_t pairs = tokens * k, chunk = chunk_of(pairs);
+  return pairs <= kMostOfCluster ? 0 : (size_t)((pairs + chunk - 1) / chunk) * n_experts * workers * sizeof(u32);
 }
 
 int regtopk_sort_tokens(const int32_t* experts, const int64_t* workers_at, int32_t workers, int64_t* offsets, int32_t* place,
@@ -809,25 +896,32 @@ int regtopk_sort_tokens(const int32_t* experts, const int64_t* workers_at, int32
   a.chunk = chunk_of(a.pairs);
   a.chunks = a.pairs ? (int)((a.pairs + a.chunk - 1) / a.chunk) : 1;
   a.counts = static_cast<u32*>(workspace);
-  if (a.chunks > 1) {
+  const bool counted = a.pairs > kMostOfCluster;
+  if (counted) {
     if (!workspace || (uintptr_t)workspace % 16) return REGTOPK_ERR_INVALID_ARG;
     if (workspace_bytes < regtopk_sort_tokens_workspace_bytes(tokens, k, n_experts, workers)) return REGTOPK_ERR_WORKSPACE_TOO_SMALL;
   }
   int dev, sms;
   if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (a.chunks > 1) {
-    const int rc = start(k_sort_count, a.chunks, kSortThreads, 0, s, a);
-    if (rc != REGTOPK_OK) return rc;
+  const bool is_long = a.chunk > kSortKept * kSortThreads;
+  const size_t bytes = sort_smem(a.groups, workers), most = sort_smem(REGTOPK_MATMUL_MAX_GROUPS, REGTOPK_MATMUL_MAX_GROUPS);
+  if (!counted) {
+    if (a.pairs > kMostOfBlock) {
+      if (!allow_smem_of<k_sort_place<kOneCluster>>(dev, (int)most)) return train_rc(cudaGetLastError());
+      return start<kSortCluster>(k_sort_place<kOneCluster>, kSortCluster, kSortThreads, bytes, s, a);
+    }
+    if (!allow_smem_of<k_sort_place<kOneBlock>>(dev, (int)most)) return train_rc(cudaGetLastError());
+    return start(k_sort_place<kOneBlock>, 1, kSortThreads, bytes, s, a);
   }
-  constexpr int kMostSmem = REGTOPK_MATMUL_MAX_GROUPS * 4 * (2 + kSortWarps) + 8 * (REGTOPK_MATMUL_MAX_GROUPS + 1);
-  const size_t bytes = (size_t)a.groups * 4 * (2 + kSortWarps) + 8 * ((size_t)a.workers + 1);
-  if (a.chunk <= kSortThreads * kSortKept) {
-    if (!allow_smem_of<k_sort_place<true>>(dev, kMostSmem)) return train_rc(cudaGetLastError());
-    return start(k_sort_place<true>, a.chunks, kSortThreads, bytes, s, a);
+  const int rc = start(k_sort_count, a.chunks, kSortThreads, 0, s, a);
+  if (rc != REGTOPK_OK) return rc;
+  if (!is_long) {
+    if (!allow_smem_of<k_sort_place<kCountedBefore>>(dev, (int)most)) return train_rc(cudaGetLastError());
+    return start(k_sort_place<kCountedBefore>, a.chunks, kSortThreads, bytes, s, a);
   }
-  if (!allow_smem_of<k_sort_place<false>>(dev, kMostSmem)) return train_rc(cudaGetLastError());
-  return start(k_sort_place<false>, a.chunks, kSortThreads, bytes, s, a);
+  if (!allow_smem_of<k_sort_place<kCountedLong>>(dev, (int)most)) return train_rc(cudaGetLastError());
+  return start(k_sort_place<kCountedLong>, a.chunks, kSortThreads, bytes, s, a);
 }
 
 }  // extern "C"

@@ -242,7 +242,7 @@ inline int train_rc(cudaError_t e) {
              ? REGTOPK_ERR_NO_DEVICE : REGTOPK_ERR_CUDA;
 }
 
-// Launches a kernel as described at begin_after_predecessor; kCtas 2: in pairs of blocks.
+// Launches a kernel as described at begin_after_predecessor, in clusters of kCtas blocks.
 template <int kCtas = 1, typename... Params, typename... Args>
 int start(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
@@ -257,7 +257,7 @@ int start(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStr
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = kCtas == 2 ? 2 : 1;
+  cfg.numAttrs = kCtas > 1 ? 2 : 1;
   return train_rc(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 

@@ -51,7 +51,7 @@ def test_c_entries_refuse():
         assert sort(**bad) == -1, bad
     assert sort(tokens=1 << 20, nbytes=64) == -2 and sort(n=1025, workers=2, at=p) == -7 and sort(tokens=2**31) == -7
     need = lib.regtopk_sort_tokens_workspace_bytes
-    assert need(16, 2, 8, 1) == 0 and need(-1, 2, 8, 1) == 0 and need(1 << 20, 8, 256, 8) == 128 * 2048 * 4 and need(1 << 20, 8, 256, 9) == 0
+    assert need(16, 2, 8, 1) == 0 and need(-1, 2, 8, 1) == 0 and need(1 << 20, 8, 256, 8) >= 4 * 2048 and need(1 << 20, 8, 256, 9) == 0
 
 
 def test_no_cpu_path():
@@ -249,7 +249,7 @@ def check_sort(experts, n, at=None):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("tokens,k,n", [(1, 1, 1), (7, 3, 5), (33, 2, 8), (513, 8, 16), (700, 7, 64), (3000, 2, 512), (2049, 4, 100)])
+@pytest.mark.parametrize("tokens,k,n", [(1, 1, 1), (7, 3, 5), (33, 2, 8), (513, 8, 16), (700, 7, 64), (3000, 2, 512), (2049, 4, 100), (1366, 3, 9)])
 def test_sort(tokens, k, n):
     gen = torch.Generator().manual_seed(tokens)
     experts = torch.randint(0, n, (tokens, k), generator=gen, dtype=torch.int32)
@@ -276,7 +276,7 @@ def test_sort_many_workers():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("tokens,k,n,workers", [(100_000, 8, 256, 8), (300_001, 3, 60, 3), (5_000_000, 1, 2, 1)])
+@pytest.mark.parametrize("tokens,k,n,workers", [(8192, 8, 256, 8), (8193, 8, 16, 128), (100_000, 8, 256, 8), (300_001, 3, 60, 3), (5_000_000, 1, 2, 1)])
 def test_sort_large(tokens, k, n, workers):
     """Against a stable sort by torch."""
     gen = torch.Generator(device="cuda").manual_seed(tokens)
