@@ -132,14 +132,18 @@ __device__ __forceinline__ double reciprocal_64(double x) {
 
 constexpr int kMostShare = 4096;  // tokens of a warp
 
-// A whole token in binary64, for the few whose numbers lie too close for binary32.  slots and numbers: room for k and n_experts.  Short
-// loops: what such a token costs is the time that a warp alone takes, of which the fetching of instructions is a good part.
+// A token once more in binary64, for the few whose numbers lie too close for binary32.  slots and numbers: room for k and n_experts.
 // The largest are looked for among the numbers rounded to binary32, which keeps their order; where several round to the same, the numbers
 // themselves decide.
+// What such a token costs is the time that a warp alone takes, binary64's operations above all.  So k_route leaves in the token's first
+// expert the lanes whose groups remain, and in its first weight a number that the k largest reach: only what may reach it, in binary32, is
+// worked out in binary64.  No lanes: it is not certain which groups remain, and everything is.
 template <typename T, int N>
 __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int* slots, double* numbers, int lane) {
   const T* row = static_cast<const T*>(a.logits) + t * a.ld;
   const Share own(a, lane);
+  const u32 lanes = (u32)a.experts[t * a.k];
+  const float reached = lanes ? a.weights[t * a.k] : -INFINITY;
   float l[N], most = -INFINITY;
   read_logits<T, N>(l, row, own, a.wide);
   bool bad = false;
@@ -149,7 +153,7 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
     bad |= !(l[i] <= FLT_MAX);
   }
   bad = __any_sync(kAll, bad);
-  const bool scored = a.bias || (a.groups > 1 && a.top == 2);
+  const bool judged = a.groups > 1 && a.top == 2, scored = a.bias || (judged && !lanes);
   double total = 1.0, per_total = 1.0;
   if (!a.sigmoid && (scored || !a.renormalise)) {
     most = warp_max(most);
@@ -159,31 +163,41 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
     total = warp_sum(total);
     per_total = reciprocal_64(total);
   }
+  u32 todo = 0;  // of this lane's experts
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float c = l[i];
+    if (a.bias) {
+      const float s = a.sigmoid ? reciprocal_fast(1.0f + exp2_fast(c * -kLog2E)) : exp2_fast((c - most) * kLog2E) * (float)per_total;
+      c = s + (i < own.count ? a.bias[own.first + i] : 0.0f);
+    }
+    if (l[i] != -INFINITY && !(c < reached) && (!lanes || (lanes >> lane & 1u))) todo |= 1u << i;
+  }
   double t1 = -INFINITY, t2 = -INFINITY;  // of this lane, then of its group
-#pragma unroll 2
-  for (int i = 0; i < own.count; ++i) {
-    const float logit = to_float(row[own.first + i]);
+  u32 key[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) key[i] = 0;
+  for (; __any_sync(kAll, todo); todo &= todo - 1) {
+    if (!todo) continue;
+    const int at = __ffs(todo) - 1;
+    const float logit = to_float(row[own.first + at]);
     double s = logit, c = logit;
     if (scored) {
       const double e = exp_64(a.sigmoid ? -fabs(s) : s - (double)most), r = a.sigmoid ? reciprocal_64(1.0 + e) : per_total;
       s = a.sigmoid && logit >= 0.0f ? r : e * r;
-      if (a.bias) c = s = s + (double)a.bias[own.first + i];
+      if (a.bias) c = s = s + (double)a.bias[own.first + at];
     }
-    if (logit == -INFINITY) c = -INFINITY;
+    numbers[own.first + at] = c;
     if (c == -INFINITY) s = -INFINITY;
     else if (s != s) s = -DBL_MAX;
-    numbers[own.first + i] = c;
+    const u32 k = c == -INFINITY ? 0u : c != c ? 1u : ordered((float)c + 0.0f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = i == at ? k : key[i];
     t2 = fmax(t2, fmin(t1, s));
     t1 = fmax(t1, s);
   }
   const double* c = numbers + own.first;
-  u32 key[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const double v = i < own.count ? c[i] : -INFINITY;
-    key[i] = v == -INFINITY ? 0u : v != v ? 1u : ordered((float)v + 0.0f);
-  }
-  if (a.groups > 1) {
+  if (a.groups > 1 && !lanes) {
     for (int o = 1; o < a.lanes; o <<= 1) {
       const double o1 = __shfl_xor_sync(kAll, t1, o), o2 = __shfl_xor_sync(kAll, t2, o);
       t2 = fmax(fmin(t1, o1), fmax(t2, o2));
@@ -206,19 +220,20 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
     for (int i = 1; i < N; ++i) best = max(best, key[i]);
     const u32 m = __reduce_max_sync(kAll, best);
     if (m == 0) break;
-    int at = -1, same = 0;  // this lane's first with that key, and how many it has
+    int at = -1;
+    u32 open = 0;  // this lane's with that key, and the first of them
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) {
-      same += key[i] == m;
+      open |= key[i] == m ? 1u << i : 0u;
       at = key[i] == m ? i : at;
     }
     u32 holders = __ballot_sync(kAll, at >= 0);
-    if (m != 1u && __any_sync(kAll, same > 1 || (holders & (holders - 1)))) {
+    if (m != 1u && __any_sync(kAll, (open & (open - 1)) || (holders & (holders - 1)))) {
       double largest = -INFINITY;
       if (at >= 0) {
 #pragma unroll 1
         for (int i = 0; i < own.count; ++i)
-          if (c[i] > largest && ordered((float)c[i] + 0.0f) == m) {
+          if (open >> i & 1u && c[i] > largest && ordered((float)c[i] + 0.0f) == m) {
             largest = c[i];
             at = i;
           }
@@ -230,7 +245,6 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
     }
     if (lane == __ffs(holders) - 1) {
       slots[found] = own.first + at;
-      numbers[own.first + at] = -INFINITY;
 #pragma unroll
       for (int i = 0; i < N; ++i) key[i] = i == at ? 0u : key[i];
     }
@@ -276,9 +290,9 @@ __device__ __forceinline__ void write_if(u32 a, u32 y, u32 to, int offset, int x
   asm volatile("{\n.reg .pred p;\nsetp.eq.u32 p, %0, %1;\n@p st.shared.v2.b32 [%2], {%3, %1};\n}" ::"r"(a), "r"(y), "r"(to + offset), "r"(x) : "memory");
 }
 
-// How experts are compared: by their logits (without bias: the order is the same), or by c.  With groups that are judged by two of their
-// scores these are needed all the same, and then c stands in for the logits' order: see `by_logit` in k_route.
-enum How { kByLogit, kBySoftmax, kBySigmoid };
+// How experts are compared: by their logits (without bias: the order is the same), or by c, a score and its bias.  Judged: by their logits, but
+// their groups by two scores.
+enum How { kByLogit, kBySoftmax, kBySigmoid, kJudgedBySoftmax, kJudgedBySigmoid };
 
 // A token's experts are found by k times taking the largest key of the warp.  A key is a number in the order of c whose low bits say
 // which of the lane's experts it belongs to, so that one reduction finds number and place; a lane keeps its keys sorted.
@@ -303,12 +317,13 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
   int2* all = all_found[warp];
   u32* unsure = all_unsure[warp];
   const Share own(a, lane);
-  const bool by_logit = HOW == kByLogit || !a.bias, exact = sizeof(T) == 2 && by_logit;
-  const u32 low_bits = exact ? 511u : (u32)(N - 1), pair_bits = HOW == kByLogit ? low_bits : (u32)(N - 1);
-  float bias[HOW == kByLogit ? 1 : N];
-  if (HOW != kByLogit) {
+  constexpr bool kSigmoid = HOW == kBySigmoid || HOW == kJudgedBySigmoid, kSoftmax = HOW == kBySoftmax || HOW == kJudgedBySoftmax;
+  constexpr bool by_logit = !(HOW == kBySoftmax || HOW == kBySigmoid), exact = sizeof(T) == 2 && by_logit;
+  constexpr u32 low_bits = exact ? 511u : (u32)(N - 1), pair_bits = HOW == kByLogit ? low_bits : (u32)(N - 1);
+  float bias[by_logit ? 1 : N];
+  if (!by_logit) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) bias[i] = a.bias && i < own.count ? a.bias[own.first + i] : 0.0f;
+    for (int i = 0; i < N; ++i) bias[by_logit ? 0 : i] = i < own.count ? a.bias[own.first + i] : 0.0f;
   }
   int64_t t0 = ((int64_t)blockIdx.x * kRouteWarps + warp) * a.share;
   const int64_t end = min(t0 + a.share, a.tokens);
@@ -321,6 +336,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
   __syncwarp();
   for (; t0 < end; t0 += a.batch) {
     int count = 0;           // this lane's token's: experts found,
+    u32 lanes = kAll;        // lanes whose groups remain,
     float most = 0.0f, total = 1.0f, margin = 0.0f;  // largest logit, sum of the exponentials, error of a difference of scores
     u32 close = 0;           // a bit a token
     for (int r = 0; r < a.batch; ++r) {
@@ -332,7 +348,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
       if (t + 1 < end) read_logits<T, N>(ahead, logits + (t + 1) * a.ld, own, a.wide);
       const bool mine = lane >> a.places_log2 == r;
       float top = 0.0f, sum = 1.0f, per_sum = 1.0f;
-      if (HOW == kBySoftmax || (HOW == kByLogit && !a.sigmoid && !a.renormalise)) {
+      if (kSoftmax || (!kSigmoid && !a.sigmoid && !a.renormalise)) {
         top = l[0];
 #pragma unroll
         for (int i = 1; i < N; ++i) top = fmaxf(top, l[i]);
@@ -344,7 +360,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
         per_sum = 1.0f / sum;
         if (mine) most = top, total = sum;
       }
-      const float apart = HOW == kByLogit ? 0.0f : HOW == kBySigmoid ? 0x1p-20f : 0x1p-18f * per_sum;
+      const float apart = HOW == kByLogit ? 0.0f : kSigmoid ? 0x1p-20f : 0x1p-18f * per_sum;
       if (mine) margin = apart;
       u32 key[N], pair1 = 0, pair2 = 0;  // pair: the keys of this lane's two largest scores, where experts are compared by other numbers
 #pragma unroll
@@ -352,19 +368,17 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
         float c = l[i];
         const u32 low = exact ? 511u - (u32)(own.first + i) & 511u : (u32)(N - 1 - i);  // behind the last expert it may wrap
         if (HOW != kByLogit) {
-          const float s = HOW == kBySigmoid ? reciprocal_fast(1.0f + exp2_fast(c * -kLog2E)) : exp2_fast((c - top) * kLog2E) * per_sum;
-          const float biased = c == -INFINITY ? -INFINITY : s + bias[i];
+          const float s = kSigmoid ? reciprocal_fast(1.0f + exp2_fast(c * -kLog2E)) : exp2_fast((c - top) * kLog2E) * per_sum;
+          const float scored = c == -INFINITY ? -INFINITY : by_logit ? s : s + bias[by_logit ? 0 : i];
           if (by_logit) {
-            const u32 k = ordered(biased) & ~pair_bits;
+            const u32 k = ordered(scored) & ~pair_bits;
             pair2 = max(pair2, min(pair1, k));
             pair1 = max(pair1, k);
-            c += 0.0f;
           } else {
-            c = biased;
+            c = scored;
           }
-        } else {
-          c += 0.0f;
         }
+        if (by_logit) c += 0.0f;
         key[i] = (ordered(c) & ~low_bits) | low;
       }
       if (kSorted) sort_descending<N>(key);
@@ -388,7 +402,8 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
           pair1 = max(pair1, o1);
         }
         const float t1 = unordered(pair1 & ~pair_bits), t2 = unordered(pair2 & ~pair_bits);
-        const float strength = pair1 <= kNone ? -INFINITY : (HOW != kByLogit && a.top == 2 && pair2 > kNone ? t1 + t2 : t1) + 0.0f;
+        const bool two = HOW != kByLogit && a.top == 2 && pair2 > kNone;
+        const float strength = pair1 <= kNone ? -INFINITY : (two ? t1 + t2 : t1) + 0.0f;
         u32 group = own.group < a.groups ? (ordered(strength) & ~31u) | (31u - own.group) : 0u, last = 0;
         bool kept = false;
         for (int g = 0; g < a.kept; ++g) {
@@ -398,10 +413,14 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
         }
         if (!(exact && HOW == kByLogit) && a.kept < a.groups) {
           const float v = unordered(last & ~31u), w = unordered(__reduce_max_sync(kAll, group) & ~31u);
-          near = w > -INFINITY && !(v - w > fmaf(0x1p-23f * (32 + 2 * N), fabsf(v) + fabsf(w), 2.0f * apart));
+          const float size = pair1 <= kNone ? 0.0f : fabsf(t1) + (two ? fabsf(t2) : 0.0f);  // two scores may cancel
+          const float most_size = __uint_as_float(__reduce_max_sync(kAll, __float_as_uint(size)));
+          near = w > -INFINITY && !(v - w > fmaf(0x1p-22f * (32 + 2 * N), most_size, 2.0f * apart));
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) key[i] = kept ? key[i] : 0u;
+        const u32 those = near ? 0u : __ballot_sync(kAll, kept);
+        if (mine) lanes = those;
       }
       // the k largest keys and the one after them, four at a time.  The lane that holds one writes it down and goes on to its next; without
       // branches, which would take longer than all this.  What is no expert is written down too.
@@ -453,18 +472,31 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
       }
     }
     near |= (close >> r & 1u) != 0;
-    if (__any_sync(kAll, near)) {
+    const u32 all_near = __ballot_sync(kAll, near);
+    if (all_near) {
       any = true;
       if (near && t < end) atomicOr(&unsure[(t - begin) >> 5], 1u << ((t - begin) & 31));
+      if (all_near >> (r << a.places_log2) & (0xFFFFFFFFu >> (32 - places))) near = true;
     }
     const bool there = j < count;
     const float logit = there ? to_float(logits[t * a.ld + e]) : 0.0f;
     float w = weight_of(a, logit, there, places, most, total);
     // a NaN or an infinity anywhere makes the scores of a softmax NaN
-    if (!a.sigmoid && (HOW == kBySoftmax ? total != total : first >= kInfinite)) w = __uint_as_float(0x7FC00000u);
+    if (!a.sigmoid && (kSoftmax ? total != total : first >= kInfinite)) w = __uint_as_float(0x7FC00000u);
     if (j < a.k && r < a.batch && t < end) {
+      w = there ? w * a.scale : 0.0f;
+      if (near && j == 0) {  // what route_in_64_bits goes on from
+        const bool strange = first > (kInfinite | low_bits);  // a NaN, which came first here and comes last there
+        e = strange ? 0 : (int)lanes;
+        w = -INFINITY;
+        if (count == a.k && !strange) {
+          const float v = unordered((u32)all[r * (places + 1) + a.k - 1].y & ~low_bits);
+          w = v - fmaf(N * 0x1p-21f, fabsf(v), 2.0f * margin);
+          if (!(w == w)) w = -INFINITY;
+        }
+      }
       a.experts[t * a.k + j] = e;
-      a.weights[t * a.k + j] = there ? w * a.scale : 0.0f;
+      a.weights[t * a.k + j] = w;
     }
     __syncwarp();
   }
@@ -796,8 +828,10 @@ template <typename T, int N> int launch_route(RouteArgs& a, int sms, cudaStream_
   a.batch = 1;
   while (a.batch << a.places_log2 < 32 && a.batch < 8 && a.batch < each) a.batch *= 2;
   const unsigned grid = (unsigned)((a.tokens + each * kRouteWarps - 1) / (each * kRouteWarps));
-  if (a.bias || (a.groups > 1 && a.top == 2))
+  if (a.bias)
     return a.sigmoid ? start(k_route<T, N, kBySigmoid>, grid, kRouteThreads, 0, s, a) : start(k_route<T, N, kBySoftmax>, grid, kRouteThreads, 0, s, a);
+  if (a.groups > 1 && a.top == 2)
+    return a.sigmoid ? start(k_route<T, N, kJudgedBySigmoid>, grid, kRouteThreads, 0, s, a) : start(k_route<T, N, kJudgedBySoftmax>, grid, kRouteThreads, 0, s, a);
   return start(k_route<T, N, kByLogit>, grid, kRouteThreads, 0, s, a);
 }
 template <typename T> int launch_route_of(RouteArgs& a, int sms, cudaStream_t s) {

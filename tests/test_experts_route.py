@@ -95,6 +95,30 @@ def test_route(tokens, experts, k, groups, kept, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("experts,k,groups,kept", [(256, 8, 8, 4), (256, 8, 2, 1), (64, 6, 1, 1), (128, 3, 4, 2), (100, 8, 1, 1), (8, 2, 1, 1), (96, 4, 3, 2), (32, 1, 1, 1)])
+def test_route_of_many_tokens(experts, k, groups, kept, dtype):
+    """Enough tokens for the kernel that takes four at a time: ordinary ones, and with ties, neighbours, masks and NaN among them."""
+    gen = torch.Generator().manual_seed(experts + k)
+    tokens = 2501
+    logits = (1.5 * torch.randn(tokens, experts, generator=gen)).to(dtype)
+    logits[100:160] = (torch.randint(-3, 3, (60, experts), generator=gen) / 4).to(dtype)
+    logits[200:260] = (logits[200:260].float().round() + torch.randint(0, 9, (60, experts), generator=gen) * 2.0 ** -22).to(dtype)
+    logits[300:320, : experts // 2] = -INF
+    logits[320:330] = -INF
+    logits[330:340, 1:] = -INF
+    logits[340] = torch.finfo(dtype).min
+    logits[341, :7] = 9.0  # one lane's
+    bias = (0.1 * torch.randn(experts, generator=gen)).cuda()
+    logits = logits.cuda()
+    for scores, b, top, renormalise in (("sigmoid", bias, 2, True), ("softmax", bias, 1, False), ("softmax", None, 2, True), ("sigmoid", None, 1, False), ("softmax", None, 1, False)):
+        check_route(logits, k, scores=scores, bias=b, groups=groups, groups_kept=kept, group_top=top, renormalise=renormalise, scale=2.5)
+    logits[400, experts - 1], logits[401, 0] = float("nan"), INF
+    e, w = rt.route(logits, k)
+    assert w[400:402].isnan().all() and w[402:].isfinite().all() and ((e[400:] >= 0) & (e[400:] < experts)).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_ties(scores, dtype):
