@@ -97,6 +97,22 @@ template <typename T, int KIND, bool GATED> __device__ __forceinline__ void forw
   }
 }
 
+template <typename T, int KIND, bool GATED, bool WHOLE>
+__device__ __forceinline__ void forward_apart(const ActArgs& a, int64_t row, int c0, int cols) {
+  const int lane = threadIdx.x & 31, first = c0 + lane, left = cols - first;
+  const T* from = static_cast<const T*>(a.a) + row * a.lda + first;
+  Octet x, u;
+  read_apart<T, WHOLE>(x, from, left);
+  if (GATED) read_apart<T, WHOLE>(u, from + cols, left);
+  if (a.values) {
+    uint8_t *values = a.values + row * a.ld_values + first, *scales = a.scales + row * a.ld_scales + (c0 >> 5);
+    store_rows8_apart<WHOLE>(x, values, scales, lane, left);
+    if (GATED) store_rows8_apart<WHOLE>(u, values + cols, scales + a.half_blocks, lane, left);
+  }
+  forward_of<T, KIND, GATED>(x, u);
+  store_apart<T, WHOLE>(x, static_cast<T*>(a.y) + row * a.ldy + first, left);
+}
+
 template <typename T, int KIND, bool GATED, bool VEC>
 __global__ void __launch_bounds__(kActThreads) k_activation(const __grid_constant__ ActArgs a) {
   begin_after_predecessor();
@@ -129,19 +145,9 @@ __global__ void __launch_bounds__(kActThreads) k_activation(const __grid_constan
     }
   } else {
     const Spot<false> at(a.at, first_piece<false>());
-    const int lane = threadIdx.x & 31;
     if (!at.there) return;
-    const T* row = static_cast<const T*>(a.a) + at.row * a.lda;
-    Octet x, u;
-    read_eight<T, false, false>(x, row, at.c0, lane, cols);
-    if (GATED) read_eight<T, false, false>(u, row + cols, at.c0, lane, cols);
-    if (a.values) {
-      uint8_t *values = a.values + at.row * a.ld_values, *scales = a.scales + at.row * a.ld_scales;
-      store_rows8_apart(x, values, scales, at.c0, lane, cols);
-      if (GATED) store_rows8_apart(u, values + cols, scales + a.half_blocks, at.c0, lane, cols);
-    }
-    forward_of<T, KIND, GATED>(x, u);
-    store_eight<T, false>(x, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, lane, cols);
+    if (cols - at.c0 >= 256) forward_apart<T, KIND, GATED, true>(a, at.row, at.c0, cols);
+    else forward_apart<T, KIND, GATED, false>(a, at.row, at.c0, cols);
   }
 }
 
@@ -162,12 +168,33 @@ template <typename T, int KIND, bool GATED> __device__ __forceinline__ void back
   }
 }
 
+template <typename T, int KIND, bool GATED, bool KEPT8, bool WHOLE>
+__device__ __forceinline__ void backward_apart(const ActArgs& a, int64_t row, int c0, int cols) {
+  const int lane = threadIdx.x & 31, first = c0 + lane, left = cols - first;
+  Octet d, x, u;
+  if (KEPT8) {
+    const uint8_t *from = static_cast<const uint8_t*>(a.a) + row * a.lda + first, *scales = a.in_scales + row * a.ld_in_scales + (c0 >> 5);
+    read_rows8_apart<WHOLE>(x, from, scales, lane, left);
+    if (GATED) read_rows8_apart<WHOLE>(u, from + cols, scales + a.half_blocks, lane, left);
+  } else {
+    const T* from = static_cast<const T*>(a.a) + row * a.lda + first;
+    read_apart<T, WHOLE>(x, from, left);
+    if (GATED) read_apart<T, WHOLE>(u, from + cols, left);
+  }
+  read_apart<T, WHOLE>(d, static_cast<const T*>(a.dy) + row * a.ld_dy + first, left);
+  backward_of<T, KIND, GATED>(x, u, d);
+  T* da = static_cast<T*>(a.da) + row * a.ld_da + first;
+  store_apart<T, WHOLE>(x, da, left);
+  if (GATED) store_apart<T, WHOLE>(u, da + cols, left);
+  if (a.y) store_apart<T, WHOLE>(d, static_cast<T*>(a.y) + row * a.ldy + first, left);
+}
+
 template <typename T, int KIND, bool GATED, bool KEPT8, bool VEC>
 __global__ void __launch_bounds__(kActThreads) k_activation_back(const __grid_constant__ ActArgs a) {
   begin_after_predecessor();
   const int cols = (int)a.at.cols;
-  Octet d, x, u;
   if constexpr (VEC) {
+    Octet d, x, u;
     Eight<T> in[kActStep], wide_x[KEPT8 ? 1 : kActStep], wide_u[KEPT8 ? 1 : kActStep];
     Packed8 packed_x[KEPT8 ? kActStep : 1], packed_u[KEPT8 ? kActStep : 1];
 #pragma unroll
@@ -216,23 +243,9 @@ __global__ void __launch_bounds__(kActThreads) k_activation_back(const __grid_co
     }
   } else {
     const Spot<false> at(a.at, first_piece<false>());
-    const int lane = threadIdx.x & 31;
     if (!at.there) return;
-    if (KEPT8) {
-      const uint8_t *row = static_cast<const uint8_t*>(a.a) + at.row * a.lda, *scales = a.in_scales + at.row * a.ld_in_scales;
-      read_rows8_apart(x, row, scales, at.c0, lane, cols);
-      if (GATED) read_rows8_apart(u, row + cols, scales + a.half_blocks, at.c0, lane, cols);
-    } else {
-      const T* row = static_cast<const T*>(a.a) + at.row * a.lda;
-      read_eight<T, false, false>(x, row, at.c0, lane, cols);
-      if (GATED) read_eight<T, false, false>(u, row + cols, at.c0, lane, cols);
-    }
-    read_eight<T, false, false>(d, static_cast<const T*>(a.dy) + at.row * a.ld_dy, at.c0, lane, cols);
-    backward_of<T, KIND, GATED>(x, u, d);
-    T* da = static_cast<T*>(a.da) + at.row * a.ld_da;
-    store_eight<T, false>(x, da, at.c0, lane, cols);
-    if (GATED) store_eight<T, false>(u, da + cols, at.c0, lane, cols);
-    if (a.y) store_eight<T, false>(d, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, lane, cols);
+    if (cols - at.c0 >= 256) backward_apart<T, KIND, GATED, KEPT8, true>(a, at.row, at.c0, cols);
+    else backward_apart<T, KIND, GATED, KEPT8, false>(a, at.row, at.c0, cols);
   }
 }
 
@@ -256,8 +269,9 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(kActThreads) k
   } else {
     const Spot<false> at(a.at, first_piece<false>());
     if (!at.there) return;
-    read_eight<T, false, false>(f, static_cast<const T*>(a.a) + at.row * a.lda, at.c0, threadIdx.x & 31, (int)a.at.cols);
-    store_rows8_apart(f, a.values + at.row * a.ld_values, a.scales + at.row * a.ld_scales, at.c0, threadIdx.x & 31, (int)a.at.cols);
+    const int lane = threadIdx.x & 31, first = at.c0 + lane, left = (int)a.at.cols - first;
+    read_apart<T, false>(f, static_cast<const T*>(a.a) + at.row * a.lda + first, left);
+    store_rows8_apart<false>(f, a.values + at.row * a.ld_values + first, a.scales + at.row * a.ld_scales + (at.c0 >> 5), lane, left);
   }
 }
 
@@ -283,8 +297,9 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(kActThreads) k
   } else {
     const Spot<false> at(a.at, first_piece<false>());
     if (!at.there) return;
-    read_rows8_apart(f, static_cast<const uint8_t*>(a.a) + at.row * a.lda, a.in_scales + at.row * a.ld_in_scales, at.c0, threadIdx.x & 31, (int)a.at.cols);
-    store_eight<T, false>(f, static_cast<T*>(a.y) + at.row * a.ldy, at.c0, threadIdx.x & 31, (int)a.at.cols);
+    const int lane = threadIdx.x & 31, first = at.c0 + lane, left = (int)a.at.cols - first;
+    read_rows8_apart<false>(f, static_cast<const uint8_t*>(a.a) + at.row * a.lda + first, a.in_scales + at.row * a.ld_in_scales + (at.c0 >> 5), lane, left);
+    store_apart<T, false>(f, static_cast<T*>(a.y) + at.row * a.ldy + first, left);
   }
 }
 

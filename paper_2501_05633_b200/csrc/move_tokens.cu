@@ -62,43 +62,50 @@ template <bool VEC> struct Piece {
   }
 };
 
+template <typename T, bool PACKED, bool WHOLE> __device__ __forceinline__ void spread_apart(const MoveArgs& a, int64_t token, int c0, int lane, int cols) {
+  const int first = c0 + lane, left = cols - first;
+  Octet f;
+  if (PACKED) read_rows8_apart<WHOLE>(f, static_cast<const uint8_t*>(a.in) + token * a.ld_in + first, a.in_scales + token * a.ld_scales + (c0 >> 5), lane, left);
+  else read_apart<T, WHOLE>(f, static_cast<const T*>(a.in) + token * a.ld_in + first, left);
+  for (int j = 0; j < a.k; ++j) {
+    const int32_t p = a.place[token * a.k + j];
+    if (in_rows(p, a.rows)) store_apart<T, WHOLE>(f, static_cast<T*>(a.out) + (int64_t)p * a.ld_out + first, left);
+  }
+}
+
 template <typename T, bool PACKED, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_spread(const __grid_constant__ MoveArgs a) {
   begin_after_predecessor();
   const Piece<VEC> at(a);
-  if (at.there) {
-    const int cols = (int)a.cols;
-    Octet f;
+  const int cols = (int)a.cols;
+  if (VEC && at.there) {
     Eight<T> v;
-    if (PACKED && VEC) {
+    if (PACKED) {
+      Octet f;
       Packed8 p;
       p.fetch(static_cast<const uint8_t*>(a.in) + at.token * a.ld_in + at.c0, a.in_scales + at.token * a.ld_scales + (at.c0 >> 5));
       p.get(f);
       v.put(f);
-    } else if (PACKED) {
-      read_rows8_apart(f, static_cast<const uint8_t*>(a.in) + at.token * a.ld_in, a.in_scales + at.token * a.ld_scales, at.c0, at.lane, cols);
-    } else if (VEC) v.fetch(static_cast<const T*>(a.in) + at.token * a.ld_in + at.c0);
-    else read_eight<T, VEC, false>(f, static_cast<const T*>(a.in) + at.token * a.ld_in, at.c0, at.lane, cols);
+    } else {
+      v.fetch(static_cast<const T*>(a.in) + at.token * a.ld_in + at.c0);
+    }
     const int32_t* place = a.place + at.token * a.k;
     for (int j = 0; j < a.k; ++j) {
       const int32_t p = place[j];
-      if (!in_rows(p, a.rows)) continue;
-      T* to = static_cast<T*>(a.out) + (int64_t)p * a.ld_out;
-      if (VEC) v.store(to + at.c0);
-      else store_eight<T, VEC>(f, to, at.c0, at.lane, cols);
+      if (in_rows(p, a.rows)) v.store(static_cast<T*>(a.out) + (int64_t)p * a.ld_out + at.c0);
     }
+  } else if (at.there) {
+    if (cols - at.c0 >= 256) spread_apart<T, PACKED, true>(a, at.token, at.c0, at.lane, cols);
+    else spread_apart<T, PACKED, false>(a, at.token, at.c0, at.lane, cols);
   }
   clear_tail<T, VEC>(a);
 }
 
 constexpr int kJoinStep = 4;  // rows under way
 
-template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_join(const __grid_constant__ MoveArgs a) {
-  begin_after_predecessor();
-  const Piece<VEC> at(a);
-  if (!at.there) return;
-  const int cols = (int)a.cols;
-  const int32_t* place = a.place + at.token * a.k;
-  const float* weights = a.weights + at.token * a.k;
+template <typename T, typename O, bool VEC, bool WHOLE> __device__ __forceinline__ void join_piece(const MoveArgs& a, int64_t token, int c0, int lane, int cols) {
+  const int first = c0 + lane, left = cols - first;
+  const int32_t* place = a.place + token * a.k;
+  const float* weights = a.weights + token * a.k;
   Octet sum;
 #pragma unroll
   for (int i = 0; i < 4; ++i) sum[i] = both(0.0f);
@@ -114,7 +121,10 @@ template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kM
 #pragma unroll
     for (int j = 0; j < kJoinStep; ++j) {
       const bool there = in_rows(p[j], a.rows);
-      read_eight<T, VEC, false>(f[j], static_cast<const T*>(a.in) + (there ? (int64_t)p[j] * a.ld_in : 0), at.c0, at.lane, there ? cols : 0);
+      const T* row = static_cast<const T*>(a.in) + (there ? (int64_t)p[j] * a.ld_in : 0);
+      if (VEC) read_eight<T, VEC, false>(f[j], row, c0, lane, there ? cols : 0);
+      else if (WHOLE && there) read_apart<T, true>(f[j], row + first, left);
+      else read_apart<T, false>(f[j], row + first, there ? left : 0);
       if (!there) w[j] = 0.0f;
     }
 #pragma unroll
@@ -124,11 +134,55 @@ template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kM
   }
   if (a.other) {
     Octet r;
-    read_eight<O, VEC, false>(r, static_cast<const O*>(a.other) + at.token * a.ld_other, at.c0, at.lane, cols);
+    const O* row = static_cast<const O*>(a.other) + token * a.ld_other;
+    if (VEC) read_eight<O, VEC, false>(r, row, c0, lane, cols);
+    else read_apart<O, WHOLE>(r, row + first, left);
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = add2(sum[i], r[i]);
   }
-  store_eight<O, VEC>(sum, static_cast<O*>(a.out) + at.token * a.ld_out, at.c0, at.lane, cols);
+  O* out = static_cast<O*>(a.out) + token * a.ld_out;
+  if (VEC) store_eight<O, VEC>(sum, out, c0, lane, cols);
+  else store_apart<O, WHOLE>(sum, out + first, left);
+}
+
+template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kMoveThreads) k_join(const __grid_constant__ MoveArgs a) {
+  begin_after_predecessor();
+  const Piece<VEC> at(a);
+  if (!at.there) return;
+  const int cols = (int)a.cols;
+  if (!VEC && cols - at.c0 >= 256) join_piece<T, O, VEC, true>(a, at.token, at.c0, at.lane, cols);
+  else join_piece<T, O, VEC, false>(a, at.token, at.c0, at.lane, cols);
+}
+
+// 256 columns of a token's dout and of STEP of its rows.
+template <typename T, typename D, bool VEC, int STEP, bool WHOLE>
+__device__ __forceinline__ void back_unit(const MoveArgs& a, int64_t t, const int64_t (&to)[STEP], const float (&w)[STEP], float (&dot)[STEP], int c0,
+                                          int lane, int cols) {
+  const int first = c0 + (VEC ? lane * 8 : lane), left = cols - first;
+  Octet d, f[STEP];
+  const D* dout = static_cast<const D*>(a.in) + t * a.ld_in;
+  if (VEC) read_eight<D, VEC, false>(d, dout, c0, lane, cols);
+  else read_apart<D, WHOLE>(d, dout + first, left);
+#pragma unroll
+  for (int j = 0; j < STEP; ++j) {
+    const T* row = static_cast<const T*>(a.other) + (to[j] < 0 ? 0 : to[j]) * a.ld_other;
+    if (VEC) read_eight<T, VEC, false>(f[j], row, c0, lane, to[j] < 0 ? 0 : cols);
+    else if (to[j] >= 0) read_apart<T, WHOLE>(f[j], row + first, left);
+  }
+#pragma unroll
+  for (int j = 0; j < STEP; ++j) {
+    if (to[j] < 0) continue;
+    float2 s = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s = fma2(f[j][i], d[i], s);
+      f[j][i] = mul2(d[i], both(w[j]));
+    }
+    dot[j] += s.x + s.y;
+    T* out = static_cast<T*>(a.out) + to[j] * a.ld_out;
+    if (VEC) store_eight<T, VEC>(f[j], out, c0, lane, cols);
+    else store_apart<T, WHOLE>(f[j], out + first, left);
+  }
 }
 
 // A team of warps a token: its warps share the row's units of 256 columns, and each has STEP of the token's rows under way beside
@@ -151,24 +205,10 @@ template <typename T, typename D, bool VEC, int STEP> __global__ void __launch_b
       dot[j] = 0.0f;
     }
     if (there) {
-      for (int c0 = member * 256; c0 < a.cols; c0 += a.team * 256) {
-        const int cols = (int)a.cols;
-        Octet d, f[STEP];
-        read_eight<D, VEC, false>(d, static_cast<const D*>(a.in) + t * a.ld_in, c0, lane, cols);
-#pragma unroll
-        for (int j = 0; j < STEP; ++j) read_eight<T, VEC, false>(f[j], static_cast<const T*>(a.other) + (to[j] < 0 ? 0 : to[j]) * a.ld_other, c0, lane, to[j] < 0 ? 0 : cols);
-#pragma unroll
-        for (int j = 0; j < STEP; ++j) {
-          float2 s = both(0.0f);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s = fma2(f[j][i], d[i], s);
-            f[j][i] = mul2(d[i], both(w[j]));
-          }
-          if (to[j] < 0) continue;
-          dot[j] += s.x + s.y;
-          store_eight<T, VEC>(f[j], static_cast<T*>(a.out) + to[j] * a.ld_out, c0, lane, cols);
-        }
+      const int cols = (int)a.cols;
+      for (int c0 = member * 256; c0 < cols; c0 += a.team * 256) {
+        if (!VEC && cols - c0 >= 256) back_unit<T, D, VEC, STEP, true>(a, t, to, w, dot, c0, lane, cols);
+        else back_unit<T, D, VEC, STEP, false>(a, t, to, w, dot, c0, lane, cols);
       }
     }
 #pragma unroll

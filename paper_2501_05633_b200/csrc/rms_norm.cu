@@ -80,7 +80,7 @@ __global__ void __maxnreg__(U <= 2 ? 80 : 128) k_rms(const __grid_constant__ Rms
       if (a.values) {
         uint8_t *values = a.values + row * a.ld_values, *scales = a.scales + row * a.ld_scales;
         if (VEC) store_rows8(f[u], values + c0 + t.lane * 8, scales + ((c0 + t.lane * 8) >> 5), c0 + t.lane * 8 < a.cols);
-        else store_rows8_apart(f[u], values, scales, c0, t.lane, a.cols);
+        else store_rows8_apart<false>(f[u], values + c0 + t.lane, scales + (c0 >> 5), t.lane, a.cols - c0 - t.lane);
       }
     }
   }

@@ -67,11 +67,23 @@ __device__ __forceinline__ void store_rows8(const Octet& given, uint8_t* values,
   if (!(threadIdx.x & 3)) *scale = (uint8_t)byte;
 }
 
-// A warp's 256 columns from c0 on, a multiple of 256, of an 8-bit row, every 32nd a lane's (element j is column j * 32 + lane);
-// zeros in f from `cols` on.
-__device__ __forceinline__ void store_rows8_apart(const Octet& f, uint8_t* values, uint8_t* scales, int c0, int lane, int cols) {
-  const int left = cols - c0 - lane;
-  uint8_t* to = values + c0 + lane;
+// A warp's 256 columns of a row from one that is a multiple of 256 on, every 32nd a lane's: element j is column j * 32 + lane.  `at` is
+// the lane's first, `left` how many columns there are from it on; WHOLE: all 256 are there, which spares a comparison for each.  Past
+// the end f holds zeros.
+template <typename T, bool WHOLE> __device__ __forceinline__ void read_apart(Octet& f, const T* at, int left) {
+  T v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = WHOLE || j * 32 < left ? at[j * 32] : from_float<T>(0.0f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = make_float2(to_float(v[2 * i]), to_float(v[2 * i + 1]));
+}
+template <typename T, bool WHOLE> __device__ __forceinline__ void store_apart(const Octet& f, T* at, int left) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (WHOLE || j * 32 < left) at[j * 32] = from_float<T>((j & 1) ? f[j >> 1].y : f[j >> 1].x);
+}
+// The same of an 8-bit row; `scales`: of the first of the 256 columns.  The whole warp takes part.
+template <bool WHOLE> __device__ __forceinline__ void store_rows8_apart(const Octet& f, uint8_t* at, uint8_t* scales, int lane, int left) {
   u32 own = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -88,10 +100,19 @@ __device__ __forceinline__ void store_rows8_apart(const Octet& f, uint8_t* value
       own = lane == 2 * i + j ? byte : own;
     }
     const u32 pair = e4m3_pair(e[0], e[1]);
-    if (i * 64 < left) to[i * 64] = (uint8_t)pair;
-    if (i * 64 + 32 < left) to[i * 64 + 32] = (uint8_t)(pair >> 8);
+    if (WHOLE || i * 64 < left) at[i * 64] = (uint8_t)pair;
+    if (WHOLE || i * 64 + 32 < left) at[i * 64 + 32] = (uint8_t)(pair >> 8);
   }
-  if (lane < 8 && c0 + lane * 32 < cols) scales[(c0 >> 5) + lane] = (uint8_t)own;
+  if (lane < 8 && (WHOLE || lane * 31 < left)) scales[lane] = (uint8_t)own;  // lane * 32 < left + lane
+}
+template <bool WHOLE> __device__ __forceinline__ void read_rows8_apart(Octet& f, const uint8_t* at, const uint8_t* scales, int lane, int left) {
+  const float own = scale_value(lane < 8 && (WHOLE || lane * 31 < left) ? scales[lane] : 0u);
+  u32 v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = WHOLE || j * 32 < left ? at[j * 32] : 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    f[i] = mul2(pair_value(v[2 * i] | v[2 * i + 1] << 8), make_float2(__shfl_sync(kAll, own, 2 * i), __shfl_sync(kAll, own, 2 * i + 1)));
 }
 
 // Eight neighbours of an 8-bit row, as they lie in memory.
@@ -111,19 +132,6 @@ struct Packed8 {
     f[3] = mul2(pair_value(v.y >> 16), scale);
   }
 };
-
-// A warp's 256 columns, as store_rows8_apart lays them out; zeros from `cols` on.
-__device__ __forceinline__ void read_rows8_apart(Octet& f, const uint8_t* values, const uint8_t* scales, int c0, int lane, int cols) {
-  const int left = cols - c0 - lane;
-  const uint8_t* from = values + c0 + lane;
-  const float own = scale_value(lane < 8 && c0 + lane * 32 < cols ? scales[(c0 >> 5) + lane] : 0u);
-  u32 v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = j * 32 < left ? from[j * 32] : 0u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    f[i] = mul2(pair_value(v[2 * i] | v[2 * i + 1] << 8), make_float2(__shfl_sync(kAll, own, 2 * i), __shfl_sync(kAll, own, 2 * i + 1)));
-}
 
 inline int64_t blocks_of(int64_t cols) { return (cols + 31) / 32; }
 inline bool good_rows8(const uint8_t* values, int64_t ld_values, const uint8_t* scales, int64_t ld_scales, int64_t rows, int64_t cols, int halves) {
