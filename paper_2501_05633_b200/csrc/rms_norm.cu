@@ -146,15 +146,35 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_rms_back(const __grid_co
       const T* dy = ring.row_of<T, VEC, RING>(row, 0);
       const S* h = ring.row_of<S, VEC, RING>(row, 1);
       float2 sum = both(0.0f);
-      constexpr int kKept = RING ? 1 : U;  // without rings, what has been read stays in registers
-      Octet kept_g[kKept], kept_u[kKept];
+      // What has been read stays in registers where they suffice, three or four units of 16-bit types as they lie in memory: then the row's
+      // place is free after one barrier (8,192 rows of 4,096 bfloat16 columns 65 -> 59 us).
+      constexpr bool kRaw = VEC && RING && U > 2 && sizeof(T) + sizeof(S) == 4, kKeeps = !RING || kRaw || U <= 2;
+      constexpr int kKept = kKeeps ? U : 1;
+      Octet kept_g[kRaw ? 1 : kKept], kept_u[kRaw ? 1 : kKept], kept_r[kRaw || !RING ? 1 : kKept];
+      Eight<T> raw_d[kRaw ? U : 1];
+      Eight<S> raw_h[kRaw ? U : 1], raw_r[kRaw ? U : 1];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
-        Octet &g8 = kept_g[u % kKept], &v = kept_u[u % kKept], w;
-        read_eight<T, VEC, RING>(g8, dy, c0, t.lane, a.cols);  // zeros past the end
-        read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
+        Octet &g8 = kept_g[kRaw ? 0 : u % kKept], &v = kept_u[kRaw ? 0 : u % kKept], w;
+        if constexpr (kRaw) {  // zeros past the end
+          const int c = c0 + t.lane * 8;
+          raw_d[u].clear();
+          raw_h[u].clear();
+          raw_r[u].clear();
+          if (c < a.cols) {
+            raw_d[u].load(dy + c);
+            raw_h[u].load(h + c);
+            if (a.ring.row_bytes[2]) raw_r[u].load(ring.row_of<S, VEC, RING>(row, 2) + c);
+          }
+          raw_d[u].get(g8);
+          raw_h[u].get(v);
+        } else {
+          read_eight<T, VEC, RING>(g8, dy, c0, t.lane, a.cols);
+          read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
+          if (RING && kKeeps && a.ring.row_bytes[2]) read_eight<S, VEC, RING>(kept_r[u % kKept], ring.row_of<S, VEC, RING>(row, 2), c0, t.lane, a.cols);
+        }
         if (RING) read_vector<VEC>(w, weight, c0, t.lane);
         else load_vector<VEC>(w, a.weight, a.wide, c0, t.lane, a.cols);
 #pragma unroll
@@ -166,24 +186,30 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_rms_back(const __grid_co
         }
       }
       float m = warp_sum(sum.x + sum.y);
+      if (t.warps > 1 && t.lane == 0) common.exchange[turn][t.index * t.warps + t.warp].x = m;
+      if (t.warps > 1 || (RING && kKeeps)) t.sync();  // the row has been read by all, if it is kept
+      if (RING && kKeeps) ring.pass(row, t.leads());
       if (t.warps > 1) {
-        if (t.lane == 0) common.exchange[turn][t.index * t.warps + t.warp].x = m;
-        t.sync();
         const float2* v = &common.exchange[turn][t.index * t.warps];
         m = 0.0f;
         for (int i = 0; i < t.warps; ++i) m += v[i].x;
       }
       m *= -inv;
-      if (RING) asm volatile("" ::: "memory");  // what follows is read from shared memory again: kept, it would not fit the registers
+      if (RING) asm volatile("" ::: "memory");  // what follows is read, or converted, again: kept, it would not fit the registers
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int c0 = t.col0 + u * 256;
         if (c0 >= a.cols) break;
-        Octet &d = kept_g[u % kKept], &v = kept_u[u % kKept];
-        if (RING) {
+        Octet &d = kept_g[kRaw ? 0 : u % kKept], &v = kept_u[kRaw ? 0 : u % kKept];
+        if (kRaw || !kKeeps) {
           Octet w;
-          read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);
-          read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
+          if constexpr (kRaw) {
+            raw_d[u].get(d);
+            raw_h[u].get(v);
+          } else {
+            read_eight<T, VEC, RING>(d, dy, c0, t.lane, a.cols);
+            read_eight<S, VEC, RING>(v, h, c0, t.lane, a.cols);
+          }
           read_vector<VEC>(w, weight, c0, t.lane);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -194,15 +220,19 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) k_rms_back(const __grid_co
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[i] = mul2(fma2(v[i], both(m), d[i]), both(rstd));
         if (a.ring.row_bytes[2]) {
-          read_eight<S, VEC, RING>(v, ring.row_of<S, VEC, RING>(row, 2), c0, t.lane, a.cols);
+          Octet& r = kept_r[kRaw || !RING ? 0 : u % kKept];
+          if constexpr (kRaw) raw_r[u].get(r);
+          else if (!RING || !kKeeps) read_eight<S, VEC, RING>(r, ring.row_of<S, VEC, RING>(row, 2), c0, t.lane, a.cols);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) d[i] = add2(d[i], v[i]);
+          for (int i = 0; i < 4; ++i) d[i] = add2(d[i], r[i]);
         }
         if (a.dres) store_eight<S, VEC>(d, static_cast<S*>(a.dres) + row * a.ld_dres, c0, t.lane, a.cols);
         store_eight<T, VEC>(d, static_cast<T*>(a.dx) + row * a.ld_dx, c0, t.lane, a.cols);
       }
-      if (RING || t.warps > 1) t.sync();  // the row has been read by all
-      if (RING) ring.pass(row, t.leads());
+      if (!kKeeps) {
+        t.sync();
+        ring.pass(row, t.leads());
+      }
       rstd = next_rstd;
     }
     if (counted) {
@@ -388,7 +418,9 @@ int regtopk_rms_norm_backward(const void* dy, int64_t ld_dy, const void* h, int6
     a.rstd = rstd; a.weight = weight; a.dx = dx; a.dres = dresidual; a.ld_dx = ld_dx; a.ld_dres = ld_dresidual;
     a.rows = rows; a.cols = (int)cols; a.wide = (uintptr_t)weight % 16 == 0; a.groups = groups; a.offsets = offsets;
     a.partial = dweight ? static_cast<float*>(workspace) : nullptr;
-    const Plan p = plan_of(cols, rows, {size, ssize, dh ? ssize : 0}, 2, 2, 1, 1, sms);
+    // Two units a warp: with four, 8,192 rows of 4,096 bfloat16 columns take 78 us against 59 us.  Three where a row has three and is of 16-bit
+    // types, so that it needs no second warp: 32,768 rows of 768 columns 39 us against 49 us.
+    const Plan p = plan_of(cols, rows, {size, ssize, dh ? ssize : 0}, size + ssize == 4 && cols > 512 && cols <= 768 ? 3 : 2, 2, 1, 1, sms);
     a.ring = p.ring;
     const int64_t blocks = (int64_t)sms * (p.blocks < 4 ? p.blocks : 4), turns = (rows + blocks * p.ring.teams - 1) / (blocks * p.ring.teams);
     a.block_rows = turns * p.ring.teams;
