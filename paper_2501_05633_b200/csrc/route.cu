@@ -285,6 +285,12 @@ template <int N> __device__ __forceinline__ void sort_descending(u32 (&v)[N]) {
   }
 }
 
+template <int N> __device__ __forceinline__ u32 largest_of(const u32 (&v)[N]) {
+  u32 m = v[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = max(m, v[i]);
+  return m;
+}
 // The pair (x, y) to shared memory at `to` + `offset`, if a == y.
 __device__ __forceinline__ void write_if(u32 a, u32 y, u32 to, int offset, int x) {
   asm volatile("{\n.reg .pred p;\nsetp.eq.u32 p, %0, %1;\n@p st.shared.v2.b32 [%2], {%3, %1};\n}" ::"r"(a), "r"(y), "r"(to + offset), "r"(x) : "memory");
@@ -319,7 +325,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
   const Share own(a, lane);
   constexpr bool kSigmoid = HOW == kBySigmoid || HOW == kJudgedBySigmoid, kSoftmax = HOW == kBySoftmax || HOW == kJudgedBySoftmax;
   constexpr bool by_logit = !(HOW == kBySoftmax || HOW == kBySigmoid), exact = sizeof(T) == 2 && by_logit;
-  constexpr u32 low_bits = exact ? 511u : (u32)(N - 1), pair_bits = HOW == kByLogit ? low_bits : (u32)(N - 1);
+  constexpr u32 low_bits = exact ? 511u : (u32)(N - 1);
   float bias[by_logit ? 1 : N];
   if (!by_logit) {
 #pragma unroll
@@ -362,7 +368,8 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
       }
       const float apart = HOW == kByLogit ? 0.0f : kSigmoid ? 0x1p-20f : 0x1p-18f * per_sum;
       if (mine) margin = apart;
-      u32 key[N], pair1 = 0, pair2 = 0;  // pair: the keys of this lane's two largest scores, where experts are compared by other numbers
+      u32 key[N];
+      float t1 = -INFINITY, t2 = -INFINITY;  // the two largest scores, of this lane and then of its group
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         float c = l[i];
@@ -370,13 +377,9 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
         if (HOW != kByLogit) {
           const float s = kSigmoid ? reciprocal_fast(1.0f + exp2_fast(c * -kLog2E)) : exp2_fast((c - top) * kLog2E) * per_sum;
           const float scored = c == -INFINITY ? -INFINITY : by_logit ? s : s + bias[by_logit ? 0 : i];
-          if (by_logit) {
-            const u32 k = ordered(scored) & ~pair_bits;
-            pair2 = max(pair2, min(pair1, k));
-            pair1 = max(pair1, k);
-          } else {
-            c = scored;
-          }
+          t2 = fmaxf(t2, fminf(t1, scored));
+          t1 = fmaxf(t1, scored);
+          if (!by_logit) c = scored;
         }
         if (by_logit) c += 0.0f;
         key[i] = (ordered(c) & ~low_bits) | low;
@@ -384,42 +387,43 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
       if (kSorted) sort_descending<N>(key);
       bool near = false;
       if (a.groups > 1) {
-        if (HOW == kByLogit || !by_logit) {
-          if (kSorted) {
-            pair1 = key[0];
-            pair2 = N > 1 ? key[N > 1 ? 1 : 0] : 0;
-          } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-              pair2 = max(pair2, min(pair1, key[i]));
-              pair1 = max(pair1, key[i]);
-            }
-          }
-        }
-        for (int o = 1; o < a.lanes; o <<= 1) {
-          const u32 o1 = __shfl_xor_sync(kAll, pair1, o), o2 = __shfl_xor_sync(kAll, pair2, o);
-          pair2 = max(min(pair1, o1), max(pair2, o2));
-          pair1 = max(pair1, o1);
-        }
-        const float t1 = unordered(pair1 & ~pair_bits), t2 = unordered(pair2 & ~pair_bits);
-        const bool two = HOW != kByLogit && a.top == 2 && pair2 > kNone;
-        const float strength = pair1 <= kNone ? -INFINITY : (two ? t1 + t2 : t1) + 0.0f;
-        u32 group = own.group < a.groups ? (ordered(strength) & ~31u) | (31u - own.group) : 0u, last = 0;
+        u32 group, last = 0, next = 0;
         bool kept = false;
+        if (HOW == kByLogit) {
+          // judged by the largest logit: its key, of which the low bits may be the group's
+          u32 best = kSorted ? key[0] : largest_of<N>(key);
+          for (int o = 1; o < a.lanes; o <<= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
+          group = own.group < a.groups ? (best & ~(exact ? 511u : 31u)) | (31u - own.group) : 0u;
+        } else {
+          for (int o = 1; o < a.lanes; o <<= 1) {
+            const float o1 = __shfl_xor_sync(kAll, t1, o), o2 = __shfl_xor_sync(kAll, t2, o);
+            t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
+            t1 = fmaxf(t1, o1);
+          }
+          const float strength = (a.top == 2 && t2 > -INFINITY ? t1 + t2 : t1) + 0.0f;
+          group = own.group < a.groups ? ordered(strength) : 0u;
+        }
         for (int g = 0; g < a.kept; ++g) {
           last = __reduce_max_sync(kAll, group);
           kept |= group == last;
           group = group == last ? 0u : group;
         }
-        if (!(exact && HOW == kByLogit) && a.kept < a.groups) {
-          const float v = unordered(last & ~31u), w = unordered(__reduce_max_sync(kAll, group) & ~31u);
-          const float size = pair1 <= kNone ? 0.0f : fabsf(t1) + (two ? fabsf(t2) : 0.0f);  // two scores may cancel
+        next = __reduce_max_sync(kAll, group);
+        u32 those = __ballot_sync(kAll, kept);
+        if (HOW == kByLogit) {
+          const float v = unordered(last & ~31u), w = unordered(next & ~31u);
+          near = !exact && a.kept < a.groups && w > -INFINITY && !(v - w > 0x1p-17f * (fabsf(v) + fabsf(w)));
+        } else {
+          // more groups than there may be, because two are of one strength; a NaN, which the maxima pass over; or a border that is too close
+          const float size = own.group < a.groups && t1 > -INFINITY ? fabsf(t1) + (a.top == 2 && t2 > -INFINITY ? fabsf(t2) : 0.0f) : 0.0f;  // two scores may cancel
           const float most_size = __uint_as_float(__reduce_max_sync(kAll, __float_as_uint(size)));
-          near = w > -INFINITY && !(v - w > fmaf(0x1p-22f * (32 + 2 * N), most_size, 2.0f * apart));
+          const float v = unordered(last), w = a.kept < a.groups ? unordered(next) : -INFINITY;
+          near = __popc(those & __ballot_sync(kAll, t1 > -INFINITY)) > a.kept << a.lanes_log2 || (w > -INFINITY && !(v - w > fmaf(0x1p-22f, most_size, 2.0f * apart)));
+          near |= __any_sync(kAll, (kSorted ? key[0] : largest_of<N>(key)) > (kInfinite | low_bits));
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) key[i] = kept ? key[i] : 0u;
-        const u32 those = near ? 0u : __ballot_sync(kAll, kept);
+        those = near ? 0u : those;
         if (mine) lanes = those;
       }
       // the k largest keys and the one after them, four at a time.  The lane that holds one writes it down and goes on to its next; without
@@ -430,11 +434,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if (j > 0 && j0 + j > a.k) break;
-          u32 best = key[0];
-          if (!kSorted) {
-#pragma unroll
-            for (int i = 1; i < N; ++i) best = max(best, key[i]);
-          }
+          u32 best = kSorted ? key[0] : largest_of<N>(key);
           const u32 m = __reduce_max_sync(kAll, best);
           const bool holds = best == m, real = m > kNone;
           write_if(best, m, slot + j0 * 8, j * 8, own.first);
