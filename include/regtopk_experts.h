@@ -54,8 +54,8 @@ typedef struct {
  *   groups: the groups_kept groups with the largest sums of their group_top largest c remain
  *   experts[t]: the k experts with the largest c among those, in descending order
  *   weights[t]: their s, divided by the sum of them if renormalise, times scale
- * Ties go to the lower index, of groups and of experts.  The choice is that of exact arithmetic on the given numbers: where
- * binary32 cannot tell two of them apart, the scores of that token are worked out again in binary64.  An expert whose logit or c is
+ * Ties go to the lower index, of groups and of experts.  The choice is that of binary64 arithmetic on the given numbers: tokens among
+ * whose numbers binary32 cannot tell two apart are done again in it (without bias experts are compared by their logits).  An expert whose logit or c is
  * -infinity is never chosen; places for which no expert is left hold -1 and weight 0.  A NaN or +infinity among the logits
  * makes the token's softmax scores NaN; NaN is the least c that can be chosen.
  * logits [tokens][n_experts] of `type`; bias [n_experts] binary32; experts int32 and weights binary32, [tokens][k] contiguous.

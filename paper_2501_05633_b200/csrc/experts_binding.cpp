@@ -307,6 +307,11 @@ PyObject* activation_backward(PyObject* const* a) {  // dy, kept, kind, gated, w
   return Py_BuildValue("NN", THPVariable_Wrap(da), wants_y ? THPVariable_Wrap(y) : Py_NewRef(Py_None));
 }
 
+bool overlap(const Tensor& out, const Tensor& in) {
+  const at::MemOverlapStatus how = at::get_overlap_status(out, in);
+  return how == at::MemOverlapStatus::Partial || how == at::MemOverlapStatus::Full;
+}
+
 // ---- the norm ---------------------------------------------------------------------------------------------------------
 PyObject* rms_norm(PyObject* const* a) {  // x, weight, eps, residual, want_y, want_y8
   const Tensor& x = tensor(a[0], "x");
@@ -323,7 +328,10 @@ PyObject* rms_norm(PyObject* const* a) {  // x, weight, eps, residual, want_y, w
   if (wants_y) y = empty(x.sizes(), x.scalar_type(), x);
   NewPacked p{};
   if (wants_y8) p = new_packed(x.sizes(), x, 1);
-  const Tensor h = residual ? empty(x.sizes(), residual->scalar_type(), x) : x, rstd = empty(x.sizes().slice(0, x.dim() - 1), at::kFloat, x);
+  Tensor h = x, rstd;  // kept together for the backward pass
+  const auto stats = x.sizes().slice(0, x.dim() - 1);
+  if (residual) std::tie(h, rstd) = two_of(x.sizes(), residual->scalar_type(), stats, at::kFloat, x);
+  else rstd = empty(stats, at::kFloat, x);
   check(regtopk_rms_norm(x.data_ptr(), in.ld, data(residual), res.ld, weight, static_cast<float>(number(a[2])), wants_y ? y.data_ptr() : nullptr, in.cols,
                          wants_y8 ? p.v() : nullptr, p.ld_values, wants_y8 ? p.s() : nullptr, p.ld_scales, residual ? h.data_ptr() : nullptr, in.cols,
                          static_cast<float*>(rstd.data_ptr()), in.rows, in.cols, type, type_of(h, "h"), stream_of(x)), "regtopk_rms_norm");
@@ -352,6 +360,9 @@ PyObject* rms_norm_backward(PyObject* const* a) {  // dy, h, rstd, weight, dh, o
     if (given->device() != dy.device() || given->scalar_type() != at::kFloat || given->dim() != 2 || given->size(0) != groups || given->size(1) != in.cols)
       type_error("dweight must be float32 [" + std::to_string(groups) + ", " + std::to_string(in.cols) + "] on the input's device");
     ld = rows_of(*given, "dweight").ld;
+    for (const Tensor* in : {&dy, &h, &tensor(a[2], "rstd"), &tensor(a[3], "weight")})
+      if (overlap(*given, *in)) value_error("dweight and an input overlap");
+    if (dh && overlap(*given, *dh)) value_error("dweight and dh overlap");
     written(*given, "dweight");
   }
   const c10::cuda::CUDAGuard guard(dy.device());

@@ -171,7 +171,7 @@ def test_refusals():
         with pytest.raises(TypeError):
             call()
     for call in (lambda: rt.rms_norm(x, w, want_y=False), lambda: rt.rms_norm(x.t(), w[:4]), lambda: rt.rms_norm(x[:1].expand(4, 64), w),
-                 lambda: rt.rms_norm_backward(y, h, rstd, w, accumulate=True), lambda: rt.rms_norm_backward(y, h, rstd, w, dweight=torch.zeros(1, 64, device="cuda", requires_grad=True)),
+                 lambda: rt.rms_norm_backward(y, h, rstd, w, accumulate=True), lambda: rt.rms_norm_backward(y, h, rstd, w, dweight=w.view(1, 64)), lambda: rt.rms_norm_backward(y, h, rstd, w, dweight=h[:1]), lambda: rt.rms_norm_backward(y, h, rstd, w, dweight=torch.zeros(1, 64, device="cuda", requires_grad=True)),
                  lambda: rt.rms_norm_backward(y, h, rstd, w, offsets=torch.tensor([0, 1, 4], device="cuda"), dweight=w.expand(2, 64))):
         with pytest.raises(ValueError):
             call()
