@@ -100,9 +100,9 @@ template <typename T, bool PACKED, bool VEC> __global__ void __launch_bounds__(k
   clear_tail<T, VEC>(a);
 }
 
-constexpr int kJoinStep = 4;  // rows under way
 
 template <typename T, typename O, bool VEC, bool WHOLE> __device__ __forceinline__ void join_piece(const MoveArgs& a, int64_t token, int c0, int lane, int cols) {
+  constexpr int kJoinStep = VEC || sizeof(T) == 4 ? 4 : 2;  // rows under way
   const int first = c0 + lane, left = cols - first;
   const int32_t* place = a.place + token * a.k;
   const float* weights = a.weights + token * a.k;
@@ -154,40 +154,65 @@ template <typename T, typename O, bool VEC> __global__ void __launch_bounds__(kM
   else join_piece<T, O, VEC, false>(a, at.token, at.c0, at.lane, cols);
 }
 
-// 256 columns of a token's dout and of STEP of its rows.
-template <typename T, typename D, bool VEC, int STEP, bool WHOLE>
-__device__ __forceinline__ void back_unit(const MoveArgs& a, int64_t t, const int64_t (&to)[STEP], const float (&w)[STEP], float (&dot)[STEP], int c0,
-                                          int lane, int cols) {
-  const int first = c0 + (VEC ? lane * 8 : lane), left = cols - first;
-  Octet d, f[STEP];
-  const D* dout = static_cast<const D*>(a.in) + t * a.ld_in;
-  if (VEC) read_eight<D, VEC, false>(d, dout, c0, lane, cols);
-  else read_apart<D, WHOLE>(d, dout + first, left);
+// Products of a token's dout with one of its rows, and what that row's gradient is.
+template <typename T> __device__ __forceinline__ float back_of(Octet& f, const Octet& d, float w) {
+  float2 s = both(0.0f);
 #pragma unroll
-  for (int j = 0; j < STEP; ++j) {
-    const T* row = static_cast<const T*>(a.other) + (to[j] < 0 ? 0 : to[j]) * a.ld_other;
-    if (VEC) read_eight<T, VEC, false>(f[j], row, c0, lane, to[j] < 0 ? 0 : cols);
-    else if (to[j] >= 0) read_apart<T, WHOLE>(f[j], row + first, left);
+  for (int i = 0; i < 4; ++i) {
+    s = fma2(f[i], d[i], s);
+    f[i] = mul2(d[i], both(w));
   }
+  return s.x + s.y;
+}
+// 256 columns of a token's dout and of STEP of its rows, unaligned.
+template <typename T, typename D, int STEP, bool WHOLE>
+__device__ __forceinline__ void back_apart(const MoveArgs& a, const D* dout, const int64_t (&to)[STEP], const float (&w)[STEP], float (&dot)[STEP], int first,
+                                           int left) {
+  Octet d, f[STEP];
+  read_apart<D, WHOLE>(d, dout + first, left);
+#pragma unroll
+  for (int j = 0; j < STEP; ++j)
+    if (to[j] >= 0) read_apart<T, WHOLE>(f[j], static_cast<const T*>(a.other) + to[j] * a.ld_other + first, left);
 #pragma unroll
   for (int j = 0; j < STEP; ++j) {
     if (to[j] < 0) continue;
-    float2 s = both(0.0f);
+    dot[j] += back_of<T>(f[j], d, w[j]);
+    store_apart<T, WHOLE>(f[j], static_cast<T*>(a.out) + to[j] * a.ld_out + first, left);
+  }
+}
+// The columns c, c + step, ... of an aligned row, eight neighbours at a time; the next ones are on their way while these are worked on.
+template <typename T, typename D, int STEP>
+__device__ __forceinline__ void back_aligned(const MoveArgs& a, const D* dout, const int64_t (&to)[STEP], const float (&w)[STEP], float (&dot)[STEP], int c,
+                                             int step, int cols) {
+  Eight<D> next_d;
+  Eight<T> next_f[STEP];
+  const auto fetch = [&](int at) {
+    next_d.fetch(dout + at);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s = fma2(f[j][i], d[i], s);
-      f[j][i] = mul2(d[i], both(w[j]));
+    for (int j = 0; j < STEP; ++j)
+      if (to[j] >= 0) next_f[j].fetch(static_cast<const T*>(a.other) + to[j] * a.ld_other + at);
+  };
+  if (c < cols) fetch(c);
+  for (; c < cols; c += step) {
+    Octet d, f[STEP];
+    next_d.get(d);
+#pragma unroll
+    for (int j = 0; j < STEP; ++j) next_f[j].get(f[j]);
+    if (c + step < cols) fetch(c + step);
+#pragma unroll
+    for (int j = 0; j < STEP; ++j) {
+      if (to[j] < 0) continue;
+      dot[j] += back_of<T>(f[j], d, w[j]);
+      Eight<T> v;
+      v.put(f[j]);
+      v.store(static_cast<T*>(a.out) + to[j] * a.ld_out + c);
     }
-    dot[j] += s.x + s.y;
-    T* out = static_cast<T*>(a.out) + to[j] * a.ld_out;
-    if (VEC) store_eight<T, VEC>(f[j], out, c0, lane, cols);
-    else store_apart<T, WHOLE>(f[j], out + first, left);
   }
 }
 
 // A team of warps a token: its warps share the row's units of 256 columns, and each has STEP of the token's rows under way beside
 // dout.
-template <typename T, typename D, bool VEC, int STEP> __global__ void __launch_bounds__(kMoveThreads) k_join_back(const __grid_constant__ MoveArgs a) {
+template <typename T, typename D, bool VEC, int STEP> __global__ void __launch_bounds__(kMoveThreads, sizeof(T) == 4 ? 2 : VEC ? 3 : 4) k_join_back(const __grid_constant__ MoveArgs a) {
   __shared__ float part[kMoveWarps][STEP];
   begin_after_predecessor();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, member = warp % a.team, teams = kMoveWarps / a.team;
@@ -206,9 +231,14 @@ template <typename T, typename D, bool VEC, int STEP> __global__ void __launch_b
     }
     if (there) {
       const int cols = (int)a.cols;
-      for (int c0 = member * 256; c0 < cols; c0 += a.team * 256) {
-        if (!VEC && cols - c0 >= 256) back_unit<T, D, VEC, STEP, true>(a, t, to, w, dot, c0, lane, cols);
-        else back_unit<T, D, VEC, STEP, false>(a, t, to, w, dot, c0, lane, cols);
+      const D* dout = static_cast<const D*>(a.in) + t * a.ld_in;
+      if (VEC) {
+        back_aligned<T, D, STEP>(a, dout, to, w, dot, member * 256 + lane * 8, a.team * 256, cols);
+      } else {
+        for (int c0 = member * 256; c0 < cols; c0 += a.team * 256) {
+          if (cols - c0 >= 256) back_apart<T, D, STEP, true>(a, dout, to, w, dot, c0 + lane, cols - c0 - lane);
+          else back_apart<T, D, STEP, false>(a, dout, to, w, dot, c0 + lane, cols - c0 - lane);
+        }
       }
     }
 #pragma unroll
@@ -257,7 +287,8 @@ template <typename Launch> int in_parts(MoveArgs a, bool vec, size_t in_size, si
 }
 
 template <typename T, typename D, int STEP> int launch_join_back_step(const MoveArgs& a, bool vec, unsigned grid, cudaStream_t s) {
-  return vec ? start(k_join_back<T, D, true, STEP>, grid, kMoveThreads, 0, s, a) : start(k_join_back<T, D, false, STEP>, grid, kMoveThreads, 0, s, a);
+  if (vec) return start(k_join_back<T, D, true, STEP>, grid, kMoveThreads, 0, s, a);
+  return start(k_join_back<T, D, false, (sizeof(T) == 2 && STEP > 2 ? 2 : STEP)>, grid, kMoveThreads, 0, s, a);
 }
 template <typename T, typename D> int launch_join_back(const MoveArgs& a, bool vec, unsigned grid, cudaStream_t s) {
   return a.k == 1 ? launch_join_back_step<T, D, 1>(a, vec, grid, s) : a.k == 2 ? launch_join_back_step<T, D, 2>(a, vec, grid, s)
