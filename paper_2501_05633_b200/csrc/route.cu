@@ -520,8 +520,9 @@ struct RouteBackArgs {
 
 // A warp takes `batch` tokens at a time, a token's chosen experts in `places` of its lanes.  What reaches their scores, or logits, is laid
 // into rows in shared memory, from which the gradient's rows are written.  Plain softmax scores need all logits, the others only the
-// chosen ones.  Latency bounds it.  For up to 64 experts: 16,384 tokens over eight take 5.1 us, with a token a warp 10.8 us; over 64, 7 to
-// 10 us and 10 to 11 us; but over 256, 24 us and 12.5 us.
+// chosen ones.  Latency bounds it.  For many tokens over up to 64 experts: 16,384 over eight take 5.1 us, with a token a warp 10.8 us; over
+// 64, 7 us and 10 us; but over 256, 12.3 us and 9.7 us.  A quarter as many where all logits are needed, of which few lanes sum up a
+// token's: 5,003 tokens over 60 take 8.5 us, with a token a warp 5 us.
 constexpr int kBackRoom = 544, kBackMost = 64;  // numbers: several rows; the most experts
 template <typename T> __global__ void __launch_bounds__(kRouteThreads) k_route_back(const __grid_constant__ RouteBackArgs a) {
   __shared__ float all_logits[kRouteWarps][kBackRoom], all_rows[kRouteWarps][kBackRoom];
@@ -928,16 +929,16 @@ template <typename T> int launch_route_of(RouteArgs& a, int sms, cudaStream_t s)
   }
 }
 template <typename T> int launch_route_back(RouteBackArgs& a, int sms, cudaStream_t s) {
-  if (a.n_experts > kBackMost) {
-    const int64_t blocks = (a.tokens + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sms * 8;
-    return start(k_route_back_row<T>, (unsigned)(blocks < most ? blocks : most), kRouteThreads, 0, s, a);
-  }
   a.columns = divisor(a.n_experts);
   a.pitch = a.n_experts | 1;
   a.places_log2 = 0;
   while (1 << a.places_log2 < a.k) ++a.places_log2;
   a.batch = 1;  // as many as have places and room, while every SM has sixteen warps' work
   while (a.batch << a.places_log2 < 32 && 2 * a.batch * a.pitch <= kBackRoom && a.tokens >= (int64_t)sms * 16 * 2 * a.batch) a.batch *= 2;
+  if (a.batch == 1 || a.n_experts > (a.sigmoid || a.renormalise ? kBackMost : kBackMost / 4)) {
+    const int64_t blocks = (a.tokens + kRouteWarps - 1) / kRouteWarps, most = (int64_t)sms * 8;
+    return start(k_route_back_row<T>, (unsigned)(blocks < most ? blocks : most), kRouteThreads, 0, s, a);
+  }
   const int64_t each = kRouteWarps * a.batch, blocks = (a.tokens + each - 1) / each, most = (int64_t)sms * 6;
   return start(k_route_back<T>, (unsigned)(blocks < most ? blocks : most), kRouteThreads, 0, s, a);
 }

@@ -237,6 +237,27 @@ def test_route_backward(tokens, experts, k, groups, kept, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("tokens,experts,k,scores,renormalise", [(4801, 8, 2, "softmax", False), (9600, 16, 3, "softmax", False), (4799, 60, 4, "sigmoid", True),
+                                                                 (5003, 64, 8, "softmax", True), (20011, 7, 1, "sigmoid", False)])
+def test_route_backward_of_many_tokens(tokens, experts, k, scores, renormalise, dtype):
+    """Enough tokens for the kernel that takes several at a time, the last ones fewer."""
+    gen = torch.Generator().manual_seed(tokens)
+    logits = made(tokens, experts, dtype, gen, 3, 1, scale=1.5)
+    chosen = torch.rand(tokens, experts, generator=gen).argsort(1)[:, :k].to(torch.int32)
+    chosen[torch.rand(tokens, k, generator=gen) < 0.05] = -1
+    if k > 2:
+        chosen[::7, :3] = chosen[::7, :1]  # the same expert three times
+    logits[5] = -INF
+    chosen[5] = -1
+    dw = torch.randn(tokens, k, generator=gen)
+    got = rt.route_backward(dw.cuda(), logits, chosen.cuda(), scores=scores, renormalise=renormalise, scale=2.5)
+    want = ref.route_backward(dw.double().numpy(), host(logits), chosen.numpy(), scores, renormalise, 2.5)
+    most = 2.5 * np.abs(dw.double().numpy()).sum(1, keepdims=True) * np.ones_like(want)
+    assert_close(got, want, 2.0 ** -17 * (np.where(want == 0, 0.0, most) if renormalise else most * ref.scores_of(host(logits), scores)), dtype, scores)
+
+
+@pytest.mark.gpu
 def test_route_refusals():
     l = torch.zeros(4, 16, device="cuda")
     e, w = rt.route(l, 2)
