@@ -86,10 +86,12 @@ def test_other_streams(example):
     rt.training_status()
 
 
-def test_captured_step(example):
-    """A whole step as a CUDA graph, replayed on other inputs, other routes and other workers' shares among them."""
+@pytest.mark.parametrize("tokens", [500, 1500, 4000])
+def test_captured_step(example, tokens):
+    """A whole step as a CUDA graph, replayed on other inputs, other routes and other workers' shares among them; by its number of
+    tokens the sort is one block, a cluster, or two launches with a workspace."""
     gen = torch.Generator(device="cuda").manual_seed(7)
-    block, theta, x, at = parts(example, gen, tokens=500)
+    block, theta, x, at = parts(example, gen, tokens=tokens)
     dy, rows = torch.randn(x.shape, generator=gen, device="cuda"), torch.zeros(3, block.size, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -103,7 +105,7 @@ def test_captured_step(example):
         gen.manual_seed(seed)
         x.normal_(generator=gen)
         dy.normal_(generator=gen)
-        at[1], at[2] = 100 * seed, 1500 - 7 * seed
+        at[1], at[2] = 100 * seed, 3 * tokens - 7 * seed
         rows.zero_()
         graph.replay()
         want = step_of(example, block, theta, x, at, dy, torch.zeros_like(rows))
