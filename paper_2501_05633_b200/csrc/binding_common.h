@@ -201,6 +201,15 @@ std::pair<Tensor, Tensor> two_of(at::IntArrayRef size, at::ScalarType type, at::
   };
   return {part(size, type, 0), part(other_size, other_type, second)};
 }
+// Two tensors that need not live and die together: in one allocation only where they are so small (a megabyte) that what the longer one
+// keeps alive of the other does not matter, but the 0.8 us of a second allocation do.
+std::pair<Tensor, Tensor> two_if_small(at::IntArrayRef size, at::ScalarType type, at::IntArrayRef other_size, at::ScalarType other_type, const Tensor& like) {
+  int64_t n = static_cast<int64_t>(c10::elementSize(type)), m = static_cast<int64_t>(c10::elementSize(other_type));
+  for (const int64_t i : size) n *= i;
+  for (const int64_t i : other_size) m *= i;
+  if (n + m <= 1 << 20) return two_of(size, type, other_size, other_type, like);
+  return {empty(size, type, like), empty(other_size, other_type, like)};
+}
 void* stream_of(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.device().index()).stream(); }
 void* data(const Tensor* t) { return t ? t->data_ptr() : nullptr; }
 

@@ -246,7 +246,7 @@ PyObject* join_tokens_backward(PyObject* const* a) {  // dout, rows, place, weig
   if (up.rows != tokens || up.cols != in.cols) type_error("dout must have a row for each token of place, as wide as rows");
   const int64_t* filled = filled_of(offsets, from);
   const c10::cuda::CUDAGuard guard(from.device());
-  const Tensor drows = empty(from.sizes(), from.scalar_type(), from), dweights = empty(place.sizes(), at::kFloat, from);
+  const auto [drows, dweights] = two_if_small(from.sizes(), from.scalar_type(), place.sizes(), at::kFloat, from);
   check(regtopk_join_tokens_backward(dout.data_ptr(), up.ld, from.data_ptr(), in.ld, static_cast<const int32_t*>(place.data_ptr()),
                                      static_cast<const float*>(weights.data_ptr()), filled, drows.data_ptr(), in.cols,
                                      static_cast<float*>(dweights.data_ptr()), tokens, k, in.rows, in.cols, type, dtype, stream_of(from)),
@@ -298,9 +298,9 @@ PyObject* activation_backward(PyObject* const* a) {  // dy, kept, kind, gated, w
     type_error(gated ? "kept must have dy's shape, with twice the columns" : "kept must have dy's shape");
   const Rows in = pair ? p.v : rows_of(kept, "kept");
   const c10::cuda::CUDAGuard guard(dy.device());
-  const Tensor da = empty(kept.sizes(), dy.scalar_type(), dy);
-  Tensor y;
-  if (wants_y) y = empty(dy.sizes(), dy.scalar_type(), dy);
+  Tensor da, y;
+  if (wants_y) std::tie(da, y) = two_if_small(kept.sizes(), dy.scalar_type(), dy.sizes(), dy.scalar_type(), dy);
+  else da = empty(kept.sizes(), dy.scalar_type(), dy);
   check(regtopk_activation_backward(dy.data_ptr(), up.ld, kept.data_ptr(), in.ld, bytes_of(p.scales), p.s.ld, da.data_ptr(), in.cols,
                                     wants_y ? y.data_ptr() : nullptr, up.cols, up.rows, up.cols, kind, gated, type, stream_of(dy)),
         "regtopk_activation_backward");
@@ -366,11 +366,12 @@ PyObject* rms_norm_backward(PyObject* const* a) {  // dy, h, rstd, weight, dh, o
     written(*given, "dweight");
   }
   const c10::cuda::CUDAGuard guard(dy.device());
-  const Tensor dw = given ? *given : empty({groups, in.cols}, at::kFloat, dy);
+  const size_t bytes = regtopk_rms_norm_backward_workspace_bytes(in.rows, in.cols, groups);
+  Tensor dw, ws;
+  if (given) dw = *given, ws = empty({static_cast<int64_t>(bytes)}, at::kByte, dy);
+  else std::tie(dw, ws) = two_if_small({groups, in.cols}, at::kFloat, {static_cast<int64_t>(bytes)}, at::kByte, dy);
   const bool same = h.scalar_type() == dy.scalar_type();
   const Tensor dx = empty(dy.sizes(), dy.scalar_type(), dy), dres = same ? dx : empty(dy.sizes(), h.scalar_type(), dy);
-  const size_t bytes = regtopk_rms_norm_backward_workspace_bytes(in.rows, in.cols, groups);
-  const Tensor ws = empty({static_cast<int64_t>(bytes)}, at::kByte, dy);
   check(regtopk_rms_norm_backward(dy.data_ptr(), in.ld, h.data_ptr(), hr.ld, rstd, weight, data(dh), dhr.ld, dx.data_ptr(), in.cols,
                                   same ? nullptr : dres.data_ptr(), in.cols, static_cast<float*>(dw.data_ptr()), ld,
                                   static_cast<const int64_t*>(data(offsets)), groups, accumulate, in.rows, in.cols, type, type_of(h, "h"), ws.data_ptr(),
