@@ -3,8 +3,8 @@
 // Memory traffic is their floor: each reads its inputs once and writes its outputs once, and nothing is kept for the backward
 // pass but the 8-bit rows (1 + 1/32 bytes for an element, where the activation's input has two): it forms the activation
 // and its slope again from them, and the output, which the next product's weight gradients need, on the way.
-// 32,768 rows of 2,304 bfloat16 columns, gated silu: 98 us forward with the 8-bit rows, 6.2 TB/s, 122 us back, 6.2 TB/s.  Binary32's gelu is
-// bound by CUDA's erfc and expf (8,192 x 2,048, both ways, 86 us, silu 60 us).
+// 32,768 rows of 2,304 bfloat16 columns, gated silu: 98 us forward with the 8-bit rows, 6.2 TB/s, 122 us back, 6.2 TB/s.  Binary32, 8,192 x 2,048,
+// ungated, both ways: silu 60 us, gelu 61 us (86 us with CUDA's erfc), 6.0 TB/s.
 
 #include "rows8.cuh"
 
@@ -46,9 +46,20 @@ template <int KIND, bool FAST> __device__ __forceinline__ float activate(float x
       h = h * t * e;
       p = x >= 0.0f ? 1.0f - h : h;
     } else {
-      // erfc(z + r), r what z = -x / sqrt(2) has lost by rounding: without it p is off by z^2 units of 2^-22
-      const float z = -0.70710677f * x, r = fmaf(-1.2101617e-8f, x, fmaf(-0.70710677f, x, -z));
-      p = fmaf(-0.56418958f * e, r, 0.5f * erfcf(z));
+      // The same by the fit of Press, Teukolsky, Vetterling and Flannery (Numerical Recipes, 6.2): erfc(z) = t exp(-z^2 + P(t)), t = 1 / (1 + z / 2),
+      // 1.2e-7 relative for every z >= 0; half the instructions of CUDA's erfc, and exact far out without more, for z^2 = x^2 / 2.
+      const float t = reciprocal_fast(fmaf(0.35355339f, fabsf(x), 1.0f));
+      float h = fmaf(0.17087277f, t, -0.82215223f);
+      h = fmaf(h, t, 1.48851587f);
+      h = fmaf(h, t, -1.13520398f);
+      h = fmaf(h, t, 0.27886807f);
+      h = fmaf(h, t, -0.18628806f);
+      h = fmaf(h, t, 0.09678418f);
+      h = fmaf(h, t, 0.37409196f);
+      h = fmaf(h, t, 1.00002368f);
+      h = fmaf(h, t, -1.26551223f);
+      h = 0.5f * t * exp2_fast(kLog2E * h) * e;
+      p = x >= 0.0f ? 1.0f - h : h;
     }
     if (slope) *slope = fmaf(x, 0.3989422804f * e, p);
   }

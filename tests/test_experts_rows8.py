@@ -3,8 +3,8 @@
 Tolerances.  8-bit rows and what they stand for are exact.  Let u = 2^-24.  An exponential here is off by 2^-21.5 relative
 (the hardware's, in binary32 CUDA's, which is closer) and by the rounding of its argument, |z| u, z at most 64 where it is above
 2^-93; a quotient and three products add 6u: p = f(x) / x is off by 2^-17 relative.  gelu takes p for 16-bit types from a formula
-that is off by 7.5e-8 (Abramowitz and Stegun 7.1.26) and 16 u more: 2^-22 in all; in binary32 by CUDA's erfc, corrected for
-the rounding of its argument.  The slope is p + x p'(x), each term off by as much relative to itself.
+that is off by 7.5e-8 (Abramowitz and Stegun 7.1.26) and 16 u more: 2^-22 in all; in binary32 by a fit that is off
+by 1.2e-7 relative and exp(-x^2 / 2), whose argument is rounded: x^2 / 2 u, 2^-18 for x up to 11.  The slope is p + x p'(x), each term off by as much relative to itself.
 Results follow by products of one more rounding each, and are rounded once to the type.  Below 2^-120 binary32 may give 0."""
 import numpy as np
 import pytest
