@@ -96,7 +96,7 @@ int regtopk_join_tokens(const void* from, int64_t ld_from, const int32_t* place,
 
 /* The gradients of regtopk_join_tokens with weights (that of residual is dout itself):
  *   dfrom[place[t][j]] = weights[t][j] * dout[t],  dweights[t][j] = sum over the columns of dout[t] * from[place[t][j]]
- * rows of dfrom from *filled on become zeros, and dweights is 0 where there is no place.  dout of dout_type, `type` or F32. */
+ * rows of dfrom from *filled on become zeros, and dweights is 0 where there is no place.  dout of dout_type, `type` or F32; tokens < 2^31. */
 int regtopk_join_tokens_backward(const void* dout, int64_t ld_dout, const void* from, int64_t ld_from, const int32_t* place,
                                  const float* weights, const int64_t* filled, void* dfrom, int64_t ld_dfrom, float* dweights,
                                  int64_t tokens, int32_t k, int64_t rows, int64_t cols, int32_t type, int32_t dout_type,

@@ -101,7 +101,6 @@ template <typename T, bool PACKED, bool VEC> __global__ void __launch_bounds__(k
   clear_tail<T, VEC>(a);
 }
 
-
 template <typename T, typename O, bool VEC, bool WHOLE> __device__ __forceinline__ void join_piece(const MoveArgs& a, int64_t token, int c0, int lane, int cols) {
   // Rows under way: of unaligned 16-bit types two, whose fewer registers leave room for more warps (8,192 tokens of 2,047 bfloat16 columns
   // from four rows each 54 us, with four 65 us).
