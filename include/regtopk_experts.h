@@ -57,7 +57,7 @@ typedef struct {
  * Ties go to the lower index, of groups and of experts.  The choice is that of binary64 arithmetic on the given numbers: tokens among
  * whose numbers binary32 cannot tell two apart are done again in it (without bias experts are compared by their logits).  An expert whose logit or c is
  * -infinity is never chosen; places for which no expert is left hold -1 and weight 0.  A NaN or +infinity among the logits
- * makes the token's softmax scores NaN; NaN is the least c that can be chosen.
+ * makes the token's softmax scores NaN; NaN is the least c that can be chosen, and counts as -1e300 in the sum of a group.
  * logits [tokens][n_experts] of `type`; bias [n_experts] binary32; experts int32 and weights binary32, [tokens][k] contiguous.
  * 1 <= n_experts <= REGTOPK_ROUTE_MAX_EXPERTS, 1 <= k <= min(REGTOPK_ROUTE_MAX_CHOICES, n_experts), groups divides n_experts.
  * Errors: INVALID_ARG, TOO_LARGE, NO_DEVICE, CUDA. */

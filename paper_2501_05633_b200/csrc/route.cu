@@ -132,6 +132,9 @@ __device__ __forceinline__ double reciprocal_64(double x) {
 }
 
 constexpr int kMostShare = 4096;  // tokens of a warp
+// What a NaN counts as where groups are judged: below every binary32 number, and twice it is still above -infinity, which is a group
+// that has no expert left.
+constexpr double kNoNumber = -1e300;
 
 // A token once more in binary64, for the few whose numbers lie too close for binary32.  slots and numbers: room for k and n_experts.
 // The largest are looked for among the numbers rounded to binary32, which keeps their order; where several round to the same, the numbers
@@ -190,7 +193,7 @@ __device__ __noinline__ void route_in_64_bits(const RouteArgs& a, int64_t t, int
     }
     numbers[own.first + at] = c;
     if (c == -INFINITY) s = -INFINITY;
-    else if (s != s) s = -DBL_MAX;
+    else if (s != s) s = kNoNumber;
     const u32 k = c == -INFINITY ? 0u : c != c ? 1u : ordered((float)c + 0.0f);
 #pragma unroll
     for (int i = 0; i < N; ++i) key[i] = i == at ? k : key[i];
@@ -423,6 +426,7 @@ __global__ void __launch_bounds__(kRouteThreads, N <= 8 ? 4 : 2) k_route(const _
           const float v = unordered(last), w = a.kept < a.groups ? unordered(next) : -INFINITY;
           near = __popc(those & __ballot_sync(kAll, t1 > -INFINITY)) > a.kept << a.lanes_log2 || (w > -INFINITY && !(v - w > fmaf(0x1p-22f, most_size, 2.0f * apart)));
           near |= __any_sync(kAll, (kSorted ? key[0] : largest_of<N>(key)) > (kInfinite | low_bits));
+          if (HOW == kJudgedBySoftmax) near |= sum != sum;  // +infinity among the logits: no key is NaN, but every score
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) key[i] = kept ? key[i] : 0u;
