@@ -35,3 +35,33 @@ def test_groups_with_numbers_that_are_not_finite(groups, kept, scores, dtype):
                 e, w = check_route(logits.cuda(), min(4, kept * size), scores=scores, bias=bias, groups=groups, groups_kept=kept, group_top=top,
                                    renormalise=renormalise)
                 assert (e >= 0).all(), "a masked group was kept before one with NaN"
+
+
+# ---- activations ------------------------------------------------------------------------------------------------------
+def gelu_points():
+    """Both signs, far out, and around 0."""
+    rng = np.random.default_rng(4)
+    return np.concatenate([rng.standard_normal(8192), np.linspace(-12.5, 12.5, 16385), np.linspace(-1.01, 1.01, 4097), 10.0 ** np.linspace(-6, 0, 30)])
+
+
+@pytest.mark.gpu
+def test_gelu_in_binary32():
+    """Let u = 2^-24.  Further out than 1 Phi(-|x|) = e t S(t): 1 + p |x| is rounded, 1u, its reciprocal off by one in the last place, 2u, and S by 1u
+    of its last sum and 1u of those before; the exponential by 2 in the last place, 4u, and 1u of its correction; two products 2u; the fit
+    0.1u: 12u.  Nearer to 0 the sum 1/2 + x R is off by 1u of a half and 2u of x R, 3u of a Phi of 0.16 or more.  2^-20 is 16u, of Phi in f(x) and of
+    Phi and x phi(x) in the slope.  Where |x| is 0.2 to 0.3 f(x) has one rounding of the sum and one of the product, each 1u at most and less than
+    0.6u in the mean square: 1u for both; the slope's two terms and their sum likewise."""
+    x = torch.from_numpy(gelu_points()).float().cuda()
+    at = x.double().cpu().numpy()[None]
+    _, f, slope = (v[0] for v in ref.activation(at, "gelu", False))
+    y, _ = rt.activation(x, "gelu")
+    dx, again = rt.activation_backward(torch.ones_like(x), x, "gelu", want_y=True)
+    assert torch.equal(again, y)
+    x, y, dx = (v.double().cpu().numpy() for v in (x, y, dx))
+    p = np.where(x == 0, 0.5, f / np.where(x == 0, 1.0, x))
+    assert (np.abs(y - f) <= 2.0 ** -20 * np.abs(f)).all(), np.nanmax(np.abs(y - f) / np.abs(f)) * 2 ** 24
+    size = p + np.abs(slope - p)
+    assert (np.abs(dx - slope) <= 2.0 ** -20 * size).all(), np.max(np.abs(dx - slope) / size) * 2 ** 24
+    near = (np.abs(x) > 0.2) & (np.abs(x) < 0.3)
+    for got, want in ((y, f), (dx, slope)):
+        assert np.sqrt(((got[near] / want[near] - 1) ** 2).mean()) <= 2.0 ** -24
