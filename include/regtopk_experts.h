@@ -103,7 +103,9 @@ int regtopk_join_tokens_backward(const void* dout, int64_t ld_dout, const void* 
                                  void* cuda_stream);
 
 /* silu(x) = x / (1 + exp(-x));  gelu(x) = x Phi(x), Phi the normal distribution's;  gelu_tanh: Phi approximated by
- * (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2.  In binary32 Phi of gelu is right to 2^-20 relative, far out too; below 2^-120 results may be 0. */
+ * (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2.
+ * How good they are: f(x) / x and the terms p and x p'(x) of the slope, p = f(x) / x, are right to 2^-16 relative for 16-bit types (2^-15 below 2^-70; before they are
+ * rounded to the type, by 2^-9 or 2^-12) and for gelu_tanh in binary32, to 2^-20 for silu and gelu in binary32; below 2^-120 results may be 0. */
 enum { REGTOPK_ACTIVATION_SILU = 0, REGTOPK_ACTIVATION_GELU = 1, REGTOPK_ACTIVATION_GELU_TANH = 2 };
 
 /* y = f(a), a [rows][cols]; gated != 0: y = f(a[:, :cols]) * a[:, cols:], a [rows][2 cols].  y [rows][cols]; both of `type`.

@@ -92,6 +92,9 @@ def activation(a: torch.Tensor, kind: str = "silu", *, gated: bool = False, keep
                ) -> Tuple[torch.Tensor, Union[torch.Tensor, Rows8]]:
     """(y, kept): y = f(a), or f(a[..., :h]) * a[..., h:] if gated; f is "silu", "gelu" or "gelu_tanh".
 
+    gelu is x Phi(x) with the normal distribution's Phi, of large negative x too.  float32 silu and gelu are right to 2^-20 relative, 16-bit types
+    and gelu_tanh to 2^-16 before they are rounded to the type.
+
     kept is what activation_backward takes: a itself, or with keep8 its 8-bit rows.  The blocks of a gated a's second half begin
     anew, so that kept.values[..., h:] and the second half of kept.scales are 8-bit rows too."""
     y, kept = (training._native or _load()).activation(a, kind, gated, keep8)

@@ -45,23 +45,47 @@ def gelu_points():
 
 
 @pytest.mark.gpu
-def test_gelu_in_binary32():
-    """Let u = 2^-24.  Further out than 1 Phi(-|x|) = e t S(t): 1 + p |x| is rounded, 1u, its reciprocal off by one in the last place, 2u, and S by 1u
+@pytest.mark.parametrize("kind", ["gelu", "silu"])
+def test_binary32_activations(kind):
+    """gelu.  Let u = 2^-24.  Further out than 1 Phi(-|x|) = e t S(t): 1 + p |x| is rounded, 1u, its reciprocal off by one in the last place, 2u, and S by 1u
     of its last sum and 1u of those before; the exponential by 2 in the last place, 4u, and 1u of its correction; two products 2u; the fit
     0.1u: 12u.  Nearer to 0 the sum 1/2 + x R is off by 1u of a half and 2u of x R, 3u of a Phi of 0.16 or more.  2^-20 is 16u, of Phi in f(x) and of
     Phi and x phi(x) in the slope.  Where |x| is 0.2 to 0.3 f(x) has one rounding of the sum and one of the product, each 1u at most and less than
-    0.6u in the mean square: 1u for both; the slope's two terms and their sum likewise."""
+    0.6u in the mean square: 1u for both; the slope's two terms and their sum likewise.
+    silu.  The exponential is off by 4u, the sum 1 + e, its reciprocal and the product by 1u each, the slope's factors by two more: 2^-20 covers them."""
     x = torch.from_numpy(gelu_points()).float().cuda()
     at = x.double().cpu().numpy()[None]
-    _, f, slope = (v[0] for v in ref.activation(at, "gelu", False))
-    y, _ = rt.activation(x, "gelu")
-    dx, again = rt.activation_backward(torch.ones_like(x), x, "gelu", want_y=True)
+    _, f, slope = (v[0] for v in ref.activation(at, kind, False))
+    y, _ = rt.activation(x, kind)
+    dx, again = rt.activation_backward(torch.ones_like(x), x, kind, want_y=True)
     assert torch.equal(again, y)
     x, y, dx = (v.double().cpu().numpy() for v in (x, y, dx))
     p = np.where(x == 0, 0.5, f / np.where(x == 0, 1.0, x))
     assert (np.abs(y - f) <= 2.0 ** -20 * np.abs(f)).all(), np.nanmax(np.abs(y - f) / np.abs(f)) * 2 ** 24
     size = p + np.abs(slope - p)
     assert (np.abs(dx - slope) <= 2.0 ** -20 * size).all(), np.max(np.abs(dx - slope) / size) * 2 ** 24
-    near = (np.abs(x) > 0.2) & (np.abs(x) < 0.3)
+    near = (np.abs(x) > 0.2) & (np.abs(x) < 0.3) & (kind == "gelu")
     for got, want in ((y, f), (dx, slope)):
-        assert np.sqrt(((got[near] / want[near] - 1) ** 2).mean()) <= 2.0 ** -24
+        assert not near.any() or np.sqrt(((got[near] / want[near] - 1) ** 2).mean()) <= 2.0 ** -24
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+def test_16_bit_activations_far_out(kind, dtype):
+    """f(x) of large negative x has as many bits as any other.  Let u = 2^-24.  The argument z of the exponential is rounded three times, 3 |z| u; the
+    exponential is off by 2 units in the last place, 4u, its reciprocal and what that is of by 3u, products by 4u, the fit of gelu by 78u: 2^-16 = 256u
+    covers |z| up to 55, 2^-15 up to 140; what is left is larger than exp(-55) = 2^-79 in the first case.  And half a step of the type."""
+    far = {"silu": 60.0, "gelu": 12.0, "gelu_tanh": 9.0}[kind]
+    x = torch.from_numpy(np.concatenate([gelu_points(), np.linspace(-far, far, 8193)])).clamp(-far, far).to(dtype).cuda()
+    _, f, slope = (v[0] for v in ref.activation(x.double().cpu().numpy()[None], kind, False))
+    y, _ = rt.activation(x, kind)
+    dx, again = rt.activation_backward(torch.ones_like(x), x, kind, want_y=True)
+    assert torch.equal(again, y)
+    x, y, dx = (v.double().cpu().numpy() for v in (x, y, dx))
+    p = np.where(x == 0, 0.5, f / np.where(x == 0, 1.0, x))
+    info = torch.finfo(dtype)
+    for got, want, size in ((y, f, np.abs(f)), (dx, slope, p + np.abs(slope - p))):
+        slack = np.where(size > 2.0 ** -70, 2.0 ** -16, 2.0 ** -15) * size
+        half = info.eps / 2 * (np.abs(want) + slack) + info.smallest_normal * info.eps / 2  # the second of what is below the normal numbers
+        assert (np.abs(got - want) <= slack + half).all(), (x[np.abs(got - want) > slack + half][:5], np.max(np.abs(got - want) / (slack + half)))
