@@ -31,7 +31,8 @@ def pack8(x: torch.Tensor) -> Rows8:
 
 
 def unpack8(rows8: Rows8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-    """What 8-bit rows stand for.  Every such value is one of bfloat16 and of float32."""
+    """What 8-bit rows stand for, rounded to dtype.  float32 holds every value that pack8 gives, bfloat16 those of blocks whose scale byte is at
+    least 3 (below, values are multiples of 2^-136 to 2^-134, and bfloat16's smallest number is 2^-133)."""
     return (training._native or _load()).unpack8(rows8, dtype)
 
 

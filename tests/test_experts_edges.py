@@ -89,3 +89,25 @@ def test_16_bit_activations_far_out(kind, dtype):
         slack = np.where(size > 2.0 ** -70, 2.0 ** -16, 2.0 ** -15) * size
         half = info.eps / 2 * (np.abs(want) + slack) + info.smallest_normal * info.eps / 2  # the second of what is below the normal numbers
         assert (np.abs(got - want) <= slack + half).all(), (x[np.abs(got - want) > slack + half][:5], np.max(np.abs(got - want) / (slack + half)))
+
+
+# ---- 8-bit rows -------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [64, 61])
+def test_smallest_rows_in_each_type(cols):
+    """Every code with every scale byte that leaves bfloat16's numbers, rounded once to the type; float32 holds them all."""
+    codes = torch.arange(256, dtype=torch.int32).repeat(1 + cols * 12 // 256)[:cols * 12].to(torch.uint8).view(12, cols)
+    scales = torch.arange(12, dtype=torch.uint8).repeat_interleave((cols + 31) // 32).view(12, -1)
+    rows = rt.Rows8(codes.view(torch.float8_e4m3fn).cuda(), scales.view(torch.float8_e8m0fnu).cuda())
+    want = ref.unpacked(rows)
+    got = rt.unpack8(rows, F)
+    assert np.array_equal(got.double().cpu().numpy(), want, equal_nan=True)
+    for dtype in (BF, HF):
+        exact = torch.from_numpy(want).float().to(dtype)
+        assert torch.equal(rt.unpack8(rows, dtype).cpu().nan_to_num(7.0), exact.nan_to_num(7.0))
+    place = torch.arange(12, dtype=torch.int32).view(12, 1).cuda()
+    spread = rt.spread_tokens(rows, place, torch.tensor([0, 12], device="cuda"))
+    assert torch.equal(spread.cpu().nan_to_num(7.0), torch.from_numpy(want).float().to(BF).nan_to_num(7.0))
+    fine = scales[:, 0] >= 3
+    assert np.array_equal(rt.unpack8(rows).double().cpu().numpy()[fine], want[fine], equal_nan=True)
+    assert not np.array_equal(rt.unpack8(rows).double().cpu().numpy()[0], want[0], equal_nan=True)
