@@ -134,7 +134,7 @@ PyObject* route(PyObject* const* a) {  // logits, k, scores, bias, groups, group
   if (!(p.scale - p.scale == 0.0f)) value_error("scale is a finite float32 number");
   const c10::cuda::CUDAGuard guard(logits.device());
   const std::vector<int64_t> size = with_cols(logits.sizes(), k);
-  const auto [experts, weights] = two_of(size, at::kInt, size, at::kFloat, logits);
+  const auto [experts, weights] = two_if_small(size, at::kInt, size, at::kFloat, logits);
   check(regtopk_route(logits.data_ptr(), in.ld, static_cast<const float*>(data(bias)), static_cast<int32_t*>(experts.data_ptr()),
                       static_cast<float*>(weights.data_ptr()), in.rows, most, k, type, &p, stream_of(logits)), "regtopk_route");
   return Py_BuildValue("NN", THPVariable_Wrap(experts), THPVariable_Wrap(weights));
@@ -170,7 +170,7 @@ PyObject* sort_tokens(PyObject* const* a) {  // experts, n_experts, workers
   const int64_t tokens = tokens_of(experts);
   if (static_cast<int64_t>(n) * workers > REGTOPK_MATMUL_MAX_GROUPS) check(REGTOPK_ERR_TOO_LARGE, "regtopk_sort_tokens");
   const c10::cuda::CUDAGuard guard(experts.device());
-  const auto [offsets, place] = two_of({static_cast<int64_t>(n) * workers + 1}, at::kLong, experts.sizes(), at::kInt, experts);
+  const auto [offsets, place] = two_if_small({static_cast<int64_t>(n) * workers + 1}, at::kLong, experts.sizes(), at::kInt, experts);
   const size_t bytes = regtopk_sort_tokens_workspace_bytes(tokens, k, n, workers);
   Tensor ws;
   if (bytes) ws = empty({static_cast<int64_t>(bytes)}, at::kByte, experts);
@@ -328,9 +328,9 @@ PyObject* rms_norm(PyObject* const* a) {  // x, weight, eps, residual, want_y, w
   if (wants_y) y = empty(x.sizes(), x.scalar_type(), x);
   NewPacked p{};
   if (wants_y8) p = new_packed(x.sizes(), x, 1);
-  Tensor h = x, rstd;  // kept together for the backward pass
+  Tensor h = x, rstd;
   const auto stats = x.sizes().slice(0, x.dim() - 1);
-  if (residual) std::tie(h, rstd) = two_of(x.sizes(), residual->scalar_type(), stats, at::kFloat, x);
+  if (residual) std::tie(h, rstd) = two_if_small(x.sizes(), residual->scalar_type(), stats, at::kFloat, x);
   else rstd = empty(stats, at::kFloat, x);
   check(regtopk_rms_norm(x.data_ptr(), in.ld, data(residual), res.ld, weight, static_cast<float>(number(a[2])), wants_y ? y.data_ptr() : nullptr, in.cols,
                          wants_y8 ? p.v() : nullptr, p.ld_values, wants_y8 ? p.s() : nullptr, p.ld_scales, residual ? h.data_ptr() : nullptr, in.cols,

@@ -111,3 +111,22 @@ def test_smallest_rows_in_each_type(cols):
     fine = scales[:, 0] >= 3
     assert np.array_equal(rt.unpack8(rows).double().cpu().numpy()[fine], want[fine], equal_nan=True)
     assert not np.array_equal(rt.unpack8(rows).double().cpu().numpy()[0], want[0], equal_nan=True)
+
+
+# ---- outputs ----------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_large_outputs_live_on_their_own():
+    """Who keeps one of a call's outputs does not keep the others, once they are larger than a megabyte together."""
+    def alone(*tensors):
+        for t in tensors:
+            assert t.untyped_storage().nbytes() == t.nbytes
+    x, stream, w = torch.randn(1200, 512, device="cuda").to(BF), torch.randn(1200, 512, device="cuda"), torch.ones(512, device="cuda")
+    y, y8, h, rstd = rt.rms_norm(x, w, residual=stream, want_y8=True)
+    alone(y, h, rstd)
+    experts, weights = rt.route(torch.randn(70_000, 8, device="cuda"), 2)
+    alone(experts, weights)
+    alone(*rt.sort_tokens(experts.view(-1, 1).repeat(1, 2), 8))
+    alone(*rt.rms_norm_backward(y, h, rstd, w))
+    alone(*rt.join_tokens_backward(y, torch.randn(2400, 512, device="cuda").to(BF), torch.arange(2400, dtype=torch.int32, device="cuda").view(1200, 2),
+                                   torch.ones(1200, 2, device="cuda"), torch.tensor([0, 2400], device="cuda")))
+    alone(*rt.activation_backward(y, x, want_y=True))
