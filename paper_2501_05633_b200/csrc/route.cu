@@ -690,16 +690,18 @@ template <typename T> __global__ void __launch_bounds__(kRouteThreads) k_route_b
 // warp.  Where a pair goes: to the start of its group, past the pairs of the group in the chunks before, in the runs before and in its own
 // run, which a warp goes through in steps of 32.  Nothing depends on the order in which blocks or warps run.
 //   Up to 4,096 pairs: one block.  Up to 16,384: a cluster of eight, which read one another's counts in shared memory.  More: k_sort_count
-//   counts the chunks first.
+//   counts the chunks first, and every block adds up the counts of all of them, 128 at most.  Above 1 million pairs k_sort_scan adds them up once for
+//   all blocks, because that sum would grow with the square of the pairs (2^31 of them: 65,536 blocks, 65,536 chunks each): 4 million pairs in
+//   256 groups take 84 us (147 us with a sum in every block), 134 million 2.3 ms.
 // It is latency that these take: two reads from memory one after the other (experts, and workers beside them), barriers, one write.  3,000
-// pairs 6 us, 65,536 pairs some 10 us in two launches (a cluster of eight with 8,192 pairs a block: 14.6 us, most of it for comparing the
-// groups of 32 neighbours).
+// pairs 6 us, 65,536 pairs in two launches 7 us over 8 groups and 10 us over 256 (with cold caches 12.5 us, and a cluster of eight with 8,192 pairs a
+// block 14.6 us, most of it for comparing the groups of 32 neighbours).
 struct SortArgs {
   const int32_t* experts;
   const int64_t* workers_at;  // NULL: all tokens are of worker 0
   int64_t* offsets;
   int32_t* place;
-  u32* counts;  // [chunks][groups]
+  u32* counts;  // [chunks][groups]; of long sorts what lies in the chunks before, and [chunks]: the groups' sizes
   int64_t tokens, pairs;
   Divisor k;
   int workers, n_experts, groups, chunk, chunks;
@@ -744,6 +746,33 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const __grid_consta
   for (int g = threadIdx.x; g < a.groups; g += kSortThreads) a.counts[(int64_t)blockIdx.x * a.groups + g] = count[g];
 }
 
+// The counts of every chunk become the sums over the chunks before it, and the groups' sizes follow the last.  A block has 32 groups, which
+// are neighbours in memory, and a warp one of 32 runs of chunks.
+__global__ void __launch_bounds__(kSortThreads) k_sort_scan(const __grid_constant__ SortArgs a) {
+  __shared__ u32 sums[kSortWarps][32];
+  begin_after_predecessor();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = blockIdx.x * 32 + lane;
+  const int length = (a.chunks + kSortWarps - 1) / kSortWarps, first = min(warp * length, a.chunks), end = min(first + length, a.chunks);
+  u32 sum = 0;
+  if (g < a.groups) {
+#pragma unroll 8
+    for (int c = first; c < end; ++c) sum += a.counts[(int64_t)c * a.groups + g];
+  }
+  sums[warp][lane] = sum;
+  __syncthreads();
+  u32 before = 0;
+  for (int w = 0; w < warp; ++w) before += sums[w][lane];
+  if (g >= a.groups) return;
+#pragma unroll 8
+  for (int c = first; c < end; ++c) {
+    u32* at = a.counts + (int64_t)c * a.groups + g;
+    const u32 n = *at;
+    *at = before;
+    before += n;
+  }
+  if (warp == kSortWarps - 1) a.counts[(int64_t)a.chunks * a.groups + g] = before;
+}
+
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ u32 load_of_block(const u32* own, u32 block) {  // what lies at this place in another block's shared memory
@@ -754,7 +783,7 @@ __device__ __forceinline__ u32 load_of_block(const u32* own, u32 block) {  // wh
 }
 
 // How the chunks of a sort know of one another.
-enum Chunks { kOneBlock, kOneCluster, kCountedBefore, kCountedLong };  // kCountedLong: runs of more than kSortKept steps
+enum Chunks { kOneBlock, kOneCluster, kCountedBefore, kCountedLong };  // kCountedLong: runs of more than kSortKept steps, counts that are sums
 
 // dynamic shared memory: workers_at; of each group its size and what lies before it [2][groups], then runs [warps][groups]
 template <int CHUNKS> __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a) {
@@ -791,7 +820,13 @@ template <int CHUNKS> __global__ void __launch_bounds__(kSortThreads) k_sort_pla
     __syncwarp();
   }
   // the sums over chunks that have been counted before, by as many threads a group as there are
-  if (CHUNKS == kCountedBefore || CHUNKS == kCountedLong) {
+  if (CHUNKS == kCountedLong) {
+    for (int g = threadIdx.x; g < a.groups; g += kSortThreads) {
+      sizes[g] = a.counts[(int64_t)a.chunks * a.groups + g];
+      base[g] = a.counts[(int64_t)blockIdx.x * a.groups + g];
+    }
+  }
+  if (CHUNKS == kCountedBefore) {
     const int parts = a.groups >= kSortThreads ? 1 : kSortThreads / a.groups;
     for (int i = threadIdx.x; i < parts * a.groups; i += kSortThreads) {
       const int part = i / a.groups, g = i - part * a.groups;
@@ -886,7 +921,7 @@ template <int CHUNKS> __global__ void __launch_bounds__(kSortThreads) k_sort_pla
 }
 
 // Pairs of a chunk.
-constexpr int64_t kMostOfBlock = 4096, kMostOfCluster = (int64_t)kSortCluster * 2 * kSortThreads;
+constexpr int64_t kMostOfBlock = 4096, kMostOfCluster = (int64_t)kSortCluster * 2 * kSortThreads, kMostKept = kSortKept * kSortThreads;
 inline int chunk_of(int64_t pairs) {
   if (pairs <= kMostOfBlock) return (int)kMostOfBlock;
   if (pairs <= kMostOfCluster) return (int)((pairs + kSortCluster - 1) / kSortCluster);
@@ -1014,7 +1049,7 @@ int regtopk_route_backward(const float* dweights, const void* logits, int64_t ld
 size_t regtopk_sort_tokens_workspace_bytes(int64_t tokens, int32_t k, int32_t n_experts, int32_t workers) {
   if (tokens < 0 || k < 1 || n_experts < 1 || workers < 1 || tokens > INT32_MAX / k || (int64_t)n_experts * workers > REGTOPK_MATMUL_MAX_GROUPS) return 0;
   const int64_t pairs = tokens * k, chunk = chunk_of(pairs);
-  return pairs <= kMostOfCluster ? 0 : (size_t)((pairs + chunk - 1) / chunk) * n_experts * workers * sizeof(u32);
+  return pairs <= kMostOfCluster ? 0 : (size_t)((pairs + chunk - 1) / chunk + (chunk > kMostKept)) * n_experts * workers * sizeof(u32);
 }
 
 int regtopk_sort_tokens(const int32_t* experts, const int64_t* workers_at, int32_t workers, int64_t* offsets, int32_t* place,
@@ -1037,7 +1072,7 @@ int regtopk_sort_tokens(const int32_t* experts, const int64_t* workers_at, int32
   int dev, sms;
   if (!current_device(&dev, &sms)) return REGTOPK_ERR_NO_DEVICE;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const bool is_long = a.chunk > kSortKept * kSortThreads;
+  const bool is_long = a.chunk > kMostKept;
   const size_t bytes = sort_smem(a.groups, workers), most = sort_smem(REGTOPK_MATMUL_MAX_GROUPS, REGTOPK_MATMUL_MAX_GROUPS);
   if (!counted) {
     if (a.pairs > kMostOfBlock) {
@@ -1054,6 +1089,8 @@ int regtopk_sort_tokens(const int32_t* experts, const int64_t* workers_at, int32
     return start(k_sort_place<kCountedBefore>, a.chunks, kSortThreads, bytes, s, a);
   }
   if (!allow_smem_of<k_sort_place<kCountedLong>>(dev, (int)most)) return train_rc(cudaGetLastError());
+  const int scanned = start(k_sort_scan, (a.groups + 31) / 32, kSortThreads, 0, s, a);
+  if (scanned != REGTOPK_OK) return scanned;
   return start(k_sort_place<kCountedLong>, a.chunks, kSortThreads, bytes, s, a);
 }
 

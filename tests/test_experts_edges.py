@@ -130,3 +130,26 @@ def test_large_outputs_live_on_their_own():
     alone(*rt.join_tokens_backward(y, torch.randn(2400, 512, device="cuda").to(BF), torch.arange(2400, dtype=torch.int32, device="cuda").view(1200, 2),
                                    torch.ones(1200, 2, device="cuda"), torch.tensor([0, 2400], device="cuda")))
     alone(*rt.activation_backward(y, x, want_y=True))
+
+
+# ---- the order of groups ----------------------------------------------------------------------------------------------
+def test_workspace_of_the_longest_sort():
+    """A row of counts for every chunk of 32,768 pairs and one of the groups' sizes: nothing grows with the square of the pairs."""
+    need = ref.c_library().regtopk_sort_tokens_workspace_bytes
+    assert need(2**31 - 1, 1, 256, 8) == (65536 + 1) * 2048 * 4 and need(1 << 20, 1, 100, 1) == 128 * 100 * 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pairs,n,workers", [(1_500_001, 2048, 1), (10_000_001, 60, 3), (70_000_003, 33, 1), (4_300_000, 1, 1)])
+def test_sort_of_many_chunks(pairs, n, workers):
+    """Chunks whose counts are added up once for all blocks."""
+    gen = torch.Generator(device="cuda").manual_seed(pairs)
+    experts = torch.randint(-1, n, (pairs, 1), generator=gen, dtype=torch.int32, device="cuda")
+    at = torch.tensor([pairs * i // workers for i in range(workers + 1)], device="cuda")
+    offsets, place = rt.sort_tokens(experts, n, at)
+    worker = torch.searchsorted(at, torch.arange(pairs, device="cuda"), right=True) - 1
+    key = torch.where(experts.flatten() < 0, workers * n, worker * n + experts.flatten())
+    assert torch.equal(offsets, torch.cat([key.new_zeros(1), key.bincount(minlength=workers * n + 1)[:-1].cumsum(0)]))
+    order = key.argsort(stable=True)[: int(offsets[-1])]
+    assert torch.equal(place.flatten()[order].long(), torch.arange(len(order), device="cuda"))
+    assert bool((place.flatten()[key == workers * n] == -1).all())
