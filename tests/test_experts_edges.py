@@ -37,6 +37,57 @@ def test_groups_with_numbers_that_are_not_finite(groups, kept, scores, dtype):
                 assert (e >= 0).all(), "a masked group was kept before one with NaN"
 
 
+def hard_tokens(tokens, experts, dtype, gen):
+    """Every seventh token is one that the choice has to take care with: ties, neighbours, masks, numbers that are not finite."""
+    logits = (1.5 * torch.randn(tokens, experts, generator=gen)).to(dtype)
+    at = torch.arange(0, tokens, 7)
+    for kind in range(8):
+        t = at[kind::8]
+        if kind == 0:
+            logits[t] = (torch.randint(-3, 3, (len(t), experts), generator=gen) / 4).to(dtype)
+        elif kind == 1:
+            logits[t] = (logits[t].float().round() + torch.randint(0, 9, (len(t), experts), generator=gen) * 2.0 ** -22).to(dtype)
+        elif kind == 2:
+            logits[t, : experts // 2] = -INF
+        elif kind == 3:
+            logits[t] = -INF
+        elif kind == 4:
+            logits[t, 1:] = -INF
+        elif kind == 5:
+            logits[t] = torch.finfo(dtype).min
+        else:
+            logits[t, torch.randint(0, experts, (len(t),), generator=gen)] = float("nan") if kind == 6 else INF
+    return logits, at
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("experts,k,groups,kept,top", [(256, 8, 8, 4, 2), (256, 1, 1, 1, 1), (60, 2, 1, 1, 1), (8, 2, 1, 1, 1), (128, 32, 4, 2, 1), (512, 8, 1, 1, 1),
+                                                       (510, 4, 17, 5, 2), (96, 5, 3, 2, 2)])
+def test_route_of_many_tokens_a_warp(experts, k, groups, kept, top, dtype):
+    """Eleven tokens for every warp that the device holds, which takes up to eight at a time and has three left; the last warp has fewer.  Equal to calls of
+    few tokens, where a warp has one, and to the definition."""
+    gen = torch.Generator().manual_seed(experts + k)
+    each = experts // groups  # a group's experts, of which a lane has `in_lane`
+    lanes = 32 >> max(0, (groups - 1).bit_length())
+    in_lane = -(-each // lanes)
+    warps = torch.cuda.get_device_properties(0).multi_processor_count * 8 * (4 if in_lane <= 8 else 2)
+    tokens = 11 * warps - 5
+    logits, at = hard_tokens(tokens, experts, dtype, gen)
+    bias = (0.1 * torch.randn(experts, generator=gen)).cuda()
+    seen = torch.cat([at[torch.randperm(len(at), generator=gen)[:150]], torch.randint(0, tokens, (50,), generator=gen), torch.arange(tokens - 12, tokens)])
+    logits = logits.cuda()
+    for scores, b, renormalise in (("sigmoid", bias, True), ("softmax", bias, False), ("softmax", None, True), ("softmax", None, False), ("sigmoid", None, False)):
+        a = dict(scores=scores, bias=b, groups=groups, groups_kept=kept, group_top=top, renormalise=renormalise, scale=2.5)
+        experts_of, weights = rt.route(logits, k, **a)
+        for first in range(0, tokens, warps):
+            e, w = rt.route(logits[first:first + warps], k, **a)
+            assert torch.equal(experts_of[first:first + warps], e)
+            assert torch.equal(weights[first:first + warps].nan_to_num(9.0), w.nan_to_num(9.0))
+        few, w = check_route(logits[seen.cuda()], k, **a)
+        assert torch.equal(experts_of[seen.cuda()], few) and torch.equal(weights[seen.cuda()].nan_to_num(9.0), w.nan_to_num(9.0))
+
+
 # ---- activations ------------------------------------------------------------------------------------------------------
 def gelu_points():
     """Both signs, far out, and around 0."""
