@@ -5,6 +5,7 @@ import torch
 
 import paper_2501_05633_b200 as rt
 from tests import experts_reference as ref
+from tests import test_experts_norm as norm
 from tests.test_experts_route import check_route
 
 BF, HF, F = torch.bfloat16, torch.float16, torch.float32
@@ -204,3 +205,18 @@ def test_sort_of_many_chunks(pairs, n, workers):
     order = key.argsort(stable=True)[: int(offsets[-1])]
     assert torch.equal(place.flatten()[order].long(), torch.arange(len(order), device="cuda"))
     assert bool((place.flatten()[key == workers * n] == -1).all())
+
+
+# ---- the norm ---------------------------------------------------------------------------------------------------------
+# More rows than teams on a device of 148 multiprocessors, so that rows come through the rings: one, two and more warps a row, one to four units a
+# warp, rows that are kept in registers and rows that are read twice, aligned or not.  Fewer than 60 additions in a row to a weight's gradient.
+MANY_ROWS = [(4001, 96), (3700, 250), (2501, 768), (2502, 767), (1902, 1024), (1901, 1023), (700, 2048), (621, 4096), (620, 4095), (301, 8192), (200, 8200), (180, 16383), (181, 16384)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,stream", norm.TYPES)
+@pytest.mark.parametrize("rows,cols", MANY_ROWS)
+def test_norm_of_many_rows(rows, cols, dtype, stream):
+    norm.test_forward(rows, cols, dtype, stream)
+    norm.test_backward(rows, cols, dtype, stream)
+    rt.training_status()
