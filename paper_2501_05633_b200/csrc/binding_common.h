@@ -133,9 +133,9 @@ void written(const Tensor& t, const char* name) {
   t.unsafeGetTensorImpl()->bump_version();
 }
 // Refuses an output that shares memory with an input, where torch can tell.  `same`: it may be the very input.
-void apart(const Tensor& out, const Tensor& in, const char* name, bool same = false) {
+void apart(const Tensor& out, const Tensor& in, const char* name, bool same = false, const char* out_name = "out") {
   const at::MemOverlapStatus how = at::get_overlap_status(out, in);
-  if (how == at::MemOverlapStatus::Partial || (how == at::MemOverlapStatus::Full && !same)) value_error(std::string("out and ") + name + " overlap");
+  if (how == at::MemOverlapStatus::Partial || (how == at::MemOverlapStatus::Full && !same)) value_error(std::string(out_name) + " and " + name + " overlap");
 }
 const float* vector_of(const Tensor& t, int64_t n, const Tensor& x, const char* name) {
   if (t.device() != x.device() || t.scalar_type() != at::kFloat || t.numel() != n || !t.is_contiguous())

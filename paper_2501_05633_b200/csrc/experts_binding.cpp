@@ -307,11 +307,6 @@ PyObject* activation_backward(PyObject* const* a) {  // dy, kept, kind, gated, w
   return Py_BuildValue("NN", THPVariable_Wrap(da), wants_y ? THPVariable_Wrap(y) : Py_NewRef(Py_None));
 }
 
-bool overlap(const Tensor& out, const Tensor& in) {
-  const at::MemOverlapStatus how = at::get_overlap_status(out, in);
-  return how == at::MemOverlapStatus::Partial || how == at::MemOverlapStatus::Full;
-}
-
 // ---- the norm ---------------------------------------------------------------------------------------------------------
 PyObject* rms_norm(PyObject* const* a) {  // x, weight, eps, residual, want_y, want_y8
   const Tensor& x = tensor(a[0], "x");
@@ -360,9 +355,8 @@ PyObject* rms_norm_backward(PyObject* const* a) {  // dy, h, rstd, weight, dh, o
     if (given->device() != dy.device() || given->scalar_type() != at::kFloat || given->dim() != 2 || given->size(0) != groups || given->size(1) != in.cols)
       type_error("dweight must be float32 [" + std::to_string(groups) + ", " + std::to_string(in.cols) + "] on the input's device");
     ld = rows_of(*given, "dweight").ld;
-    for (const Tensor* in : {&dy, &h, &tensor(a[2], "rstd"), &tensor(a[3], "weight")})
-      if (overlap(*given, *in)) value_error("dweight and an input overlap");
-    if (dh && overlap(*given, *dh)) value_error("dweight and dh overlap");
+    for (const Tensor* in : {&dy, &h, &tensor(a[2], "rstd"), &tensor(a[3], "weight"), dh})
+      if (in) apart(*given, *in, "an input", false, "dweight");
     written(*given, "dweight");
   }
   const c10::cuda::CUDAGuard guard(dy.device());
