@@ -3,7 +3,10 @@
 //
 // A token's logits are a few hundred numbers, so that a warp keeps them in registers and chooses by comparing there; the logits are
 // read once.  What bounds the choice is the issue of instructions, not the memory: 32,768 tokens, eight of 256 experts by sigmoid scores with a
-// bias in four of eight groups, take 37 to 39 us, 720 instructions of a warp a token, where 34 MB take 5.4 us; by bfloat16 logits alone 20 us.
+// bias in four of eight groups, take 36 to 39 us, 720 instructions of a warp a token, where 34 MB take 5.4 us; by bfloat16 logits alone 20 us.
+// That is with numbers of which few are close.  Where equal ones are ordinary, tokens are worked out again in binary64, one after the other in their
+// warp: bfloat16 logits with a bias of zeros 82 us, with one of multiples of 0.001 45 us, and where all logits are equal, as in a router that
+// has not been trained, 215 to 228 us with a bias and 20 us without one.
 
 #include <float.h>
 
