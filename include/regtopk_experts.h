@@ -55,7 +55,8 @@ typedef struct {
  *   experts[t]: the k experts with the largest c among those, in descending order
  *   weights[t]: their s, divided by the sum of them if renormalise, times scale
  * Ties go to the lower index, of groups and of experts.  The choice is that of binary64 arithmetic on the given numbers: tokens among
- * whose numbers binary32 cannot tell two apart are done again in it (without bias experts are compared by their logits).  An expert whose logit or c is
+ * whose numbers binary32 cannot tell two apart are done again in it (without bias experts are compared by their logits); exponentials of less than
+ * -708 are 0 there.  An expert whose logit or c is
  * -infinity is never chosen; places for which no expert is left hold -1 and weight 0.  A NaN or +infinity among the logits
  * makes the token's softmax scores NaN; NaN is the least c that can be chosen, and counts as -1e300 in the sum of a group.
  * logits [tokens][n_experts] of `type`; bias [n_experts] binary32; experts int32 and weights binary32, [tokens][k] contiguous.
@@ -104,8 +105,9 @@ int regtopk_join_tokens_backward(const void* dout, int64_t ld_dout, const void* 
 
 /* silu(x) = x / (1 + exp(-x));  gelu(x) = x Phi(x), Phi the normal distribution's;  gelu_tanh: Phi approximated by
  * (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2.
- * How good they are: f(x) / x and the terms p and x p'(x) of the slope, p = f(x) / x, are right to 2^-16 relative for 16-bit types (2^-15 below 2^-70; before they are
- * rounded to the type, by 2^-9 or 2^-12) and for gelu_tanh in binary32, to 2^-20 for silu and gelu in binary32; below 2^-120 results may be 0. */
+ * How good they are: p = f(x) / x and the terms p and x p'(x) of the slope are right to 2^-20 relative for silu and gelu in binary32; for gelu_tanh in
+ * binary32, and for 16-bit types before they are rounded to the type (by 2^-9 or 2^-12), to 2^-16, and to 2^-15 where p is below 2^-40.  A p of less
+ * than 2^-125 may be 0. */
 enum { REGTOPK_ACTIVATION_SILU = 0, REGTOPK_ACTIVATION_GELU = 1, REGTOPK_ACTIVATION_GELU_TANH = 2 };
 
 /* y = f(a), a [rows][cols]; gated != 0: y = f(a[:, :cols]) * a[:, cols:], a [rows][2 cols].  y [rows][cols]; both of `type`.

@@ -14,7 +14,7 @@ constexpr int kActThreads = 256;
 
 // ---- f(x) = x p(x) and its slope ---------------------------------------------------------------------------------
 // FAST, for 16-bit types: exponentials and reciprocals are the hardware's approximations, and the argument of an exponential is rounded, which
-// 2^-16 of the result covers down to 2^-120; the types' own rounding is 2^-9 and 2^-12.
+// 2^-16 of p covers down to 2^-40, 2^-15 further down; the types' own rounding is 2^-9 and 2^-12.
 
 // p = 1 / (1 + exp(-x)) and q = 1 - p, without cancellation; an infinite exponential gives 0 and 1.
 template <bool FAST> __device__ __forceinline__ void logistic(float x, float& p, float& q) {
