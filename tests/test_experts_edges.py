@@ -221,6 +221,29 @@ def test_sort_of_many_chunks(pairs, n, workers):
     assert bool((place.flatten()[key == workers * n] == -1).all())
 
 
+@pytest.mark.gpu
+def test_long_sorts_captured_and_at_once():
+    """Three launches and a workspace: two captured graphs, replayed on other inputs and on two streams at once, give what calls give."""
+    n, made = 256, [torch.randint(-1, 256, (1_300_007, 1), dtype=torch.int32, device="cuda") for _ in range(4)]
+    want = [rt.sort_tokens(e, n) for e in made]
+    graphs = []
+    for _ in range(2):
+        into, g = made[0].clone(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = rt.sort_tokens(into, n)
+        graphs.append((into, g, out, torch.cuda.Stream()))
+    for first in (0, 2):
+        for i, (into, g, out, stream) in enumerate(graphs):
+            into.copy_(made[first + i])
+            stream.wait_stream(torch.cuda.current_stream())
+        for into, g, out, stream in graphs:
+            with torch.cuda.stream(stream):
+                g.replay()
+        torch.cuda.synchronize()
+        for i, (into, g, out, stream) in enumerate(graphs):
+            assert torch.equal(out[0], want[first + i][0]) and torch.equal(out[1], want[first + i][1])
+
+
 # ---- the norm ---------------------------------------------------------------------------------------------------------
 # More rows than teams on a device of 148 multiprocessors, so that rows come through the rings: one, two and more warps a row, one to four units a
 # warp, rows that are kept in registers and rows that are read twice, aligned or not.  Fewer than 60 additions in a row to a weight's gradient.
